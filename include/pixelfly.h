@@ -319,6 +319,60 @@ pf_status pf_linear_fwd(const pf_layout *layout, pf_dtype dtype, int64_t T,
                         pf_epilogue epi, void *Y_pre, void *workspace,
                         size_t ws_bytes, void *stream);
 
+/* Activations of pf_linear_fwd_act; s(y) = 1 / (1 + exp(-y)). */
+typedef enum {
+  PF_ACT_NONE = 0,
+  PF_ACT_GELU = 1,      /* exact (erf) GELU, as PF_EPI_GELU                       */
+  PF_ACT_GELU_TANH = 2, /* z s(2 sqrt(2 / pi) (z + 0.044715 z^3)): the tanh form  */
+  PF_ACT_SILU = 3,      /* z s(z)                                                 */
+  PF_ACT_RELU = 4
+} pf_activation;
+
+/*
+ * Forward with bias, activation and residual in the epilogue (a layer as a
+ * Transformer block has it):
+ *     Z = X (M o W)^T + T_lr U^T + bias         (T_lr = X V^T, as pf_linear_fwd)
+ *     Y = residual + act(Z)                     (T x N)
+ * bias: N elements, residual: T x N, both of the call's dtype; either may be
+ * NULL (zero).  Y_pre (T x N) receives Z for the backward; NULL keeps none
+ * (serving), and with PF_ACT_NONE it must be NULL.  The sums, the activation
+ * and the residual's addition are fp32; Y and Y_pre are rounded once each.
+ * residual may be Y itself (Y += act(Z) in place); no other buffers may
+ * overlap.  The mixed form takes gamma as pf_linear_fwd_mixed does.
+ * Way back: pf_linear_act_bwd, then pf_linear_bwd_data and
+ * pf_linear_bwd_weight with dY_pre for their dY; the residual's gradient is
+ * dY itself.  Everything else as pf_linear_fwd.
+ * Errors: INVALID_ARG, UNSUPPORTED, STATE, WORKSPACE, HIP.
+ */
+pf_status pf_linear_fwd_act(const pf_layout *layout, pf_dtype dtype, int64_t T, int32_t r,
+                            const void *X, const void *Wblk, const void *U, const void *V,
+                            const void *bias, pf_activation act, const void *residual, void *Y,
+                            void *Y_pre, void *T_lr, void *workspace, size_t ws_bytes,
+                            void *stream);
+pf_status pf_linear_fwd_act_mixed(const pf_layout *layout, pf_dtype dtype, int64_t T, int32_t r,
+                                  float gamma, const void *X, const void *Wblk, const void *U,
+                                  const void *V, const void *bias, pf_activation act,
+                                  const void *residual, void *Y, void *Y_pre, void *T_lr,
+                                  void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Backward of that epilogue, T x N (N a multiple of 32):
+ *     dY_pre = dY o act'(Y_pre)
+ *     dbias  = column sums of dY_pre (N elements of the call's dtype)
+ * in one pass; the sums take the unrounded products, in fp32 and a fixed
+ * order.  dbias may be NULL (no bias).  With PF_ACT_NONE, dY_pre = dY: Y_pre
+ * and dY_pre must be NULL and dbias must be given.  dY_pre may be dY or Y_pre
+ * itself.  Needs a workspace of pf_linear_act_workspace_bytes when dbias is
+ * given.  Errors: INVALID_ARG, WORKSPACE, HIP.
+ */
+pf_status pf_linear_act_bwd(pf_dtype dtype, int64_t T, int64_t N, pf_activation act, const void *dY,
+                            const void *Y_pre, void *dY_pre, void *dbias, void *workspace,
+                            size_t ws_bytes, void *stream);
+
+/* Workspace bytes of pf_linear_act_bwd with dbias (0 on invalid arguments, or
+ * when it needs none). */
+size_t pf_linear_act_workspace_bytes(pf_dtype dtype, int64_t T, int64_t N);
+
 /*
  * Backward-data (gradient of the layer w.r.t. its input):
  *     S  = dY U                         (T x r, saved for bwd_weight)
@@ -486,7 +540,7 @@ typedef enum {
   PF_KERNEL_LOWRANK_S = 4,      /* rank-r product S = dY U */
   PF_KERNEL_REDUCE = 5,         /* sums of split partial results; the b = 32
                                    backward-data pair-block gather */
-  PF_KERNEL_GELU_BWD = 6,       /* standalone GELU backward */
+  PF_KERNEL_GELU_BWD = 6,       /* standalone GELU backward, pf_linear_act_bwd */
   PF_KERNEL_ATTN_FWD = 7,
   PF_KERNEL_ATTN_BWD_DQ = 8,    /* dQ (and the row terms delta) */
   PF_KERNEL_ATTN_BWD_DKV = 9,   /* dK, dV */

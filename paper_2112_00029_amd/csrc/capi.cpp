@@ -1,20 +1,11 @@
 // C ABI of libpixelfly.so: argument validation (all before any enqueue) and
 // dispatch to the HIP kernels.  See include/pixelfly.h for the contract.
-#include <hip/hip_runtime_api.h>
+#include "capi.h"
 
-#include <algorithm>
 #include <cmath>
-#include <atomic>
 #include <cstdio>
 #include <cstring>
-#include <mutex>
 #include <new>
-#include <string>
-#include <vector>
-
-#include "layout.h"
-#include "pf_internal.h"
-#include "pixelfly.h"
 
 namespace pf {
 LaunchEvents &next_launch_events() {
@@ -29,89 +20,16 @@ int tn_items_total(const TNArgs &a, int blk, int tile) {
     n += ((a.dr[r].na_blk + GT - 1) / GT) * ((a.dr[r].nb_blk + GT - 1) / GT);
   return n;
 }
+
+namespace capi {
+thread_local std::string g_err;
+KernelTimer g_kt;
+}  // namespace capi
 }  // namespace pf
 
+using namespace pf::capi;
+
 namespace {
-
-thread_local std::string g_err;
-
-pf_status fail(pf_status s, const std::string &msg) {
-  g_err = msg;
-  return s;
-}
-
-bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
-
-// Kernel timing hook (pf_timing_begin / pf_timing_end): per kernel class,
-// event pairs recorded around the next `cap` launches.
-struct KernelTimer {
-  std::mutex mu;
-  std::atomic<int> armed{0};
-  int cap = 0;
-  std::vector<hipEvent_t> ev[PF_KERNEL_COUNT];  // 2 * cap each: start, end
-  int n[PF_KERNEL_COUNT] = {};
-
-  void release() {
-    for (auto &v : ev) {
-      for (hipEvent_t e : v)
-        if (e) (void)hipEventDestroy(e);
-      v.clear();
-    }
-    std::fill(n, n + PF_KERNEL_COUNT, 0);
-    cap = 0;
-  }
-};
-KernelTimer g_kt;
-
-// Scope around one kernel launch: when the hook is armed and the class has
-// room, hands the next launch a pair of events (recorded by the dispatch at
-// the kernel's start and end) and counts it if the launch took them.
-class Timed {
- public:
-  Timed(pf_kernel_class k, hipStream_t) : k_(k) {
-    if (!g_kt.armed.load(std::memory_order_acquire) || g_kt.n[k] >= g_kt.cap) return;
-    pf::next_launch_events() = {g_kt.ev[k][2 * g_kt.n[k]], g_kt.ev[k][2 * g_kt.n[k] + 1]};
-    on_ = true;
-  }
-  ~Timed() {
-    if (!on_) return;
-    pf::LaunchEvents &e = pf::next_launch_events();
-    if (!e.start) g_kt.n[k_]++;  // consumed by a launch
-    e.start = e.stop = nullptr;
-  }
-  Timed(const Timed &) = delete;
-  Timed &operator=(const Timed &) = delete;
-
- private:
-  pf_kernel_class k_;
-  bool on_ = false;
-};
-
-pf_status need_ptr(const void *p, const char *name) {
-  if (!p) return fail(PF_ERR_INVALID_ARG, std::string(name) + " is NULL");
-  if (!aligned16(p))
-    return fail(PF_ERR_INVALID_ARG, std::string(name) + " is not 16-byte aligned");
-  return PF_OK;
-}
-
-bool kernel_block(int32_t b) { return b == 32 || b == 64 || b == 128; }
-
-pf_status check_layout_arg(const pf_layout *L) {
-  if (!L) return fail(PF_ERR_INVALID_ARG, "layout is NULL");
-  if (!kernel_block(L->b))
-    return fail(PF_ERR_UNSUPPORTED, "kernels support b in {32, 64, 128}");
-  return PF_OK;
-}
-
-// Called after all argument checks: the layout must live on this device.
-pf_status check_state(const pf_layout *L) {
-  if (L->device < 0 || !L->dev_mem)
-    return fail(PF_ERR_STATE, "layout not uploaded (call pf_layout_upload)");
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev != L->device)
-    return fail(PF_ERR_STATE, "layout was uploaded to another device");
-  return PF_OK;
-}
 
 // Kernels address a tile of up to 512 token rows of any operand with 32-bit
 // buffer offsets: 512 rows of the widest operand must stay below 2^31 bytes.
@@ -131,11 +49,6 @@ pf_status check_extent(const pf_layout *L, pf_dtype dt, int32_t r) {
     return fail(PF_ERR_UNSUPPORTED, "rows wider than " + std::to_string(kMaxRowBytes) +
                                         " bytes are not supported");
   return PF_OK;
-}
-
-pf_status hip_status(hipError_t e, const char *what) {
-  if (e == hipSuccess) return PF_OK;
-  return fail(PF_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
 // Largest power of two <= min(gmax, n).
@@ -1095,14 +1008,6 @@ pf_status pf_linear_plan_get(const pf_layout *L, pf_dtype dtype, int64_t T, int3
   return PF_OK;
 }
 
-// Checks a caller workspace against a need of `need` bytes.
-static pf_status need_ws(size_t need, const void *ws, size_t ws_bytes) {
-  if (need == 0) return PF_OK;
-  if (ws_bytes < need)
-    return fail(PF_ERR_WORKSPACE, "workspace needs " + std::to_string(need) + " bytes");
-  return need_ptr(ws, "workspace");
-}
-
 }  // extern "C"
 
 namespace {
@@ -1135,9 +1040,36 @@ void set_mix(pf::NTArgs &a, const Mix &m) {
   }
 }
 
+// What follows the products in the forward's epilogue: kEpiNone, kEpiGelu, or
+// kEpiAct with a bias (N), an activation and a residual (T x N; both may be
+// null).
+struct FwdEpi {
+  int epi;
+  const void *bias;
+  int act;
+  const void *residual;
+};
+FwdEpi plain_epi(pf_epilogue epi) { return FwdEpi{(int)epi, nullptr, pf::kActNone, nullptr}; }
+
+pf_status check_fwd_epi(const FwdEpi &e, const void *Y_pre) {
+  pf_status st;
+  if (e.epi == pf::kEpiAct) {
+    if (e.act < pf::kActNone || e.act > pf::kActRelu) return fail(PF_ERR_INVALID_ARG, "bad activation");
+    if (e.bias && (st = need_ptr(e.bias, "bias")) != PF_OK) return st;
+    if (e.residual && (st = need_ptr(e.residual, "residual")) != PF_OK) return st;
+    if (e.act == pf::kActNone && Y_pre)
+      return fail(PF_ERR_INVALID_ARG, "Y_pre given without an activation");
+    return Y_pre ? need_ptr(Y_pre, "Y_pre") : PF_OK;
+  }
+  if (e.epi != PF_EPI_NONE && e.epi != PF_EPI_GELU) return fail(PF_ERR_INVALID_ARG, "bad epilogue");
+  if (e.epi == PF_EPI_GELU && (st = need_ptr(Y_pre, "Y_pre")) != PF_OK) return st;
+  if (e.epi == PF_EPI_NONE && Y_pre) return fail(PF_ERR_INVALID_ARG, "Y_pre given without GELU epilogue");
+  return PF_OK;
+}
+
 pf_status linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, const Mix &mix,
                      const void *X, const void *Wblk, const void *U, const void *V, void *Y,
-                     void *T_lr, pf_epilogue epi, void *Y_pre, void *workspace, size_t ws_bytes,
+                     void *T_lr, const FwdEpi &epi, void *Y_pre, void *workspace, size_t ws_bytes,
                      void *stream) {
   pf_status st = check_layout_arg(L);
   if (st != PF_OK) return st;
@@ -1149,9 +1081,7 @@ pf_status linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, c
   if (r > 0 && ((st = need_ptr(U, "U")) != PF_OK || (st = need_ptr(V, "V")) != PF_OK ||
                 (st = need_ptr(T_lr, "T_lr")) != PF_OK))
     return st;
-  if (epi != PF_EPI_NONE && epi != PF_EPI_GELU) return fail(PF_ERR_INVALID_ARG, "bad epilogue");
-  if (epi == PF_EPI_GELU && (st = need_ptr(Y_pre, "Y_pre")) != PF_OK) return st;
-  if (epi == PF_EPI_NONE && Y_pre) return fail(PF_ERR_INVALID_ARG, "Y_pre given without GELU epilogue");
+  if ((st = check_fwd_epi(epi, Y_pre)) != PF_OK) return st;
   const SkinnyPlan sp = rank_plan_ws(L, (int)dtype, T, r, false, workspace, ws_bytes, 0);
   if ((st = need_ws(sp.ws, workspace, ws_bytes)) != PF_OK) return st;
   if ((st = check_state(L)) != PF_OK) return st;
@@ -1174,8 +1104,15 @@ pf_status linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, c
   a.B = Wblk;
   a.L = T_lr; a.ldl = r; a.R = U; a.ldr = r; a.nlr = r / b;
   a.C = Y; a.ldc = L->n_out;
-  a.C2 = epi == PF_EPI_GELU ? Y_pre : nullptr;
-  a.epi = (int)epi;
+  a.C2 = Y_pre;
+  a.epi = epi.epi;
+  if (epi.epi == pf::kEpiAct) {
+    a.bias = epi.bias;
+    a.act = epi.act;
+    a.aux = epi.residual;
+    // Nothing to add or apply: the plain epilogue.
+    if (!a.bias && !a.aux && a.act == pf::kActNone) a.epi = pf::kEpiNone;
+  }
   a.M = T;
   const NTList tl = fwd_list(L, dt, T);
   a.tiles = tl.tiles;
@@ -1196,8 +1133,17 @@ pf_status pf_linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r
                         const void *Wblk, const void *U, const void *V, void *Y, void *T_lr,
                         pf_epilogue epi, void *Y_pre, void *workspace, size_t ws_bytes,
                         void *stream) {
-  return linear_fwd(L, dtype, T, r, kNoMix, X, Wblk, U, V, Y, T_lr, epi, Y_pre, workspace,
-                    ws_bytes, stream);
+  return linear_fwd(L, dtype, T, r, kNoMix, X, Wblk, U, V, Y, T_lr, plain_epi(epi), Y_pre,
+                    workspace, ws_bytes, stream);
+}
+
+pf_status pf_linear_fwd_act(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, const void *X,
+                            const void *Wblk, const void *U, const void *V, const void *bias,
+                            pf_activation act, const void *residual, void *Y, void *Y_pre,
+                            void *T_lr, void *workspace, size_t ws_bytes, void *stream) {
+  return linear_fwd(L, dtype, T, r, kNoMix, X, Wblk, U, V, Y, T_lr,
+                    FwdEpi{pf::kEpiAct, bias, (int)act, residual}, Y_pre, workspace, ws_bytes,
+                    stream);
 }
 
 pf_status pf_linear_fwd_mixed(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r,
@@ -1206,8 +1152,20 @@ pf_status pf_linear_fwd_mixed(const pf_layout *L, pf_dtype dtype, int64_t T, int
                               void *workspace, size_t ws_bytes, void *stream) {
   pf_status st = check_gamma(gamma);
   if (st != PF_OK) return st;
-  return linear_fwd(L, dtype, T, r, Mix{true, gamma, 1.f - gamma}, X, Wblk, U, V, Y, T_lr, epi,
-                    Y_pre, workspace, ws_bytes, stream);
+  return linear_fwd(L, dtype, T, r, Mix{true, gamma, 1.f - gamma}, X, Wblk, U, V, Y, T_lr,
+                    plain_epi(epi), Y_pre, workspace, ws_bytes, stream);
+}
+
+pf_status pf_linear_fwd_act_mixed(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r,
+                                  float gamma, const void *X, const void *Wblk, const void *U,
+                                  const void *V, const void *bias, pf_activation act,
+                                  const void *residual, void *Y, void *Y_pre, void *T_lr,
+                                  void *workspace, size_t ws_bytes, void *stream) {
+  pf_status st = check_gamma(gamma);
+  if (st != PF_OK) return st;
+  return linear_fwd(L, dtype, T, r, Mix{true, gamma, 1.f - gamma}, X, Wblk, U, V, Y, T_lr,
+                    FwdEpi{pf::kEpiAct, bias, (int)act, residual}, Y_pre, workspace, ws_bytes,
+                    stream);
 }
 
 }  // extern "C"

@@ -33,6 +33,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "pf_act.h"
 #include "pf_dma.h"
 #include "pf_gelu.h"
 #include "pf_launch.h"
@@ -450,16 +451,22 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
     });
     return;
   }
-  // GELU backward: the pre-activations of a pass are loaded before its sums are
-  // staged.  Rows past M and dead columns read zero (range check), so the loads
+  // GELU backward (EPI 2): the pre-activations of a pass are loaded before its sums are
+  // staged; so is the residual of EPI 3 (an empty range, zeros, without one).  Rows past M and dead columns read zero (range check), so the loads
   // need no branch.  (A pass further ahead, in two sets of registers, is no faster: 8192
   // x 4096 66.4 us so, 66.7 that way.)
   constexpr int NPASS = TM * (32 / SP), NIT = SP / RPI;
-  u32x4 ax[EPI == 2 ? NIT : 1];
-  const rsrc_t rx = make_rsrc(EPI == 2 ? (const bf16_t *)a.aux + m0 * a.ldc : nullptr,
-                              EPI == 2 ? (a.M - m0) * a.ldc * 2 : 0);
+  constexpr bool AUX = EPI >= 2;
+  u32x4 ax[AUX ? NIT : 1];
+  const bool has_aux = EPI == 2 || (EPI == 3 && a.aux);
+  const rsrc_t rx = make_rsrc(has_aux ? (const bf16_t *)a.aux + m0 * a.ldc : nullptr,
+                              has_aux ? (a.M - m0) * a.ldc * 2 : 0);
+  // EPI 3: the bias of this lane's 8 columns.
+  u32x4 bz = {0u, 0u, 0u, 0u};
+  if constexpr (EPI == 3)
+    if (a.bias && col_ok) bz = *(const u32x4 *)((const bf16_t *)a.bias + col);
   auto load_aux = [&](auto pass) __attribute__((always_inline)) {
-    if constexpr (EPI == 2) {
+    if constexpr (AUX) {
       constexpr int tm = pass / (32 / SP), half = pass % (32 / SP);
       sfor<NIT>([&](auto it) __attribute__((always_inline)) {
         const uint32_t row = (uint32_t)(wm * WTM + tm * 32 + half * SP + it * RPI + rl);
@@ -512,6 +519,24 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
           v[2 * e] *= gelu_grad_fast(__uint_as_float(x[e] << 16));
           v[2 * e + 1] *= gelu_grad_fast(__uint_as_float(x[e] & 0xffff0000u));
         }
+      } else if constexpr (EPI == 3) {  // bias, activation, residual
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[2 * e] += __uint_as_float(bz[e] << 16);
+          v[2 * e + 1] += __uint_as_float(bz[e] & 0xffff0000u);
+        }
+        if (a.C2)
+          *(u32x4 *)((bf16_t *)a.C2 + o) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                 pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+        act_apply<bf16_t>(a.act, v);
+        if (a.aux) {
+          const u32x4 x = ax[it];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[2 * e] += __uint_as_float(x[e] << 16);
+            v[2 * e + 1] += __uint_as_float(x[e] & 0xffff0000u);
+          }
+        }
       }
       *(u32x4 *)(C + o) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
                                 pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
@@ -524,7 +549,13 @@ hipError_t ntd_go(const NTArgs &a, hipStream_t s) {
   const int64_t mtiles = (a.M + BM - 1) / BM;
   const int64_t grid = mtiles * a.ntiles * std::max(1, a.nsplit);
   if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (!DENSE && a.epi == 1) {
+  if (!DENSE && a.epi == kEpiAct) {
+    if constexpr (!DENSE && !BKN)
+      launch_kernel(ntd_kernel<BLK, G, BKN, BM, BK, NS, NW, DENSE, 3, OCC>,
+                    dim3((unsigned)grid), dim3(64 * NW), s, a);
+    else
+      return hipErrorInvalidValue;
+  } else if (!DENSE && a.epi == kEpiGelu) {
     if constexpr (!DENSE) {
       if constexpr (BKN)
         launch_kernel(ntd_kernel<BLK, G, BKN, BM, BK, NS, NW, DENSE, 2, OCC>,

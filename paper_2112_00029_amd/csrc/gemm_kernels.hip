@@ -31,6 +31,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "pf_act.h"
 #include "pf_gelu.h"
 #include "pf_launch.h"
 
@@ -73,6 +74,30 @@ __device__ __forceinline__ float gelu_grad_f(float x) {
   float Phi = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
   float phi = 0.39894228040143268f * __expf(-0.5f * x * x);
   return Phi + x * phi;
+}
+
+// 8 consecutive elements (16-byte aligned).
+__device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = p[e];
+}
+__device__ __forceinline__ void load8(const bf16_t *p, float (&v)[8]) {
+  const u32x4 w = *(const u32x4 *)p;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[2 * e] = __uint_as_float(w[e] << 16);
+    v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
+  *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
+  *(f32x4 *)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8]) {
+  u32x4 w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = (uint32_t)f2bf(v[2 * e]) | ((uint32_t)f2bf(v[2 * e + 1]) << 16);
+  *(u32x4 *)p = w;
 }
 
 // fp32 outputs keep the library erff; bf16 ones take the short form.
@@ -259,7 +284,8 @@ __device__ __forceinline__ u32x4 bload(rsrc_t r, uint32_t off) {
 // NT kernel
 // ---------------------------------------------------------------------------
 // EPI: 0 plain store, 1 forward GELU (also store the pre-activation),
-// 2 backward GELU (scale by gelu' of the pre-activation a.aux).
+// 2 backward GELU (scale by gelu' of the pre-activation a.aux), 3 bias,
+// activation and residual (kEpiAct).
 template <typename T, int BLK, int G, bool BKN, int BM, bool DENSE, int EPI>
 __global__ __launch_bounds__(256, 2) void nt_kernel(NTArgs a_arg) {
   const NTArgs a = a_arg;  // local copy: lambdas below capture it by reference
@@ -583,6 +609,19 @@ __global__ __launch_bounds__(256, 2) void nt_kernel(NTArgs a_arg) {
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] *= gelu_grad_t<T>(ax[e]);
+        }
+      } else if constexpr (EPI == 3) {  // bias, activation, residual
+        // The residual is read before C is written: it may be C itself.
+        float x[8] = {}, bz[8] = {};
+        if (a.bias) load8((const T *)a.bias + col, bz);
+        if (a.aux) load8((const T *)a.aux + o, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += bz[e];
+        if (a.C2) store8((T *)a.C2 + o, v);
+        act_apply<T>(a.act, v);
+        if (a.aux) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += x[e];
         }
       }
       if constexpr (BF) {
@@ -1011,9 +1050,15 @@ static hipError_t nt_go(const NTArgs &a, hipStream_t s) {
   const int64_t mtiles = (a.M + BM - 1) / BM;
   const int64_t grid = mtiles * a.ntiles * std::max(1, a.nsplit);
   if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  // Epilogue variants: the forward takes the GELU-forward one, the
-  // backward-data (B read as [k][n]) the GELU-backward one.
-  if (!DENSE && a.epi == 1) {
+  // Epilogue variants: the forward takes the GELU-forward one or the one of
+  // bias, activation and residual, the backward-data (B read as [k][n]) the
+  // GELU-backward one.
+  if (!DENSE && a.epi == kEpiAct) {
+    if constexpr (!DENSE && !BKN)
+      launch_kernel(nt_kernel<T, BLK, G, BKN, BM, DENSE, 3>, dim3((unsigned)grid), dim3(256), s, a);
+    else
+      return hipErrorInvalidValue;
+  } else if (!DENSE && a.epi == kEpiGelu) {
     if constexpr (!DENSE) {
       if constexpr (BKN) launch_kernel(nt_kernel<T, BLK, G, BKN, BM, DENSE, 2>,
                                        dim3((unsigned)grid), dim3(256), s, a);

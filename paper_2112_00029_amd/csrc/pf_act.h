@@ -1,0 +1,135 @@
+// Activations of the layer's epilogue and their derivatives, chosen by a
+// launch argument (uniform over a launch).
+//
+//   gelu       x Phi(x)                      Phi(x) + x phi(x)
+//   gelu_tanh  x s(y), y = 2 k (x + c x^3),  s + x s (1 - s) y',
+//              k = sqrt(2 / pi), c = 0.044715   y' = 2 k (1 + 3 c x^2)
+//   silu       x s(x)                        s + x s (1 - s)
+//   relu       x for x > 0, else 0           1 for x > 0, else 0
+// s(y) = 1 / (1 + exp(-y)); 0.5 (1 + tanh(y / 2)) is the same number.  Both s and
+// 1 - s come from e = exp(-|y|), r = 1 / (1 + e): r and e r, whichever side, so that
+// neither cancels or overflows.
+// bf16 results take the hardware exponential and reciprocal (1 ulp each: far below
+// their own rounding) and the short normal CDF; fp32 results take the library's
+// functions.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "pf_gelu.h"
+#include "pf_internal.h"
+
+namespace pf {
+namespace {
+
+// s = s(y), c = 1 - s(y).
+template <typename T>
+__device__ __forceinline__ void act_sigmoid(float y, float &s, float &c) {
+  float e, r;
+  if constexpr (sizeof(T) == 2) {
+    e = __builtin_amdgcn_exp2f(fabsf(y) * -1.4426950408889634f);
+    r = __builtin_amdgcn_rcpf(1.0f + e);
+  } else {
+    e = expf(-fabsf(y));
+    r = 1.0f / (1.0f + e);
+  }
+  const float er = e * r;
+  s = y < 0.f ? er : r;
+  c = y < 0.f ? r : er;
+}
+
+constexpr float kTanh2k = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+constexpr float kTanhC = 0.044715f;
+
+template <typename T>
+__device__ __forceinline__ float act_gelu(float x) {
+  if constexpr (sizeof(T) == 2) return gelu_fast(x);
+  else return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
+}
+template <typename T>
+__device__ __forceinline__ float act_gelu_grad(float x) {
+  if constexpr (sizeof(T) == 2) return gelu_grad_fast(x);
+  else {
+    const float cdf = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
+    return cdf + x * (0.39894228040143268f * expf(-0.5f * x * x));
+  }
+}
+template <typename T>
+__device__ __forceinline__ float act_gelu_tanh(float x) {
+  float s, c;
+  act_sigmoid<T>(kTanh2k * __builtin_fmaf(kTanhC * x, x * x, x), s, c);
+  return x * s;
+}
+template <typename T>
+__device__ __forceinline__ float act_gelu_tanh_grad(float x) {
+  // Beyond |x| = 16, s (1 - s) is below 1e-125: the clamp only keeps the
+  // square finite.
+  const float z = fminf(fmaxf(x, -16.f), 16.f), z2 = z * z;
+  float s, c;
+  act_sigmoid<T>(kTanh2k * __builtin_fmaf(kTanhC * z, z2, z), s, c);
+  const float g = __builtin_fmaf(z * s * c, kTanh2k * __builtin_fmaf(3 * kTanhC, z2, 1.0f), s);
+  return x != x ? x : g;
+}
+template <typename T>
+__device__ __forceinline__ float act_silu(float x) {
+  float s, c;
+  act_sigmoid<T>(x, s, c);
+  return x * s;
+}
+template <typename T>
+__device__ __forceinline__ float act_silu_grad(float x) {
+  float s, c;
+  act_sigmoid<T>(x, s, c);
+  return __builtin_fmaf(x * c, s, s);
+}
+
+// v[i] = act(v[i]); T: the type the results are stored in.
+template <typename T, int N>
+__device__ __forceinline__ void act_apply(int act, float (&v)[N]) {
+  switch (act) {
+    case kActGelu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = act_gelu<T>(v[e]);
+      break;
+    case kActGeluTanh:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = act_gelu_tanh<T>(v[e]);
+      break;
+    case kActSilu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = act_silu<T>(v[e]);
+      break;
+    case kActRelu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+      break;
+    default: break;
+  }
+}
+
+// v[i] *= act'(x[i]).
+template <typename T, int N>
+__device__ __forceinline__ void act_grad_apply(int act, float (&v)[N], const float (&x)[N]) {
+  switch (act) {
+    case kActGelu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= act_gelu_grad<T>(x[e]);
+      break;
+    case kActGeluTanh:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= act_gelu_tanh_grad<T>(x[e]);
+      break;
+    case kActSilu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= act_silu_grad<T>(x[e]);
+      break;
+    case kActRelu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = x[e] > 0.f ? v[e] : 0.f;
+      break;
+    default: break;
+  }
+}
+
+}  // namespace
+}  // namespace pf

@@ -44,6 +44,13 @@ struct TNItem {
   int32_t out_blk[kTNMax * kTNMax];
 };
 
+// Epilogues of the NT kernels (NTArgs::epi).  kEpiGelu: GELU of the forward
+// (C2 = the pre-activation, C = gelu) or, for backward-data, GELU' of aux.
+// kEpiAct (forward only): z = sum + bias, C2 (if not null) = z, C = aux + act(z).
+constexpr int kEpiNone = 0, kEpiGelu = 1, kEpiAct = 2;
+// Activations (pf_activation).
+constexpr int kActNone = 0, kActGelu = 1, kActGeluTanh = 2, kActSilu = 3, kActRelu = 4;
+
 // Arguments of the NT kernel family.
 struct NTArgs {
   const void *A;        // T x lda (X or dY)
@@ -61,8 +68,10 @@ struct NTArgs {
   void *C;              // T x ldc output
   int64_t ldc;
   void *C2;             // GELU forward: pre-activation output
-  const void *aux;      // GELU backward: pre-activation input
-  int epi;
+  const void *aux;      // GELU backward: pre-activation input; kEpiAct: residual or null
+  int epi;              // kEpi* below
+  const void *bias;     // kEpiAct: N elements or null
+  int act;              // kEpiAct: kAct* below
   int64_t M;            // tokens
   const NTTile *tiles;  // null in dense mode
   int ntiles;           // output column tiles (dense mode: ceil(nblk / G))
@@ -294,6 +303,21 @@ struct BflyArgs {
   int nb, k, nfac;  // n / 32, 2^nfac (blocks per group), factors
 };
 hipError_t launch_bfly(bool bwd, const BflyArgs &a, hipStream_t s);
+
+// Backward of the activation epilogue (act.hip): column chunks of 16 bytes, cw
+// of them per workgroup (a power of two, at most 64), `groups` workgroups
+// across N and nparts parts of rows_per_part token rows.  With nparts > 1 and
+// a dbias the parts' sums go to partials [nparts][N] and launch_act_dbias adds
+// them; with one part the kernel stores dbias itself (partials null).
+struct ActBwdArgs {
+  const void *dY, *Z;
+  void *dZ, *dbias;
+  float *partials;
+  int64_t T, N, rows_per_part;
+  int act, cw, groups, nparts;
+};
+hipError_t launch_act_bwd(int dtype, const ActBwdArgs &a, hipStream_t s);
+hipError_t launch_act_dbias(int dtype, const ActBwdArgs &a, hipStream_t s);
 
 // The allocation-free attention backward keeps its row terms in a
 // file-scope device array of kAttnScratchRows floats (16 MiB per GPU);

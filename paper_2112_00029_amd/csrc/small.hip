@@ -19,6 +19,7 @@
 
 #include <algorithm>
 
+#include "pf_act.h"
 #include "pf_dma.h"
 #include "pf_gelu.h"
 #include "pf_launch.h"
@@ -58,7 +59,7 @@ __device__ __forceinline__ float gelu_grad_s(float x) {
 
 // T: bf16 or float storage.  NH: sub-blocks per step (2 for bf16 blocks of 32,
 // half a 128-byte step each).  BKN: B read as [k][n].  EPI: 0 none, 1 GELU
-// forward, 2 GELU backward.
+// forward, 2 GELU backward, 3 bias, activation and residual (kEpiAct).
 template <typename T, int NH, bool BKN, bool DENSE, int EPI, int NW>
 __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   constexpr int ES = sizeof(T), KW = 128 / NH / ES;  // K width of a sub-block
@@ -111,9 +112,14 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   const int64_t et = m0 + (il & 31);
   const int64_t eoff = et * n.ldc + col0 + ig * 8 + (il >> 5) * 4;
   const bool elive = threadIdx.x < 256 && et < n.M;
-  f32x4 aux = {0.f, 0.f, 0.f, 0.f};
+  // (EPI 3: its residual and bias.)
+  f32x4 aux = {0.f, 0.f, 0.f, 0.f}, bz = {0.f, 0.f, 0.f, 0.f};
   if constexpr (EPI == 2)
     if (elive) aux = get4((const T *)n.aux + eoff);
+  if constexpr (EPI == 3) {
+    if (elive && n.aux) aux = get4((const T *)n.aux + eoff);
+    if (elive && n.bias) bz = get4((const T *)n.bias + col0 + ig * 8 + (il >> 5) * 4);
+  }
 
   // Lane part of the copies.  Rows of 8 chunks are swizzled by row pair (two
   // variants: even / odd windows), rows of 4 by groups of 4 rows; a [k][n]
@@ -272,6 +278,15 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   } else if constexpr (EPI == 2) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] *= gelu_grad_s<T>(aux[q]);
+  } else if constexpr (EPI == 3) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] += bz[q];
+    if (n.C2) put4((T *)n.C2 + eoff, v);
+    act_apply<T>(n.act, v);
+    if (n.aux) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] += aux[q];
+    }
   }
   put4((T *)n.C + eoff, v);
 }
@@ -287,7 +302,11 @@ hipError_t small_go(const SmallArgs &a, int64_t grid, bool deep, hipStream_t s) 
 
 template <typename T, int NH, bool BKN>
 hipError_t small_epi(const SmallArgs &a, int64_t grid, bool deep, hipStream_t s) {
-  if (a.nt.epi == 1) return small_go<T, NH, BKN, false, BKN ? 2 : 1>(a, grid, deep, s);
+  if (a.nt.epi == kEpiAct) {
+    if constexpr (BKN) return hipErrorInvalidValue;
+    else return small_go<T, NH, BKN, false, 3>(a, grid, deep, s);
+  }
+  if (a.nt.epi == kEpiGelu) return small_go<T, NH, BKN, false, BKN ? 2 : 1>(a, grid, deep, s);
   return small_go<T, NH, BKN, false, 0>(a, grid, deep, s);
 }
 

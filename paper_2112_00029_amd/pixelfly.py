@@ -25,6 +25,7 @@ PF_ERR_WORKSPACE, PF_ERR_HIP, PF_ERR_NOMEM, PF_ERR_STATE = -3, -4, -5, -6
 PF_BF16, PF_FP32 = 0, 1
 PF_EPI_NONE, PF_EPI_GELU = 0, 1
 PF_OP_NT, PF_OP_NN, PF_OP_TN = 0, 1, 2
+PF_ACT_NONE, PF_ACT_GELU, PF_ACT_GELU_TANH, PF_ACT_SILU, PF_ACT_RELU = 0, 1, 2, 3, 4
 # Kernel classes of the timing hook (pf_kernel_class).
 KERNEL_CLASSES = ["spmm_fwd", "spmm_bwd_data", "sddmm", "lowrank_t", "lowrank_s", "reduce",
                   "gelu_bwd", "attn_fwd", "attn_bwd_dq", "attn_bwd_dkv", "dense", "butterfly"]
@@ -102,6 +103,12 @@ _SIGS = {
                                         _p, _p, _sz, _p]),
     "pf_linear_bwd_weight_mixed": (_i32, [_p, _i32, _i64, _i32, _f32, _p, _p, _p, _p, _p, _p, _p,
                                           _p, _p, _p, _sz, _p]),
+    "pf_linear_fwd_act": (_i32, [_p, _i32, _i64, _i32, _p, _p, _p, _p, _p, _i32, _p, _p, _p, _p, _p,
+                                 _sz, _p]),
+    "pf_linear_fwd_act_mixed": (_i32, [_p, _i32, _i64, _i32, _f32, _p, _p, _p, _p, _p, _i32, _p, _p,
+                                       _p, _p, _p, _sz, _p]),
+    "pf_linear_act_bwd": (_i32, [_i32, _i64, _i64, _i32, _p, _p, _p, _p, _p, _sz, _p]),
+    "pf_linear_act_workspace_bytes": (_sz, [_i32, _i64, _i64]),
     "pf_gelu_bwd": (_i32, [_i32, _i64, _p, _p, _p, _p]),
     "pf_attn_fwd": (_i32, [_p, _i32, _i32, _i32, _i32, _f32, _p, _p, _p, _p, _p, _p]),
     "pf_attn_bwd": (_i32, [_p, _i32, _i32, _i32, _i32, _f32, _p, _p, _p, _p, _p, _p, _p, _p,
@@ -347,6 +354,32 @@ def pf_linear_bwd_weight_mixed(layout, dtype, T, r, gamma, dY, X, Wblk, T_lr, S,
                                            _ptr(dY), _ptr(X), _ptr(Wblk), _ptr(T_lr), _ptr(S),
                                            _ptr(dWblk), _ptr(dU), _ptr(dV), _ptr(dgamma),
                                            _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_linear_fwd_act(layout, dtype, T, r, X, Wblk, U, V, bias, act, residual, Y, Y_pre, T_lr,
+                      workspace=None, ws_bytes=0, stream=None) -> None:
+    """act: PF_ACT_*; bias, residual and Y_pre may be None."""
+    _check(_lib.pf_linear_fwd_act(layout.handle, _dt(dtype), T, r, _ptr(X), _ptr(Wblk), _ptr(U),
+                                  _ptr(V), _ptr(bias), act, _ptr(residual), _ptr(Y), _ptr(Y_pre),
+                                  _ptr(T_lr), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_linear_fwd_act_mixed(layout, dtype, T, r, gamma, X, Wblk, U, V, bias, act, residual, Y, Y_pre,
+                            T_lr, workspace=None, ws_bytes=0, stream=None) -> None:
+    _check(_lib.pf_linear_fwd_act_mixed(layout.handle, _dt(dtype), T, r, float(gamma), _ptr(X),
+                                        _ptr(Wblk), _ptr(U), _ptr(V), _ptr(bias), act,
+                                        _ptr(residual), _ptr(Y), _ptr(Y_pre), _ptr(T_lr),
+                                        _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_linear_act_bwd(dtype, T, N, act, dY, Y_pre, dY_pre, dbias, workspace=None, ws_bytes=0,
+                      stream=None) -> None:
+    _check(_lib.pf_linear_act_bwd(_dt(dtype), T, N, act, _ptr(dY), _ptr(Y_pre), _ptr(dY_pre),
+                                  _ptr(dbias), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_linear_act_workspace_bytes(dtype, T, N) -> int:
+    return int(_lib.pf_linear_act_workspace_bytes(_dt(dtype), T, N))
 
 
 def pf_gelu_bwd(dtype, n, dH, H_pre, dH_pre, stream=None) -> None:

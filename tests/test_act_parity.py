@@ -1,0 +1,328 @@
+"""GPU parity of the layer with bias, activation and residual in its epilogue
+and of the way back through it, against the formulas in float64.
+
+Tolerances, element by element, derived from the arithmetic:
+  * storing in a type t rounds by at most u = finfo(t).eps / 2 of the value
+    (bf16 2^-8, fp32 2^-24);
+  * T_lr is stored in the call's type before its product with U: u |T| |U|^T;
+  * fp32 sums of n terms: n 2^-24 of the sum of the terms' absolute values
+    (the order does not matter for the bound);
+  * the activations are Lipschitz with a constant below 1.13, their own fp32
+    evaluation is within 1e-6 (1 + |z|) of the value (short normal CDF: 6e-8 near
+    zero and 3e-5 of the value in the far tail, where the value is below 1e-3
+    times its argument; hardware exponential and reciprocal one ulp each);
+  * derivatives: bounded by 1.13, evaluated within 3e-6 (GELU's density and CDF
+    cancel near z = -0.75)."""
+import numpy as np
+import pytest
+
+from tests._gpu_util import torch_cuda
+
+pytestmark = pytest.mark.gpu
+
+ACTS = ["none", "gelu", "gelu_tanh", "silu", "relu"]
+LIP = 1.13
+
+
+def _act(t, z, act):
+    if act == "gelu":
+        return 0.5 * z * t.special.erfc(-z / 2 ** 0.5)
+    if act == "gelu_tanh":
+        return 0.5 * z * (1 + t.tanh((2 / np.pi) ** 0.5 * (z + 0.044715 * z ** 3)))
+    if act == "silu":
+        return z * t.sigmoid(z)
+    return z.clamp(min=0) if act == "relu" else z
+
+
+def _slope(t, z, act):
+    z = z.detach().requires_grad_(True)
+    if act == "relu":
+        return (z > 0).double()
+    return t.autograd.grad(_act(t, z, act).sum(), z)[0]
+
+
+def _mask(nbo, nbi, ms):
+    s = min(nbo, nbi)
+    x = (np.arange(nbo)[:, None] % s) ^ (np.arange(nbi)[None, :] % s)
+    return ((x & (x - 1)) == 0) & (x < ms)
+
+
+class Layer:
+    """Inputs of one layer on the GPU and its exact pre-activation in fp64."""
+
+    def __init__(self, dtype, T, K, N, b, ms, r, seed=0, gamma=None):
+        t = self.t = torch_cuda()
+        from paper_2112_00029_amd import pixelfly as pf
+        self.pf, self.dtype, self.T, self.K, self.N, self.r = pf, dtype, T, K, N, r
+        self.dt = t.bfloat16 if dtype == "bf16" else t.float32
+        self.u = t.finfo(self.dt).eps / 2
+        g = t.Generator(device="cuda").manual_seed(seed)
+        rnd = lambda shape, std: t.randn(shape, generator=g, device="cuda").mul_(std).to(self.dt)
+        m = _mask(N // b, K // b, ms)
+        i, j = np.nonzero(m)
+        fan = len(i) / (N // b) * b
+        self.x, self.w = rnd((T, K), 1.0), rnd((len(i), b, b), fan ** -0.5)
+        self.U = rnd((N, r), 0.5 * r ** -0.5) if r else None
+        self.V = rnd((r, K), K ** -0.5) if r else None
+        self.bias, self.res = rnd((N,), 0.5), rnd((T, N), 1.0)
+        self.L = pf.pf_layout_create(N, K, b, ms)
+        pf.pf_layout_upload(self.L)
+        W = t.zeros((N // b, K // b, b, b), dtype=t.float64, device="cuda")
+        W[t.from_numpy(i).cuda(), t.from_numpy(j).cuda()] = self.w.double()
+        W = W.permute(0, 2, 1, 3).reshape(N, K)
+        al, be = (1.0, 1.0) if gamma is None else (gamma, 1 - gamma)
+        x = self.x.double()
+        self.z = al * x @ W.t()
+        mag = al * x.abs() @ W.abs().t()
+        self.tol = t.zeros_like(self.z)
+        if r:
+            tl = x @ self.V.double().t()
+            self.z = self.z + be * tl @ self.U.double().t()
+            lr = be * tl.abs() @ self.U.double().abs().t()
+            mag = mag + lr
+            self.tol = self.tol + 1.01 * self.u * lr
+            tmag = x.abs() @ self.V.double().abs().t()
+            self.tol = self.tol + be * K * 2.0 ** -24 * tmag @ self.U.double().abs().t()
+        self.tol = self.tol + (K + r + 4) * 2.0 ** -24 * (mag + self.bias.double().abs())
+        self.ws_bytes = pf.pf_workspace_bytes(self.L, T, r, dtype)
+        self.ws = t.empty((max(self.ws_bytes, 256),), dtype=t.uint8, device="cuda")
+
+    def empty(self, cols):
+        return self.t.full((self.T, cols), float("nan"), dtype=self.dt, device="cuda")
+
+    def run(self, act, bias=True, res=True, pre=True, gamma=None, inplace=False, stream=None):
+        pf = self.pf
+        y = self.res.clone() if inplace else self.empty(self.N)
+        ypre = self.empty(self.N) if pre and act != "none" else None
+        tl = self.empty(self.r) if self.r else None
+        a = getattr(pf, "PF_ACT_" + act.upper())
+        args = (self.x, self.w, self.U, self.V, self.bias if bias else None, a,
+                (y if inplace else self.res) if res else None, y, ypre, tl, self.ws, self.ws_bytes, stream)
+        if gamma is None:
+            pf.pf_linear_fwd_act(self.L, self.dtype, self.T, self.r, *args)
+        else:
+            pf.pf_linear_fwd_act_mixed(self.L, self.dtype, self.T, self.r, gamma, *args)
+        return y, ypre, tl
+
+    def check(self, y, ypre, act, bias=True, res=True):
+        t = self.t
+        z = self.z + self.bias.double() if bias else self.z
+        if ypre is not None:
+            bad = (ypre.double() - z).abs() - (self.u * z.abs() + self.tol * (1 + self.u))
+            assert not (bad > 0).any() and not ypre.isnan().any(), ("ypre", float(bad.max()))
+        ref = _act(t, z, act)
+        if res:
+            ref = ref + self.res.double()
+        bound = self.u * ref.abs() + LIP * (1 + self.u) * self.tol + 1e-6 * (1 + z.abs())
+        bad = (y.double() - ref).abs() - bound
+        assert not (bad > 0).any() and not y.isnan().any(), ("y", act, float(bad.max()))
+
+
+# One for every kernel and tile a forward can run on: few tiles (bf16 and
+# fp32, blocks of 32, 64 and 128, ragged rows), 32- to 256-column tiles, tall and
+# short-K ones, 256 x 256 in bands.
+SHAPES = [
+    ("bf16", 1, 256, 512, 64, 4, 64), ("bf16", 33, 320, 416, 32, 8, 32), ("bf16", 8, 512, 256, 128, 2, 0),
+    ("fp32", 5, 256, 512, 64, 4, 64), ("fp32", 200, 224, 288, 32, 4, 32), ("fp32", 2048, 1024, 1024, 32, 8, 32),
+    ("fp32", 2001, 1024, 1024, 128, 4, 128), ("bf16", 1000, 768, 768, 32, 16, 96),
+    ("bf16", 1000, 1024, 4096, 64, 16, 128), ("bf16", 2100, 1024, 4096, 64, 16, 0),
+    ("bf16", 4100, 4096, 1024, 64, 16, 128), ("bf16", 2509, 2048, 8192, 32, 32, 64),
+    ("bf16", 2049, 1024, 4096, 128, 8, 256), ("bf16", 8200, 512, 512, 128, 2, 128),
+]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(map(str, s)))
+def test_forward_every_activation(shape):
+    lay = Layer(*shape)
+    for act in ACTS:
+        for bias, res in ((True, True), (True, False), (False, True), (False, False)):
+            if not bias and act not in ("gelu", "none"):
+                continue
+            print(f"[layer] {shape} {act} bias={bias} res={res}", flush=True)
+            y, ypre, _ = lay.run(act, bias, res)
+            lay.check(y, ypre, act, bias, res)
+
+
+@pytest.mark.parametrize("shape", [SHAPES[1], SHAPES[5], SHAPES[8], SHAPES[11]],
+                         ids=lambda s: "-".join(map(str, s)))
+def test_residual_in_place_and_no_pre_activation(shape):
+    lay = Layer(*shape)
+    y, _, t0 = lay.run("silu", pre=False)
+    z, _, t1 = lay.run("silu", pre=False, inplace=True)
+    lay.check(y, None, "silu")
+    assert lay.t.equal(y, z) and (t0 is None or lay.t.equal(t0, t1))
+
+
+@pytest.mark.parametrize("dtype,T,K,N,b,r", [("bf16", 40, 256, 512, 64, 64), ("bf16", 2100, 1024, 4096, 64, 128),
+                                             ("fp32", 300, 512, 512, 32, 32), ("bf16", 4100, 1024, 2048, 32, 0)])
+@pytest.mark.parametrize("gamma", [1.0, 0.6])
+def test_forward_mixed(dtype, T, K, N, b, r, gamma):
+    lay = Layer(dtype, T, K, N, b, 8, r, gamma=gamma)
+    y, ypre, _ = lay.run("gelu_tanh", gamma=gamma)
+    lay.check(y, ypre, "gelu_tanh")
+
+
+@pytest.mark.parametrize("dtype,T,K,N,b,ms,r", [("bf16", 40, 256, 512, 64, 4, 64), ("fp32", 300, 512, 512, 32, 8, 32),
+                                                ("bf16", 2100, 1024, 4096, 64, 16, 128)])
+def test_gelu_alone_is_the_gelu_epilogue(dtype, T, K, N, b, ms, r):
+    """Without bias and residual: the bits of pf_linear_fwd's GELU epilogue,
+    and with no activation either those of its plain one."""
+    lay = Layer(dtype, T, K, N, b, ms, r)
+    pf, t = lay.pf, lay.t
+    y, ypre, tl = lay.run("gelu", bias=False, res=False)
+    y2, p2, t2 = lay.empty(N), lay.empty(N), lay.empty(r)
+    pf.pf_linear_fwd(lay.L, dtype, T, r, lay.x, lay.w, lay.U, lay.V, y2, t2, pf.PF_EPI_GELU, p2, lay.ws,
+                     lay.ws_bytes)
+    assert t.equal(y, y2) and t.equal(ypre, p2) and t.equal(tl, t2)
+    y, _, _ = lay.run("none", bias=False, res=False)
+    pf.pf_linear_fwd(lay.L, dtype, T, r, lay.x, lay.w, lay.U, lay.V, y2, t2, pf.PF_EPI_NONE, None, lay.ws,
+                     lay.ws_bytes)
+    assert t.equal(y, y2)
+
+
+def test_infinities_in_bias_and_residual():
+    """-inf pre-activations of a whole column through ReLU are zero, a residual
+    of +inf stays, and neighbours are not touched."""
+    lay = Layer("bf16", 70, 256, 512, 64, 4, 64)
+    lay.bias[7] = -float("inf")
+    lay.res[3, 9] = float("inf")
+    y, ypre, _ = lay.run("relu")
+    assert (ypre[:, 7] == -float("inf")).all() and lay.t.equal(y[:, 7], lay.res[:, 7])
+    assert y[3, 9] == float("inf")
+    keep = lay.t.ones_like(y, dtype=lay.t.bool)
+    keep[:, 7] = False
+    keep[3, 9] = False
+    assert y[keep].isfinite().all()
+
+
+def _bwd(t, pf, dtype, T, N, act, dy, z, dbias=True, alias=None):
+    dt = dy.dtype
+    wsb = pf.pf_linear_act_workspace_bytes(dtype, T, N) if dbias else 0
+    ws = t.full((max(wsb, 256),), 255, dtype=t.uint8, device="cuda")
+    dz = None if act == "none" else alias if alias is not None else t.full_like(dy, float("nan"))
+    db = t.full((N,), float("nan"), dtype=dt, device="cuda") if dbias else None
+    pf.pf_linear_act_bwd(dtype, T, N, getattr(pf, "PF_ACT_" + act.upper()), dy, None if act == "none" else z, dz,
+                         db, ws if wsb else None, wsb)
+    return dz, db
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,N", [(1, 32), (3, 64), (17, 544), (130, 256), (257, 2080), (2100, 4096), (5000, 96)])
+def test_backward(dtype, T, N):
+    t = torch_cuda()
+    from paper_2112_00029_amd import pixelfly as pf
+    dt = t.bfloat16 if dtype == "bf16" else t.float32
+    u = t.finfo(dt).eps / 2
+    g = t.Generator(device="cuda").manual_seed(T + N)
+    dy = t.randn((T, N), generator=g, device="cuda").to(dt)
+    z = (t.randn((T, N), generator=g, device="cuda") * 2).to(dt)
+    for act in ACTS:
+        print(f"[act_bwd] {dtype} T={T} N={N} {act}", flush=True)
+        dz, db = _bwd(t, pf, dtype, T, N, act, dy, z)
+        ref = dy.double() * (_slope(t, z.double(), act) if act != "none" else 1.0)
+        err = 3e-6 * dy.double().abs()
+        if act == "none":
+            assert dz is None
+        else:
+            bad = (dz.double() - ref).abs() - (u * ref.abs() + (1 + u) * err)
+            assert not (bad > 0).any() and not dz.isnan().any(), (act, float(bad.max()))
+        s = ref.sum(0)
+        tol = err.sum(0) + T * 2.0 ** -24 * (ref.abs().sum(0) + err.sum(0))
+        bad = (db.double() - s).abs() - (u * s.abs() + (1 + u) * tol)
+        assert not (bad > 0).any() and not db.isnan().any(), (act, "dbias", float(bad.max()))
+        if act != "none":
+            # No bias; and in place of either input.
+            dz2, _ = _bwd(t, pf, dtype, T, N, act, dy, z, dbias=False)
+            a = dy.clone()
+            dz3, db3 = _bwd(t, pf, dtype, T, N, act, a, z, alias=a)
+            b = z.clone()
+            dz4, db4 = _bwd(t, pf, dtype, T, N, act, dy, b, alias=b)
+            assert t.equal(dz, dz2) and t.equal(dz, dz3) and t.equal(dz, dz4)
+            assert t.equal(db, db3) and t.equal(db, db4)
+
+
+def test_backward_extreme_pre_activations():
+    """Far tails of either sign, zeros, the largest finite values: finite
+    derivatives with the limits 0 and 1; NaN stays NaN (ReLU: 0)."""
+    t = torch_cuda()
+    from paper_2112_00029_amd import pixelfly as pf
+    z = t.zeros((1, 64), device="cuda")
+    pts = [0.0, -0.0, 1e-30, -1e-30, 20.0, -20.0, 100.0, -100.0, 1e10, -1e10, 3e38, -3e38, float("nan")]
+    z[0, : len(pts)] = t.tensor(pts, device="cuda")
+    for dtype, dt in (("bf16", t.bfloat16), ("fp32", t.float32)):
+        zz, one = z.to(dt), t.ones((1, 64), dtype=dt, device="cuda")
+        for act in ACTS[1:]:
+            dz, _ = _bwd(t, pf, dtype, 1, 64, act, one, zz)
+            d = dz[0].double().tolist()
+            mid = 0.5 if act != "relu" else 0.0
+            assert d[0] == mid and d[1] == mid and abs(d[2] - (1.0 if act == "relu" else 0.5)) < 1e-6
+            assert abs(d[3] - mid) < 1e-6
+            for i in (4, 6, 8, 10):
+                assert abs(d[i] - 1) < 1e-6, (act, pts[i], d[i])
+            for i in (5, 7, 9, 11):
+                assert abs(d[i]) < 1e-6, (act, pts[i], d[i])
+            assert d[12] == 0 if act == "relu" else np.isnan(d[12])
+
+
+def test_backward_against_differences():
+    """fp32: the gradient of sum(c Y) in the bias by central differences of the
+    forward, through the whole layer."""
+    t = torch_cuda()
+    lay = Layer("fp32", 24, 256, 512, 64, 4, 64, seed=3)
+    pf = lay.pf
+    g = t.Generator(device="cuda").manual_seed(9)
+    c = t.randn((24, 512), generator=g, device="cuda")
+    for act in ACTS[1:4]:
+        y, ypre, _ = lay.run(act)
+        _, db = _bwd(t, pf, "fp32", 24, 512, act, c, ypre)
+        for j in (0, 77, 511):
+            keep = lay.bias[j].clone()
+            h, vals = 2.0 ** -6, []
+            for sgn in (1, -1):
+                lay.bias[j] = keep + sgn * h
+                y, _, _ = lay.run(act)
+                vals.append((y.double()[:, j] * c.double()[:, j]).sum().item())
+            lay.bias[j] = keep
+            num = (vals[0] - vals[1]) / (2 * h)
+            # Central differences: h^2 / 6 of the third derivative (below 2.5 for
+            # these activations), plus the fp32 rounding of the outputs over h.
+            mag = c[:, j].abs().sum().item()
+            assert abs(num - db[j].item()) <= mag * (h * h / 6 * 2.5 + 8 * 2.0 ** -24 / h + 1e-5), (act, j)
+
+
+def test_repeat_calls_streams_and_graph():
+    """Bitwise repeatable; on a side stream; captured once and replayed with the
+    program's own work in between."""
+    t = torch_cuda()
+    lay = Layer("bf16", 2100, 1024, 4096, 64, 16, 128)
+    pf = lay.pf
+    y0, p0, t0 = lay.run("gelu")
+    wsb = pf.pf_linear_act_workspace_bytes("bf16", 2100, 4096)
+    ws = t.empty((wsb,), dtype=t.uint8, device="cuda")
+    dz, db = t.empty_like(y0), t.empty((4096,), dtype=t.bfloat16, device="cuda")
+    pf.pf_linear_act_bwd("bf16", 2100, 4096, pf.PF_ACT_GELU, lay.res, p0, dz, db, ws, wsb)
+    t.cuda.synchronize()
+    side = t.cuda.Stream()
+    side.wait_stream(t.cuda.current_stream())
+    y1, p1, t1 = lay.run("gelu", stream=side)
+    side.synchronize()
+    assert t.equal(y0, y1) and t.equal(p0, p1) and t.equal(t0, t1)
+    ref_dz, ref_db = dz.clone(), db.clone()
+    y, p, tl = lay.empty(4096), lay.empty(4096), lay.empty(128)
+    x0 = lay.x.clone()
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        pf.pf_linear_fwd_act(lay.L, "bf16", 2100, 128, lay.x, lay.w, lay.U, lay.V, lay.bias, pf.PF_ACT_GELU,
+                             lay.res, y, p, tl, lay.ws, lay.ws_bytes)
+        pf.pf_linear_act_bwd("bf16", 2100, 4096, pf.PF_ACT_GELU, lay.res, p, dz, db, ws, wsb)
+    for i in range(4):
+        lay.x.copy_(x0 * (1 if i % 2 == 0 else 2))
+        for o in (y, p, dz, db):
+            o.fill_(float("nan"))
+        graph.replay()
+        t.cuda.synchronize()
+        if i % 2 == 0:
+            assert t.equal(y, y0) and t.equal(p, p0) and t.equal(dz, ref_dz) and t.equal(db, ref_db)
+        else:
+            ye, pe, _ = lay.run("gelu")
+            assert t.equal(y, ye) and t.equal(p, pe)
