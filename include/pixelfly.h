@@ -500,6 +500,107 @@ pf_status pf_attn_bwd_noalloc(const pf_layout *layout, int32_t B, int32_t H,
                               void *dK, void *dV, void *stream);
 
 /*
+ * Attention with a learned relative position bias by buckets:
+ *     S_ij = scale q_i . k_j + table[head][bucket(p_j - p_i)]
+ * on the kept blocks, p the positions of key j and query i in their sequence.
+ *
+ * A plan holds the bucket of every distance key - query of a sequence of up to
+ * seq tokens (a multiple of 64, the side of the layouts it is used with):
+ * bucket[seq - 1 + distance] for distance -(seq - 1) .. seq - 1 (host memory,
+ * read during the call only), each in 0 .. n_buckets - 1, or -1 for a distance
+ * that is not attended at all (e.g. every positive one: causal attention; the
+ * blocks it leaves empty cost nothing, whatever the layout keeps).  n_buckets
+ * at most 256.  pf_relpos_create_log makes the logarithmic map: of a
+ * direction's n buckets the first e = n / 2 hold one distance each, distance
+ * d >= e lies in bucket e + floor((n - e) ln(d / e) / ln(max_distance / e)), at
+ * most n - 1 (settled in integers).  bidirectional != 0: n = n_buckets / 2, keys
+ * after the query in buckets n + ...; 0: n = n_buckets, keys after the query
+ * are not attended.  max_distance > e.  Host only; pf_relpos_upload copies the
+ * plan to the current device (one-time, synchronous on `stream`), which it then
+ * serves alone.  pf_relpos_buckets_get gives the map as pf_relpos_create takes
+ * it (valid until pf_relpos_destroy); its outputs may be NULL.
+ * Errors: INVALID_ARG, NOMEM, HIP.
+ */
+typedef struct pf_relpos pf_relpos; /* opaque; immutable after create */
+pf_status pf_relpos_create(int64_t seq, int32_t n_buckets, const int32_t *bucket, pf_relpos **out);
+pf_status pf_relpos_create_log(int64_t seq, int32_t n_buckets, int64_t max_distance,
+                               int32_t bidirectional, pf_relpos **out);
+pf_status pf_relpos_buckets_get(const pf_relpos *relpos, const int32_t **bucket, int64_t *seq,
+                                int32_t *n_buckets);
+pf_status pf_relpos_upload(pf_relpos *relpos, void *stream);
+void pf_relpos_destroy(pf_relpos *relpos);
+
+/*
+ * Lay a table (H x n_buckets fp32) out by distance, as the attention calls read
+ * it: bias holds H x pf_relpos_bias_floats(relpos) floats, in a form of the
+ * library's own.  Once per change of the table: the layers that share one share
+ * its bias, a serving program keeps it.  An entry of -inf masks its bucket, as
+ * does any below about -1e30.  Errors: INVALID_ARG, STATE, HIP.
+ */
+size_t pf_relpos_bias_floats(const pf_relpos *relpos);
+pf_status pf_relpos_bias(const pf_relpos *relpos, int32_t H, const float *table, float *bias,
+                         void *stream);
+
+/* Rows of 64 contiguous bf16 elements: sequence, head and token strides in
+ * elements (multiples of 8; token stride 64 or more).  Sequences or heads of an
+ * input may share memory (stride 0), those of an output may not. */
+typedef struct {
+  void *data;
+  int64_t seq, head, token;
+} pf_attn_tensor;
+
+/*
+ * Forward: O = softmax(S) V, lse = log(sum exp S) per row (natural log).
+ * Q, O: B sequences x H heads x Sq rows; K, V: B x H_kv heads x Skv tokens, query
+ * head h reading key/value head h / (H / H_kv); bf16, d = 64, layout square with
+ * b = 64 and the plan's seq as its side; Sq and Skv any in 1 .. seq.  lse:
+ * [B][H][Sq] fp32.  scale > 0.
+ *
+ * q_start, kv_len: B int32 each in device memory, or NULL.  Row i of sequence n
+ * stands at position q_start[n] + i (NULL: i) and key j at position j; the tokens of
+ * the sequence are its first kv_len[n] (NULL: Skv); both are clamped to their
+ * range.  With q_start the call is the serving form: the newest Sq rows (one, or
+ * a chunk) of every sequence against all its keys, their own included.
+ * A row attends to the tokens of its sequence whose block the layout keeps and
+ * whose distance has a bucket.  One that attends to nothing gets O = 0 and lse =
+ * -inf; so do rows at positions past their sequence's tokens.  Memory of tokens
+ * past kv_len is not used, whatever it holds.  (A NaN or infinity in an attended
+ * block's K or V spreads to rows of that block, masked pairs included.)
+ * Needs pf_attn_relpos_workspace_bytes of workspace (0: may be NULL).
+ * Errors: INVALID_ARG, UNSUPPORTED, STATE, WORKSPACE, HIP.
+ */
+pf_status pf_attn_relpos_fwd(const pf_layout *layout, const pf_relpos *relpos, int32_t B, int32_t H,
+                             int32_t H_kv, int32_t Sq, int32_t Skv, int32_t d, float scale,
+                             const pf_attn_tensor *Q, const pf_attn_tensor *K,
+                             const pf_attn_tensor *V, const float *bias, const pf_attn_tensor *O,
+                             float *lse, const int32_t *q_start, const int32_t *kv_len,
+                             void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Backward for L = <dO, O> of whole sequences (S rows and S tokens each, no
+ * q_start), from the forward's O and lse:
+ *     delta = rowsum(dO o O), P = exp(S - lse), dV = P^T dO,
+ *     dS = P o (dO V^T - delta), dQ = dS K * scale, dK = dS^T Q * scale,
+ *     dtable[h][c] = sum of dS over all sequences and pairs of bucket c
+ * dK and dV of a key/value head are sums over its query heads.  dtable: H x
+ * n_buckets fp32, written whole (zeros for buckets no pair has).  Gradients of
+ * rows past kv_len are zero.  Every sum has a fixed order: repeat calls agree
+ * bitwise.  Needs pf_attn_relpos_workspace_bytes(layout, relpos, B, H, S).
+ * Errors: INVALID_ARG, UNSUPPORTED, STATE, WORKSPACE, HIP.
+ */
+pf_status pf_attn_relpos_bwd(const pf_layout *layout, const pf_relpos *relpos, int32_t B, int32_t H,
+                             int32_t H_kv, int32_t S, int32_t d, float scale,
+                             const pf_attn_tensor *Q, const pf_attn_tensor *K,
+                             const pf_attn_tensor *V, const float *bias, const pf_attn_tensor *O,
+                             const float *lse, const pf_attn_tensor *dO, const pf_attn_tensor *dQ,
+                             const pf_attn_tensor *dK, const pf_attn_tensor *dV, float *dtable,
+                             const int32_t *kv_len, void *workspace, size_t ws_bytes, void *stream);
+
+/* Workspace bytes of pf_attn_relpos_fwd and pf_attn_relpos_bwd (the larger). */
+size_t pf_attn_relpos_workspace_bytes(const pf_layout *layout, const pf_relpos *relpos, int32_t B,
+                                      int32_t H, int32_t Sq);
+
+/*
  * Dense comparator GEMM built from the same MFMA tiles as the sparse
  * kernels (the speedup baseline: an equally shaped dense layer):
  *   PF_OP_NT: C[M][N] = A[M][K] . B[N][K]^T   (forward,  X W^T)
@@ -539,7 +640,7 @@ typedef enum {
   PF_KERNEL_LOWRANK_T = 3,      /* rank-r product T_lr = X V^T */
   PF_KERNEL_LOWRANK_S = 4,      /* rank-r product S = dY U */
   PF_KERNEL_REDUCE = 5,         /* sums of split partial results; the b = 32
-                                   backward-data pair-block gather */
+                                   backward-data pair-block gather; pf_relpos_bias */
   PF_KERNEL_GELU_BWD = 6,       /* standalone GELU backward, pf_linear_act_bwd */
   PF_KERNEL_ATTN_FWD = 7,
   PF_KERNEL_ATTN_BWD_DQ = 8,    /* dQ (and the row terms delta) */

@@ -29,7 +29,8 @@ SOURCES = (
      ("butterfly.hip", "butterfly", ()), ("gemm_tnw.hip", "gemm_tnw", ()),
      ("pairs.hip", "pairs", ()), ("small.hip", "small", ()),
      ("gemm_tnd.hip", "gemm_tnd", ()), ("act.hip", "act", ()),
-     ("capi_block.cpp", "capi_block", ())]
+     ("capi_block.cpp", "capi_block", ()), ("relpos.hip", "relpos", ()),
+     ("relpos.cpp", "relpos_plan", ())]
     + [("gemm_kernels.hip", f"gemm_kernels_p{p}", (f"PF_GK_PART={p}",)) for p in range(7)]
     + [("gemm_dma.hip", f"gemm_dma_b{b}_{k}", (f"PF_PART_BLK={b}", f"PF_PART_BKN={k}"))
        for b in (32, 64, 128) for k in (0, 1)]
@@ -40,6 +41,7 @@ SOURCES = (
 # results out of AGPRs (no accvgpr copies) and lowers register use.
 SOURCE_FLAGS = {
     "attn_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "relpos.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 FLAGS = [

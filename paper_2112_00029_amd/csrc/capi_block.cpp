@@ -1,7 +1,13 @@
 // C ABI of the operators round the matrices of a Transformer block: the way
-// back through the layer's activation epilogue.  Argument validation (all
-// before any enqueue) and dispatch; see include/pixelfly.h for the contract.
+// back through the layer's activation epilogue, and attention with a relative
+// position bias.  Argument validation (all before any enqueue) and dispatch;
+// see include/pixelfly.h for the contract.
 #include "capi.h"
+
+#include <cmath>
+#include <new>
+
+#include "relpos.h"
 
 using namespace pf::capi;
 
@@ -82,6 +88,268 @@ pf_status pf_linear_act_bwd(pf_dtype dtype, int64_t T, int64_t N, pf_activation 
   if (!need) return PF_OK;
   Timed t(PF_KERNEL_REDUCE, s);
   return hip_status(pf::launch_act_dbias((int)dtype, a, s), "bias gradient sum");
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Relative position bias
+// ---------------------------------------------------------------------------
+namespace {
+
+// Checks shared by the two ways of making a plan.
+pf_status relpos_dims(int64_t seq, int32_t n_buckets, const void *out) {
+  if (!out) return fail(PF_ERR_INVALID_ARG, "out is NULL");
+  if (seq < 64 || seq % 64 || seq / 64 > 16384)
+    return fail(PF_ERR_INVALID_ARG, "seq must be a multiple of 64, 64 .. 2^20");
+  if (n_buckets < 1 || n_buckets > pf::kRelposMaxBuckets)
+    return fail(PF_ERR_INVALID_ARG, "n_buckets must be in 1 .. " + std::to_string(pf::kRelposMaxBuckets));
+  return PF_OK;
+}
+
+pf_status relpos_state(const pf_relpos *R) {
+  if (R->device < 0 || !R->dev_mem)
+    return fail(PF_ERR_STATE, "position bias plan not uploaded (call pf_relpos_upload)");
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev != R->device)
+    return fail(PF_ERR_STATE, "position bias plan was uploaded to another device");
+  return PF_OK;
+}
+
+// Kernels address one head's rows of a sequence with 32-bit byte offsets, up
+// to 64 rows before the first and past the last included.
+constexpr int64_t kMaxToken = (int64_t)1 << 24;
+pf_status check_rows(const pf_attn_tensor *t, const char *name, int64_t rows, bool out, int32_t B, int32_t heads) {
+  const std::string n = name;
+  if (!t) return fail(PF_ERR_INVALID_ARG, n + " is NULL");
+  pf_status st = need_ptr(t->data, name);
+  if (st != PF_OK) return st;
+  if (t->seq % 8 || t->head % 8 || t->token % 8)
+    return fail(PF_ERR_INVALID_ARG, n + ": strides must be multiples of 8 elements");
+  if (t->token < 64 || t->seq < 0 || t->head < 0)
+    return fail(PF_ERR_INVALID_ARG, n + ": token stride below 64, or a negative stride");
+  if (t->token > kMaxToken || (rows + 64) * t->token * 2 > 0x7fffffff)
+    return fail(PF_ERR_UNSUPPORTED, n + ": a head's rows of one sequence span 2^31 bytes or more");
+  if (out && ((B > 1 && t->seq < 64) || (heads > 1 && t->head < 64)))
+    return fail(PF_ERR_INVALID_ARG, n + " is written: its sequences and heads must not overlap");
+  return PF_OK;
+}
+
+struct RelposDims {
+  int32_t B, H, H_kv, Sq, Skv, d;
+  float scale;
+};
+pf_status check_relpos(const pf_layout *L, const pf_relpos *R, const RelposDims &m, const float *bias,
+                       const int32_t *q_start, const int32_t *kv_len) {
+  pf_status st = check_layout_arg(L);
+  if (st != PF_OK) return st;
+  if (!R) return fail(PF_ERR_INVALID_ARG, "position bias plan is NULL");
+  if (L->n_out != L->n_in || L->n_out != R->seq)
+    return fail(PF_ERR_INVALID_ARG, "layout must be square with the plan's sequence length as its side");
+  if (L->b != 64 || m.d != 64) return fail(PF_ERR_UNSUPPORTED, "attention supports b = 64, d = 64");
+  if (m.B < 1 || m.H < 1 || m.H_kv < 1 || m.H % m.H_kv)
+    return fail(PF_ERR_INVALID_ARG, "B, H and H_kv must be >= 1 and H_kv divide H");
+  if (m.H > 65535) return fail(PF_ERR_UNSUPPORTED, "more than 65535 heads");
+  if (m.Sq < 1 || m.Sq > R->seq || m.Skv < 1 || m.Skv > R->seq)
+    return fail(PF_ERR_INVALID_ARG, "Sq and Skv must be in 1 .. the layout's side");
+  if ((int64_t)m.B * m.H > 0x7fffffff / (R->nb + 1)) return fail(PF_ERR_INVALID_ARG, "too many blocks");
+  if (!(m.scale > 0.f) || !std::isfinite(m.scale))
+    return fail(PF_ERR_INVALID_ARG, "scale must be positive and finite");
+  if ((st = need_ptr(bias, "bias")) != PF_OK) return st;
+  if (((uintptr_t)q_start | (uintptr_t)kv_len) & 3)
+    return fail(PF_ERR_INVALID_ARG, "q_start or kv_len is not 4-byte aligned");
+  return PF_OK;
+}
+
+pf::RowView view(const pf_attn_tensor *t) { return {t->data, t->seq, t->head, t->token}; }
+pf::RowViewOut view_out(const pf_attn_tensor *t) { return {t->data, t->seq, t->head, t->token}; }
+
+pf::RelposArgs relpos_args(const pf_layout *L, const pf_relpos *R, const RelposDims &m, const float *bias,
+                           const int32_t *q_start, const int32_t *kv_len) {
+  pf::RelposArgs a{};
+  a.bias = bias;
+  a.bias_ld = 4 * R->seq;
+  a.q_start = q_start; a.kv_len = kv_len;
+  a.info = R->d_info; a.order = R->d_order;
+  a.row_ptr = L->d_row_ptr; a.col_idx = L->d_col_idx;
+  a.col_ptr = L->d_col_ptr; a.row_idx = L->d_row_idx;
+  a.B = m.B; a.H = m.H; a.Hkv = m.H_kv; a.G = m.H / m.H_kv;
+  a.Sq = m.Sq; a.Skv = m.Skv; a.seq = (int)R->seq; a.nb = R->nb;
+  // A chunk starts anywhere in a block.
+  a.ntile = (m.Sq + (q_start ? 63 : 0) + 63) / 64;
+  a.nbucket = R->n_buckets;
+  a.omin = R->omin; a.omax = R->omax;
+  a.scale = m.scale;
+  return a;
+}
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+}  // namespace
+
+extern "C" {
+
+pf_status pf_relpos_create(int64_t seq, int32_t n_buckets, const int32_t *bucket, pf_relpos **out) {
+  pf_status st = relpos_dims(seq, n_buckets, out);
+  if (st != PF_OK) return st;
+  if (!bucket) return fail(PF_ERR_INVALID_ARG, "bucket is NULL");
+  pf_relpos *R = nullptr;
+  try {
+    R = new pf_relpos;
+    const std::string err = pf::build_relpos(*R, seq, n_buckets, bucket);
+    if (!err.empty()) {
+      delete R;
+      return fail(PF_ERR_INVALID_ARG, err);
+    }
+  } catch (const std::bad_alloc &) {
+    delete R;
+    return PF_ERR_NOMEM;
+  }
+  *out = R;
+  return PF_OK;
+}
+
+pf_status pf_relpos_create_log(int64_t seq, int32_t n_buckets, int64_t max_distance, int32_t bidirectional,
+                               pf_relpos **out) {
+  pf_status st = relpos_dims(seq, n_buckets, out);
+  if (st != PF_OK) return st;
+  try {
+    std::vector<int32_t> bucket;
+    const std::string err = pf::log_buckets(seq, n_buckets, max_distance, bidirectional != 0, bucket);
+    if (!err.empty()) return fail(PF_ERR_INVALID_ARG, err);
+    return pf_relpos_create(seq, n_buckets, bucket.data(), out);
+  } catch (const std::bad_alloc &) {
+    return PF_ERR_NOMEM;
+  }
+}
+
+pf_status pf_relpos_buckets_get(const pf_relpos *R, const int32_t **bucket, int64_t *seq, int32_t *n_buckets) {
+  if (!R) return fail(PF_ERR_INVALID_ARG, "position bias plan is NULL");
+  if (bucket) *bucket = R->bucket.data() + 1;
+  if (seq) *seq = R->seq;
+  if (n_buckets) *n_buckets = R->n_buckets;
+  return PF_OK;
+}
+
+pf_status pf_relpos_upload(pf_relpos *R, void *stream) {
+  if (!R) return fail(PF_ERR_INVALID_ARG, "position bias plan is NULL");
+  if (R->dev_mem) return PF_OK;
+  int dev = -1;
+  pf_status st = hip_status(hipGetDevice(&dev), "hipGetDevice");
+  if (st != PF_OK) return st;
+  const size_t nb = R->bucket.size() * 4, ni = R->info.size() * 4, no = R->order.size() * 4;
+  char *mem = nullptr;
+  if (hipMalloc((void **)&mem, up256(nb) + up256(ni) + up256(std::max<size_t>(no, 4))) != hipSuccess)
+    return fail(PF_ERR_NOMEM, "hipMalloc for the position bias plan failed");
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t e = hipMemcpyAsync(mem, R->bucket.data(), nb, hipMemcpyHostToDevice, s);
+  if (e == hipSuccess) e = hipMemcpyAsync(mem + up256(nb), R->info.data(), ni, hipMemcpyHostToDevice, s);
+  if (e == hipSuccess && no)
+    e = hipMemcpyAsync(mem + up256(nb) + up256(ni), R->order.data(), no, hipMemcpyHostToDevice, s);
+  if (e == hipSuccess) e = hipStreamSynchronize(s);
+  if (e != hipSuccess) {
+    (void)hipFree(mem);
+    return hip_status(e, "position bias plan upload");
+  }
+  R->d_bucket = (const int32_t *)mem;
+  R->d_info = (const int32_t *)(mem + up256(nb));
+  R->d_order = (const uint32_t *)(mem + up256(nb) + up256(ni));
+  R->dev_mem = mem;
+  R->device = dev;
+  return PF_OK;
+}
+
+void pf_relpos_destroy(pf_relpos *R) {
+  if (!R) return;
+  if (R->dev_mem) {
+    int cur = -1;
+    (void)hipGetDevice(&cur);
+    if (cur != R->device) (void)hipSetDevice(R->device);
+    (void)hipFree(R->dev_mem);
+    if (cur >= 0 && cur != R->device) (void)hipSetDevice(cur);
+  }
+  delete R;
+}
+
+size_t pf_relpos_bias_floats(const pf_relpos *R) { return R ? (size_t)R->seq * 4 : 0; }
+
+pf_status pf_relpos_bias(const pf_relpos *R, int32_t H, const float *table, float *bias, void *stream) {
+  if (!R) return fail(PF_ERR_INVALID_ARG, "position bias plan is NULL");
+  if (H < 1 || H > 65535) return fail(PF_ERR_INVALID_ARG, "H must be in 1 .. 65535");
+  pf_status st;
+  if ((st = need_ptr(table, "table")) != PF_OK || (st = need_ptr(bias, "bias")) != PF_OK) return st;
+  if ((st = relpos_state(R)) != PF_OK) return st;
+  hipStream_t s = (hipStream_t)stream;
+  Timed t(PF_KERNEL_REDUCE, s);
+  return hip_status(pf::launch_relpos_bias({R->d_bucket, table, bias, (int)R->seq, R->n_buckets}, H, s),
+                    "position bias kernel");
+}
+
+size_t pf_attn_relpos_workspace_bytes(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t Sq) {
+  if (!L || !R || B < 1 || H < 1 || Sq < 1) return 0;
+  const size_t rows = (size_t)B * H;
+  return up256(rows * Sq * sizeof(float)) + up256(rows * ((Sq + 63) / 64) * R->n_buckets * sizeof(float));
+}
+
+pf_status pf_attn_relpos_fwd(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t H_kv,
+                             int32_t Sq, int32_t Skv, int32_t d, float scale, const pf_attn_tensor *Q,
+                             const pf_attn_tensor *K, const pf_attn_tensor *V, const float *bias,
+                             const pf_attn_tensor *O, float *lse, const int32_t *q_start,
+                             const int32_t *kv_len, void *workspace, size_t ws_bytes, void *stream) {
+  const RelposDims m{B, H, H_kv, Sq, Skv, d, scale};
+  pf_status st = check_relpos(L, R, m, bias, q_start, kv_len);
+  if (st != PF_OK) return st;
+  if ((st = check_rows(Q, "Q", Sq, false, B, H)) != PF_OK || (st = check_rows(K, "K", Skv, false, B, H_kv)) != PF_OK ||
+      (st = check_rows(V, "V", Skv, false, B, H_kv)) != PF_OK || (st = check_rows(O, "O", Sq, true, B, H)) != PF_OK ||
+      (st = need_ptr(lse, "lse")) != PF_OK)
+    return st;
+  (void)workspace;
+  (void)ws_bytes;
+  if ((st = check_state(L)) != PF_OK || (st = relpos_state(R)) != PF_OK) return st;
+  pf::RelposArgs a = relpos_args(L, R, m, bias, q_start, kv_len);
+  a.Q = view(Q); a.K = view(K); a.V = view(V); a.Oout = view_out(O);
+  a.lse = lse;
+  hipStream_t s = (hipStream_t)stream;
+  Timed t(PF_KERNEL_ATTN_FWD, s);
+  return hip_status(pf::launch_relpos_fwd(a, s), "attention forward kernel");
+}
+
+pf_status pf_attn_relpos_bwd(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t H_kv,
+                             int32_t S, int32_t d, float scale, const pf_attn_tensor *Q,
+                             const pf_attn_tensor *K, const pf_attn_tensor *V, const float *bias,
+                             const pf_attn_tensor *O, const float *lse, const pf_attn_tensor *dO,
+                             const pf_attn_tensor *dQ, const pf_attn_tensor *dK, const pf_attn_tensor *dV,
+                             float *dtable, const int32_t *kv_len, void *workspace, size_t ws_bytes,
+                             void *stream) {
+  const RelposDims m{B, H, H_kv, S, S, d, scale};
+  pf_status st = check_relpos(L, R, m, bias, nullptr, kv_len);
+  if (st != PF_OK) return st;
+  if ((st = check_rows(Q, "Q", S, false, B, H)) != PF_OK || (st = check_rows(K, "K", S, false, B, H_kv)) != PF_OK ||
+      (st = check_rows(V, "V", S, false, B, H_kv)) != PF_OK || (st = check_rows(O, "O", S, false, B, H)) != PF_OK ||
+      (st = check_rows(dO, "dO", S, false, B, H)) != PF_OK || (st = check_rows(dQ, "dQ", S, true, B, H)) != PF_OK ||
+      (st = check_rows(dK, "dK", S, true, B, H_kv)) != PF_OK ||
+      (st = check_rows(dV, "dV", S, true, B, H_kv)) != PF_OK || (st = need_ptr(lse, "lse")) != PF_OK ||
+      (st = need_ptr(dtable, "dtable")) != PF_OK)
+    return st;
+  if ((st = need_ws(pf_attn_relpos_workspace_bytes(L, R, B, H, S), workspace, ws_bytes)) != PF_OK) return st;
+  if ((st = check_state(L)) != PF_OK || (st = relpos_state(R)) != PF_OK) return st;
+  pf::RelposArgs a = relpos_args(L, R, m, bias, nullptr, kv_len);
+  a.Q = view(Q); a.K = view(K); a.V = view(V); a.O = view(O); a.dO = view(dO);
+  a.dQ = view_out(dQ); a.dK = view_out(dK); a.dV = view_out(dV);
+  a.lse_in = lse;
+  a.delta = (float *)workspace;
+  a.partials = (float *)((char *)workspace + up256((size_t)B * H * S * sizeof(float)));
+  hipStream_t s = (hipStream_t)stream;
+  {
+    Timed t(PF_KERNEL_ATTN_BWD_DQ, s);
+    if ((st = hip_status(pf::launch_relpos_bwd_dq(a, s), "attention dQ kernel")) != PF_OK) return st;
+  }
+  {
+    Timed t(PF_KERNEL_ATTN_BWD_DKV, s);
+    if ((st = hip_status(pf::launch_relpos_bwd_dkv(a, s), "attention dK/dV kernel")) != PF_OK) return st;
+  }
+  Timed t(PF_KERNEL_REDUCE, s);
+  return hip_status(pf::launch_relpos_dtable(a, dtable, s), "table gradient sum");
 }
 
 }  // extern "C"

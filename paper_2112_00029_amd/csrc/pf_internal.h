@@ -319,6 +319,55 @@ struct ActBwdArgs {
 hipError_t launch_act_bwd(int dtype, const ActBwdArgs &a, hipStream_t s);
 hipError_t launch_act_dbias(int dtype, const ActBwdArgs &a, hipStream_t s);
 
+// Attention with a relative position bias (relpos.hip).  A tensor is rows of 64
+// contiguous bf16 elements, strides in elements.
+struct RowView {
+  const void *p;
+  int64_t seq, head, tok;
+};
+struct RowViewOut {
+  void *p;
+  int64_t seq, head, tok;
+};
+constexpr int kRelposMaxBuckets = 256;
+// info[d + nb - 1] of the blocks d block columns right of their block row: -1 if
+// every pair's bucket is -1, the bucket if all pairs share one, else
+// kRelposMixed + m, m naming the block's 64 words in `order`: word l holds the
+// distances 2 l and 2 l + 1 of the block's 128 (key - query + 64) in ascending
+// order of bucket: position, position << 8, bucket << 16, bucket << 24.
+constexpr int kRelposMixed = 256;
+struct RelposArgs {
+  RowView Q, K, V, O, dO;
+  RowViewOut Oout, dQ, dK, dV;
+  const float *bias;     // [H][bias_ld]: by distance (+ seq), then by descending distance
+  int64_t bias_ld;
+  float *lse;            // [B][H][Sq]
+  const float *lse_in;
+  float *delta;          // [B][H][Sq]
+  float *partials;       // [B][H][ntile][nbucket]
+  const int32_t *q_start, *kv_len;  // [B] or null
+  const int32_t *info;
+  const uint32_t *order;
+  const int32_t *row_ptr, *col_idx, *col_ptr, *row_idx;
+  int B, H, Hkv, G;      // G = H / Hkv
+  int Sq, Skv, seq, nb;  // seq: side of the layout, nb = seq / 64
+  int ntile;             // 64-row tiles per sequence and head of the launch
+  int nbucket;
+  int omin, omax;        // block offsets (key - query) that hold an attended distance
+  float scale;
+};
+struct RelposBiasArgs {
+  const int32_t *bucket;  // [2 seq]: bucket of distance e - seq, -1 at e = 0
+  const float *table;     // [H][nbucket]
+  float *out;             // [H][4 seq]
+  int seq, nbucket;
+};
+hipError_t launch_relpos_bias(const RelposBiasArgs &a, int H, hipStream_t s);
+hipError_t launch_relpos_fwd(const RelposArgs &a, hipStream_t s);
+hipError_t launch_relpos_bwd_dq(const RelposArgs &a, hipStream_t s);
+hipError_t launch_relpos_bwd_dkv(const RelposArgs &a, hipStream_t s);
+hipError_t launch_relpos_dtable(const RelposArgs &a, float *dtable, hipStream_t s);
+
 // The allocation-free attention backward keeps its row terms in a
 // file-scope device array of kAttnScratchRows floats (16 MiB per GPU);
 // attn_scratch gives this device's address of it (looked up on the first

@@ -1,0 +1,771 @@
+// Block-sparse attention with a learned relative position bias by buckets
+// (gfx950): S = scale Q K^T + table[head][bucket(key - query)] on the kept
+// 64 x 64 blocks, softmax over the kept keys, O = P V, and its gradients, that
+// of the table included.  Head dim 64, bf16 I/O, fp32 softmax and sums.
+//
+// The products are those of attn_kernels.hip: two waves per 64-row block, 32
+// rows each, everything transposed so that a lane owns one row, 32x32x16 MFMA,
+// tiles copied global -> LDS directly into swizzled rows.  What is added:
+//
+//  * The bias depends on key - query alone, so a 64 x 64 block needs 127 values
+//    of its head, which relpos_bias_kernel has laid out by distance, in log2 units.
+//    Most blocks lie in one bucket (beyond the largest distance every block
+//    does): there the bias is one scalar, added in the fma that scales the score, at
+//    no cost.  For the others the block's 128-value window goes to LDS as 128 units of
+//    16 bytes, unit W holding values W .. W + 3: a lane's four consecutive keys are
+//    then one aligned ds_read_b128 whatever its row, free of bank conflicts, and the
+//    eight reads of a block differ by immediates.
+//  * A pair whose bucket is -1 has bias -inf: probability 0.  Blocks wholly
+//    outside the attended distances, and key blocks past a sequence's length, are
+//    cut off a row's block list before the loop; the running maximum starts at a
+//    finite -1e30, so that a row with nothing to attend to sums to 0 (O = 0, lse =
+//    -inf) without a NaN on the way.
+//  * Rows and tokens past a sequence's length read as zeros by the buffers'
+//    range check, whatever the memory holds there.
+//  * Table gradient: sums of dS per bucket, in fp32.  A block of one bucket adds up
+//    in a register per lane.  Of the others the sums along the diagonals are
+//    wanted: register e of an accumulator holds one key for 16 query lanes, so two DPP
+//    row shifts (left by the key's index in its 16, right by 16 minus it, zeros
+//    shifted in) add it to the diagonals that end and begin in those 16 keys: two
+//    VALU instructions per 64 scores and no LDS.  The diagonals then go to the
+//    plan's order by bucket and a segmented scan over the wave leaves one sum per
+//    bucket.  No atomics; every sum has a fixed order.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "pf_attn.h"
+#include "pf_launch.h"
+
+namespace pf {
+namespace {
+
+constexpr int WIN = 128 * 16;        // bytes of a bias window in LDS
+constexpr float kFloor = -1e30f;     // running maximum before any key (log2 units)
+
+// Token rows [0, n) of a head: range-checked, 16 bytes at a time.
+__device__ __forceinline__ rsrc_t rows_rsrc(const bf16_t *p, int n, uint32_t row_bytes) {
+  return make_rsrc(p, n > 0 ? (int64_t)(n - 1) * row_bytes + D * 2 : 0);
+}
+
+// Copies of one tile of 64 token rows by the two waves of a workgroup, as
+// TileCopy of attn_kernels.hip with a row stride.  All of the address is in the
+// lane offset, which the range check sees.
+struct RowCopy {
+  uint32_t voff[2], step;
+  int w4;
+  __device__ __forceinline__ void init(int lane, int w, uint32_t row_bytes) {
+    const int x = (((lane >> 4) & 1) << 2) | (((lane >> 5) & 1) << 1);
+    w4 = w * 4;
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+      voff[o] = (uint32_t)(w4 * 8 + (lane >> 3)) * row_bytes + (uint32_t)(((lane & 7) ^ x ^ o) << 4);
+    step = 8 * row_bytes;
+  }
+  // off: byte offset of the tile's first row.
+  __device__ __forceinline__ void issue(rsrc_t r, uint32_t off, uint8_t *tile) const {
+    sfor<4>([&](auto i) __attribute__((always_inline)) {
+      dma16(r, tile + (w4 + i) * 1024, voff[i & 1] + off + i * step, 0);
+    });
+  }
+};
+
+// A window of the bias (128 values from byte offset `off` of the head's
+// array) as 16-byte units; wave w copies units 64 w .. 64 w + 63.
+__device__ __forceinline__ void copy_window(rsrc_t r, int off, uint8_t *win, int lane, int w) {
+  dma16(r, win + w * 1024, (uint32_t)(off + (w * 64 + lane) * 4), 0);
+}
+
+// MFMA operand rows i0 + l % 32 (k as frag_r) from range-checked memory.
+__device__ __forceinline__ bf16x8 frag_b(rsrc_t r, int row, uint32_t row_bytes, int ks, int lane) {
+  const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(
+      r, (int)((uint32_t)row * row_bytes + ks * 32 + (lane >> 5) * 16), 0, 0);
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// Row l % 32's 64 columns (two transposed accumulators) times scale, or zeros
+// where !live, to dst when `store`.
+__device__ __forceinline__ void put_row(bf16_t *dst, const f32x16 (&o)[2], float scale, bool live,
+                                        bool store, int lane) {
+#pragma unroll
+  for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int e = 8 * p;
+      const uint32_t x0 = pack2(o[dt][e] * scale, o[dt][e + 1] * scale);
+      const uint32_t x1 = pack2(o[dt][e + 2] * scale, o[dt][e + 3] * scale);
+      const uint32_t y0 = pack2(o[dt][e + 4] * scale, o[dt][e + 5] * scale);
+      const uint32_t y1 = pack2(o[dt][e + 6] * scale, o[dt][e + 7] * scale);
+      const auto s0 = __builtin_amdgcn_permlane32_swap(x0, y0, false, false);
+      const auto s1 = __builtin_amdgcn_permlane32_swap(x1, y1, false, false);
+      u32x4 v = {s0[0], s1[0], s0[1], s1[1]};
+      if (!live) v = u32x4{0u, 0u, 0u, 0u};
+      if (store) *(u32x4 *)(dst + dt * 32 + p * 16 + (lane >> 5) * 8) = v;
+    }
+}
+
+// x of another lane by a DPP control; lanes without a source read 0.
+template <int CTRL>
+__device__ __forceinline__ float dpp0(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dppi(int old, int x) {
+  return __builtin_amdgcn_update_dpp(old, x, CTRL, ROWS, 0xf, false);
+}
+constexpr int kRowShl = 0x100, kRowShr = 0x110, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
+
+// One step of a scan over the lanes of a wave, segmented by id (equal ids lie
+// next to one another): adds the source lane's sum where the ids agree.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void seg_step(float &sum, int id) {
+  const int oid = dppi<CTRL, ROWS>(-1, id);
+  const float o = __uint_as_float(dppi<CTRL, ROWS>(0, (int)__float_as_uint(sum)));
+  sum += oid == id ? o : 0.f;
+}
+__device__ __forceinline__ void seg_scan(float &sum, int id) {
+  seg_step<kRowShr + 1, 0xf>(sum, id);
+  seg_step<kRowShr + 2, 0xf>(sum, id);
+  seg_step<kRowShr + 4, 0xf>(sum, id);
+  seg_step<kRowShr + 8, 0xf>(sum, id);
+  seg_step<kRowBcast15, 0xa>(sum, id);
+  seg_step<kRowBcast31, 0xc>(sum, id);
+}
+
+// First and one past the last position of a row's block list whose column
+// lies in [lo, hi] (columns ascend).
+__device__ __forceinline__ void trim(const int32_t *col, int &p0, int &p1, int lo, int hi) {
+  if (p0 < p1 && ld_meta(col + p1 - 1) > hi) {
+    int a = p0, b = p1 - 1;  // first position with a column above hi
+    while (a < b) {
+      const int m = (a + b) >> 1;
+      if (ld_meta(col + m) > hi) b = m;
+      else a = m + 1;
+    }
+    p1 = a;
+  }
+  if (p0 < p1 && ld_meta(col + p0) < lo) {
+    int a = p0 + 1, b = p1;  // first position with a column of lo or more
+    while (a < b) {
+      const int m = (a + b) >> 1;
+      if (ld_meta(col + m) >= lo) b = m;
+      else a = m + 1;
+    }
+    p0 = a;
+  }
+}
+
+// Tokens of sequence b.
+__device__ __forceinline__ int seq_len(const RelposArgs &a, int b) {
+  return a.kv_len ? min(max(ld_meta(a.kv_len + b), 0), a.Skv) : a.Skv;
+}
+
+// Bias of a block: what the plan says about its distances (info, see
+// RelposArgs) and the bias of its middle one, which is that of all of them when
+// info names one bucket.
+struct BlockBias {
+  int info;
+  float mid;
+};
+
+// ---------------------------------------------------------------------------
+// Forward
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  uint8_t *const ks = stage_buf<0, TILE>(), *const vs = stage_buf<1, TILE>();
+  uint8_t *const w0 = stage_buf<2, WIN>(), *const w1 = stage_buf<3, WIN>();
+
+  const int bid = xcd_remap(blockIdx.x, gridDim.x);
+  const int bh = bid / a.ntile, tile = bid % a.ntile;
+  const int b = bh / a.H, h = bh % a.H, hk = h / a.G;
+  const int len = seq_len(a, b);
+  const int start = a.q_start ? min(max(ld_meta(a.q_start + b), 0), a.seq) : 0;
+  const int qb = (start >> 6) + tile;
+  // Row index of this lane's query, and the rows that hold tokens.
+  const int row = qb * BQ + w * 32 + (lane & 31) - start;
+  const int nrow = min(max(len - start, 0), a.Sq);
+  if (qb * BQ - start >= a.Sq) return;  // a tile past the last row
+
+  const bf16_t *Q = (const bf16_t *)a.Q.p + b * a.Q.seq + h * a.Q.head;
+  const bf16_t *K = (const bf16_t *)a.K.p + b * a.K.seq + hk * a.K.head;
+  const bf16_t *V = (const bf16_t *)a.V.p + b * a.V.seq + hk * a.V.head;
+  const float *bias = a.bias + (int64_t)h * a.bias_ld;
+  const uint32_t qrb = (uint32_t)(a.Q.tok * 2), krb = (uint32_t)(a.K.tok * 2), vrb = (uint32_t)(a.V.tok * 2);
+  const rsrc_t rq = rows_rsrc(Q, nrow, qrb), rk = rows_rsrc(K, len, krb), rv = rows_rsrc(V, len, vrb);
+  const rsrc_t rb = make_rsrc(bias, (int64_t)a.seq * 8);
+  const float c = a.scale * kLog2e;
+
+  int p0 = 0, p1 = 0;
+  if (nrow > qb * BQ - start && qb < a.nb) {
+    p0 = ld_meta(a.row_ptr + qb);
+    p1 = ld_meta(a.row_ptr + qb + 1);
+    trim(a.col_idx, p0, p1, qb + a.omin, min(qb + a.omax, (len + BQ - 1) / BQ - 1));
+  }
+  f32x16 o[2];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
+  float m_run = kFloor, l_run = 0.f;  // l_run: this lane's keys only
+
+  if (p0 < p1) {
+    RowCopy kc, vc;
+    kc.init(lane, w, krb);
+    vc.init(lane, w, vrb);
+    auto block_bias = [&](int col) __attribute__((always_inline)) {
+      const int d = col - qb;
+      return BlockBias{ld_meta(a.info + d + a.nb - 1), ld_meta(bias + d * BQ + a.seq)};
+    };
+    auto issue_k = [&](int col, uint8_t *win) __attribute__((always_inline)) {
+      kc.issue(rk, (uint32_t)(col * BQ) * krb, ks);
+      copy_window(rb, ((col - qb) * BQ + a.seq - BQ) * 4, win, lane, w);
+    };
+    int ccur = ld_meta(a.col_idx + p0);
+    issue_k(ccur, w0);
+    bf16x8 qf[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) qf[i] = frag_b(rq, row, qrb, i, lane);
+    BlockBias bb = block_bias(ccur);
+    // The next block, one iteration ahead (the last one again at the end: its
+    // copies land and are not read).
+    int cn = ld_meta(a.col_idx + min(p0 + 1, p1 - 1));
+
+    // Unit of this lane's first key in the window: key - query + 64.
+    const int unit = 64 + (lane >> 5) * 4 - (w * 32 + (lane & 31));
+    f32x16 s[2];
+    auto step = [&](int p, const uint8_t *wc, uint8_t *wn) __attribute__((always_inline)) {
+      wait_vm<0>();  // this wave's K and window have landed,
+      barrier();     // every wave's have, and the last block's V is read
+      vc.issue(rv, (uint32_t)(ccur * BQ) * vrb, vs);
+      const BlockBias bn = block_bias(cn);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[kt][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[kt] = MFMA32(frag_r(ks, kt * 32, i, lane), qf[i], s[kt]);
+      }
+      wait_vm<4>();  // (no wait: the four V copies may be in flight)
+      barrier();     // every wave has read K
+      issue_k(cn, wn);
+      // Scores in log2 units: s cm + ca.
+      float cm = c, ca = bb.mid;
+      const int tail = len - ccur * BQ;  // keys of the block that exist
+      if (bb.info >= kRelposMixed || tail < BQ) {
+        const uint8_t *u = wc + unit * 16;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int e4 = 0; e4 < 4; ++e4) {
+            const f32x4 bv = *(const f32x4 *)(u + (kt * 32 + e4 * 8) * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[kt][e4 * 4 + j] = __builtin_fmaf(s[kt][e4 * 4 + j], c, bv[j]);
+          }
+        if (tail < BQ) {
+          const int k0 = (lane >> 5) * 4;
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (k0 + kt * 32 + (e >> 2) * 8 + (e & 3) >= tail) s[kt][e] = -INFINITY;
+        }
+        cm = 1.f;
+        ca = 0.f;
+      }
+      float bmax = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) bmax = fmaxf(bmax, s[kt][e]);
+      // The reference m_run (the same in both lanes of a query) moves only when
+      // some lane's maximum grew by more than 8 (log2 units): until then the
+      // probabilities stay below 2^8.
+      const float bm = __builtin_fmaf(bmax, cm, ca);
+      if (__builtin_amdgcn_ballot_w64(bm > m_run + 8.0f)) {
+        const float m_cand = fmaxf(m_run, max_xor32(bm));
+        const float alpha = fast_exp2(m_run - m_cand);
+        m_run = m_cand;
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+      }
+      const float off = ca - m_run;
+      float rs = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = fast_exp2(__builtin_fmaf(s[kt][e], cm, off));
+          s[kt][e] = x;
+          rs += x;
+        }
+      l_run += rs;
+      ccur = cn;
+      bb = bn;
+      cn = ld_meta(a.col_idx + min(p + 2, p1 - 1));
+      wait_vm<5>();  // V has landed; the next K and window stay in flight
+      barrier();
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const bf16x8 pb = pack_k(s[kt], j);
+#pragma unroll
+          for (int dt = 0; dt < 2; ++dt)
+            o[dt] = MFMA32(frag_t(vs, kt * 32 + j * 16, dt * 32, lane), pb, o[dt]);
+        }
+    };
+    for (int p = p0; p < p1; p += 2) {
+      step(p, w0, w1);
+      if (p + 1 < p1) step(p + 1, w1, w0);
+    }
+    wait_vm<0>();  // no copy outlives the workgroup
+  }
+
+  l_run = add_xor32(l_run);
+  const bool store = row >= 0 && row < a.Sq, live = row < nrow;
+  bf16_t *O = (bf16_t *)a.Oout.p + b * a.Oout.seq + h * a.Oout.head + (int64_t)row * a.Oout.tok;
+  put_row(O, o, l_run == 0.f ? 0.f : 1.f / l_run, live, store, lane);
+  if (lane < 32 && store)
+    a.lse[(int64_t)bh * a.Sq + row] = live ? (m_run + __log2f(l_run)) * kLn2 : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------
+// Backward, pass 1: delta, dQ, and the table gradient's sums of this block row
+// ---------------------------------------------------------------------------
+constexpr int DPITCH = 136;  // floats per diagonal row (units 1 .. 132 are written)
+
+__global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  uint8_t *const ks = stage_buf<0, TILE>(), *const vs = stage_buf<1, TILE>();
+  uint8_t *const w0 = stage_buf<2, WIN>(), *const w1 = stage_buf<3, WIN>();
+  // Per wave: the diagonals of a block by lane row (16 queries, one half of the
+  // keys), zero where a row has none; sums per bucket.
+  __shared__ float diag[2][4 * DPITCH];
+  __shared__ float bsum[2][kRelposMaxBuckets];
+
+  const int bid = xcd_remap(blockIdx.x, gridDim.x);
+  const int bh = bid / a.ntile, qb = bid % a.ntile;
+  const int b = bh / a.H, h = bh % a.H, hk = h / a.G;
+  const int len = seq_len(a, b);
+  const int row = qb * BQ + w * 32 + (lane & 31);
+
+  const bf16_t *Q = (const bf16_t *)a.Q.p + b * a.Q.seq + h * a.Q.head;
+  const bf16_t *K = (const bf16_t *)a.K.p + b * a.K.seq + hk * a.K.head;
+  const bf16_t *V = (const bf16_t *)a.V.p + b * a.V.seq + hk * a.V.head;
+  const bf16_t *O = (const bf16_t *)a.O.p + b * a.O.seq + h * a.O.head;
+  const bf16_t *dO = (const bf16_t *)a.dO.p + b * a.dO.seq + h * a.dO.head;
+  const float *bias = a.bias + (int64_t)h * a.bias_ld;
+  const uint32_t qrb = (uint32_t)(a.Q.tok * 2), krb = (uint32_t)(a.K.tok * 2), vrb = (uint32_t)(a.V.tok * 2);
+  const uint32_t orb = (uint32_t)(a.O.tok * 2), grb = (uint32_t)(a.dO.tok * 2);
+  const rsrc_t rq = rows_rsrc(Q, len, qrb), rk = rows_rsrc(K, len, krb), rv = rows_rsrc(V, len, vrb);
+  const rsrc_t ro = rows_rsrc(O, len, orb), rg = rows_rsrc(dO, len, grb);
+  const rsrc_t rb = make_rsrc(bias, (int64_t)a.seq * 8);
+  const float c = a.scale * kLog2e;
+
+  for (int i = lane; i < 4 * DPITCH; i += 64) diag[w][i] = 0.f;
+  for (int i = lane; i < a.nbucket; i += 64) bsum[w][i] = 0.f;
+
+  int p0 = 0, p1 = 0;
+  if (len > qb * BQ) {
+    p0 = ld_meta(a.row_ptr + qb);
+    p1 = ld_meta(a.row_ptr + qb + 1);
+    trim(a.col_idx, p0, p1, qb + a.omin, min(qb + a.omax, (len + BQ - 1) / BQ - 1));
+  }
+  f32x16 dq[2];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) dq[0][e] = dq[1][e] = 0.f;
+
+  // delta = rowsum(dO o O); rows past the length read zeros.
+  bf16x8 qf[4], gf[4];
+  float delta = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    qf[i] = frag_b(rq, row, qrb, i, lane);
+    gf[i] = frag_b(rg, row, grb, i, lane);
+    const bf16x8 of = frag_b(ro, row, orb, i, lane);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) delta += (float)of[e] * (float)gf[i][e];
+  }
+  delta = add_xor32(delta);
+  const bool live = row < len, store = row < a.Sq;
+  if (lane < 32 && store) a.delta[(int64_t)bh * a.Sq + row] = delta;
+  // Rows without a token or without a key: probability 0 everywhere.
+  const float lse = live ? a.lse_in[(int64_t)bh * a.Sq + row] : -INFINITY;
+  const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+
+  if (p0 < p1) {
+    RowCopy kc, vc;
+    kc.init(lane, w, krb);
+    vc.init(lane, w, vrb);
+    auto block_bias = [&](int col) __attribute__((always_inline)) {
+      const int d = col - qb;
+      return BlockBias{ld_meta(a.info + d + a.nb - 1), ld_meta(bias + d * BQ + a.seq)};
+    };
+    auto issue_k = [&](int col, uint8_t *win) __attribute__((always_inline)) {
+      kc.issue(rk, (uint32_t)(col * BQ) * krb, ks);
+      copy_window(rb, ((col - qb) * BQ + a.seq - BQ) * 4, win, lane, w);
+    };
+    int ccur = ld_meta(a.col_idx + p0);
+    vc.issue(rv, (uint32_t)(ccur * BQ) * vrb, vs);
+    issue_k(ccur, w0);
+    BlockBias bb = block_bias(ccur);
+    int cn = ld_meta(a.col_idx + min(p0 + 1, p1 - 1));
+    const int unit = 64 + (lane >> 5) * 4 - (w * 32 + (lane & 31));
+    // First diagonal unit of this lane: key - query + 64 at key 0 of its half,
+    // query its row's first less lane % 16 (see the shifts below).
+    float *const dg = &diag[w][(lane >> 4) * DPITCH + 64 + (lane >> 5) * 4 - (lane & 15) -
+                               16 * ((lane >> 4) & 1) - 32 * w];
+
+    int ucur = -1;       // bucket that usum belongs to
+    float usum = 0.f;
+    auto flush = [&]() __attribute__((always_inline)) {
+      if (ucur >= 0) {
+        seg_scan(usum, 0);
+        if (lane == 63) bsum[w][ucur] += usum;
+      }
+      usum = 0.f;
+    };
+
+    f32x16 s, dp;
+    auto scores = [&](int kt) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s = MFMA32(frag_r(ks, kt * 32, i, lane), qf[i], s);
+        dp = MFMA32(frag_r(vs, kt * 32, i, lane), gf[i], dp);
+      }
+    };
+    auto step = [&](int p, const uint8_t *wc, uint8_t *wn) __attribute__((always_inline)) {
+      wait_vm<0>();  // this wave's copies of the block have landed,
+      barrier();     // every wave's have
+      const int tail = len - ccur * BQ;
+      const bool mixed = bb.info >= kRelposMixed;
+      // Order by bucket of a mixed block's distances, two per lane.
+      const uint32_t ord = mixed ? a.order[(int64_t)(bb.info - kRelposMixed) * 64 + lane] : 0u;
+      if (!mixed && bb.info != ucur) {
+        flush();
+        ucur = bb.info;
+      }
+      float acc[5] = {};
+      auto grads = [&](auto kt_) __attribute__((always_inline)) {
+        constexpr int kt = decltype(kt_)::value;
+        float cm = c, ca = bb.mid - lse2;
+        if (mixed || tail < BQ) {
+          const uint8_t *u = wc + unit * 16;
+#pragma unroll
+          for (int e4 = 0; e4 < 4; ++e4) {
+            const f32x4 bv = *(const f32x4 *)(u + (kt * 32 + e4 * 8) * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[e4 * 4 + j] = __builtin_fmaf(s[e4 * 4 + j], c, bv[j]);
+          }
+          if (tail < BQ) {
+            const int k0 = (lane >> 5) * 4 + kt * 32;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (k0 + (e >> 2) * 8 + (e & 3) >= tail) s[e] = -INFINITY;
+          }
+          cm = 1.f;
+          ca = -lse2;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float pr = fast_exp2(__builtin_fmaf(s[e], cm, ca));
+          s[e] = pr * (dp[e] - delta);  // dS^T
+        }
+        if (mixed) {
+          // Key 16 a + j + 4 (l / 32) of this half, query lane x of its 16:
+          // diagonal 16 a - x from lane x + j, 16 (a + 1) - x from x + j - 16.
+          sfor<16>([&](auto ee) __attribute__((always_inline)) {
+            constexpr int e = decltype(ee)::value;
+            constexpr int j = ((e >> 2) & 1) * 8 + (e & 3), m = kt * 2 + (e >> 3);
+            if constexpr (j == 0) {
+              acc[m] += s[e];
+            } else {
+              acc[m] += dpp0<kRowShl + j>(s[e]);
+              acc[m + 1] += dpp0<kRowShr + 16 - j>(s[e]);
+            }
+          });
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) usum += s[e];
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const bf16x8 d = pack_k(s, j);
+#pragma unroll
+          for (int dt = 0; dt < 2; ++dt)
+            dq[dt] = MFMA32(frag_t(ks, kt * 32 + j * 16, dt * 32, lane), d, dq[dt]);
+        }
+      };
+      const BlockBias bn = block_bias(cn);
+      scores(0);
+      grads(std::integral_constant<int, 0>{});
+      scores(1);
+      wait_vm<0>();
+      barrier();  // every wave has read V
+      vc.issue(rv, (uint32_t)(cn * BQ) * vrb, vs);
+      grads(std::integral_constant<int, 1>{});
+      if (mixed) {
+#pragma unroll
+        for (int m = 0; m < 5; ++m) dg[16 * m] = acc[m];
+        const int o0 = ord & 127, o1 = (ord >> 8) & 127, i0 = (ord >> 16) & 255, i1 = ord >> 24;
+        const float *dd = diag[w];
+        float v0 = 0.f, v1 = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          v0 += dd[r * DPITCH + o0];
+          v1 += dd[r * DPITCH + o1];
+        }
+        // Two sorted distances per lane.  A lane whose two lie in different
+        // buckets closes the first one's segment with its v0.
+        float sum = i0 == i1 ? v0 + v1 : v1;
+        seg_scan(sum, i1);
+        // Sum of the lanes before, if their last bucket is this lane's first.
+        const int pid = dppi<0x138, 0xf>(-1, i1);  // wave_shr:1
+        const float prev = __uint_as_float(dppi<0x138, 0xf>(0, (int)__float_as_uint(sum)));
+        const int nid = dppi<0x130, 0xf>(-1, i0);  // wave_shl:1
+        if (i0 != i1) bsum[w][i0] += v0 + (pid == i0 ? prev : 0.f);
+        if (nid != i1) bsum[w][i1] += sum;
+      }
+      ccur = cn;
+      bb = bn;
+      cn = ld_meta(a.col_idx + min(p + 2, p1 - 1));
+      wait_vm<4>();
+      barrier();  // every wave has read K
+      issue_k(ccur, wn);
+    };
+    for (int p = p0; p < p1; p += 2) {
+      step(p, w0, w1);
+      if (p + 1 < p1) step(p + 1, w1, w0);
+    }
+    flush();
+    wait_vm<0>();  // no copy outlives the workgroup
+  }
+  put_row((bf16_t *)a.dQ.p + b * a.dQ.seq + h * a.dQ.head + (int64_t)row * a.dQ.tok, dq, a.scale, live,
+          store, lane);
+  __syncthreads();
+  float *P = a.partials + ((int64_t)bh * a.ntile + qb) * a.nbucket;
+  for (int i = threadIdx.x; i < a.nbucket; i += 128) P[i] = bsum[0][i] + bsum[1][i];
+}
+
+// ---------------------------------------------------------------------------
+// Backward, pass 2: dK and dV (a key block of one key/value head; its G query
+// heads and their kept query blocks one after another)
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(128) void relpos_bwd_dkv_kernel(RelposArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  uint8_t *const qs0 = stage_buf<0, TILE>(), *const gs0 = stage_buf<1, TILE>();
+  uint8_t *const qs1 = stage_buf<2, TILE>(), *const gs1 = stage_buf<3, TILE>();
+  uint8_t *const w0 = stage_buf<4, WIN>(), *const w1 = stage_buf<5, WIN>();
+  // Row terms of the 64 queries: lse (log2 units), then -delta.
+  __shared__ __attribute__((aligned(16))) float rt0[2 * BQ], rt1[2 * BQ];
+
+  const int bid = xcd_remap(blockIdx.x, gridDim.x);
+  const int bhk = bid / a.ntile, kb = bid % a.ntile;
+  const int b = bhk / a.Hkv, hk = bhk % a.Hkv;
+  const int len = seq_len(a, b);
+  const int key = kb * BQ + w * 32 + (lane & 31);
+
+  const bf16_t *K = (const bf16_t *)a.K.p + b * a.K.seq + hk * a.K.head;
+  const bf16_t *V = (const bf16_t *)a.V.p + b * a.V.seq + hk * a.V.head;
+  const uint32_t qrb = (uint32_t)(a.Q.tok * 2), krb = (uint32_t)(a.K.tok * 2), vrb = (uint32_t)(a.V.tok * 2);
+  const uint32_t grb = (uint32_t)(a.dO.tok * 2);
+  const float c = a.scale * kLog2e;
+
+  int p0 = 0, p1 = 0;
+  if (len > kb * BQ) {
+    p0 = ld_meta(a.col_ptr + kb);
+    p1 = ld_meta(a.col_ptr + kb + 1);
+    trim(a.row_idx, p0, p1, kb - a.omax, min(kb - a.omin, (len + BQ - 1) / BQ - 1));
+  }
+  f32x16 dk[2], dv[2];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) dk[0][e] = dk[1][e] = dv[0][e] = dv[1][e] = 0.f;
+
+  if (p0 < p1) {
+    const rsrc_t rk = rows_rsrc(K, len, krb), rv = rows_rsrc(V, len, vrb);
+    RowCopy qc, gc;
+    qc.init(lane, w, qrb);
+    gc.init(lane, w, grb);
+    bf16x8 kf[4], vf[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      kf[i] = frag_b(rk, key, krb, i, lane);
+      vf[i] = frag_b(rv, key, vrb, i, lane);
+    }
+    // Work item: query head g of the group, position p of the column's list.
+    struct Item {
+      int g, p;
+    };
+    auto next = [&](Item it) __attribute__((always_inline)) {
+      return it.p + 1 < p1 ? Item{it.g, it.p + 1} : Item{it.g + 1, p0};
+    };
+    float rt = 0.f;  // row term of the block in flight (wave 0: lse, wave 1: -delta)
+    BlockBias bf{0, 0.f};  // its bias
+    auto issue = [&](Item it, uint8_t *qt, uint8_t *gt, uint8_t *win) __attribute__((always_inline)) {
+      const int h = hk * a.G + it.g, qb = ld_meta(a.row_idx + it.p);
+      const bf16_t *Q = (const bf16_t *)a.Q.p + b * a.Q.seq + h * a.Q.head;
+      const bf16_t *dO = (const bf16_t *)a.dO.p + b * a.dO.seq + h * a.dO.head;
+      qc.issue(rows_rsrc(Q, len, qrb), (uint32_t)(qb * BQ) * qrb, qt);
+      gc.issue(rows_rsrc(dO, len, grb), (uint32_t)(qb * BQ) * grb, gt);
+      // The head's bias by descending distance: by query - key.
+      const float *rev = a.bias + (int64_t)h * a.bias_ld + 2 * (int64_t)a.seq;
+      copy_window(make_rsrc(rev, (int64_t)a.seq * 8), ((qb - kb) * BQ + a.seq - BQ) * 4, win, lane, w);
+      bf = BlockBias{ld_meta(a.info + (kb - qb) + a.nb - 1), ld_meta(rev + (qb - kb) * BQ + a.seq)};
+      const int q = qb * BQ + lane;
+      const float *src = (w == 0 ? a.lse_in : a.delta) + (int64_t)(b * a.H + h) * a.Sq;
+      float x = q < len ? src[q] : (w == 0 ? -INFINITY : 0.f);
+      rt = w == 0 ? (x == -INFINITY ? INFINITY : x * kLog2e) : -x;
+    };
+    const int unit = 64 + (lane >> 5) * 4 - (w * 32 + (lane & 31));
+    auto step = [&](Item nx, uint8_t *qt, uint8_t *gt, const uint8_t *wc, float (&rc)[2 * BQ],
+                    uint8_t *qn, uint8_t *gn, uint8_t *wn) __attribute__((always_inline)) {
+      wait_vm<0>();
+      // The stage's row terms were last read two blocks ago, before the
+      // previous barrier.
+      rc[w * BQ + lane] = rt;
+      const BlockBias bb = bf;
+      wait_vm<0>();
+      barrier();
+      if (nx.g < a.G) issue(nx, qn, gn, wn);
+      const bool mixed = bb.info >= kRelposMixed;
+      const float *lsep = &rc[(lane >> 5) * 4], *delp = lsep + BQ;
+      const uint8_t *u = wc + unit * 16;
+#pragma unroll
+      for (int qq = 0; qq < 2; ++qq) {
+        // S[query][key], dP[query][key] of 32 queries x this wave's 32 keys;
+        // dP starts at -delta.
+        f32x16 s = {}, dp;
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          const f32x4 de = *(const f32x4 *)(delp + qq * 32 + e4 * 8);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dp[e4 * 4 + j] = de[j];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s = MFMA32(frag_r(qt, qq * 32, i, lane), kf[i], s);
+          dp = MFMA32(frag_r(gt, qq * 32, i, lane), vf[i], dp);
+        }
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          const f32x4 ls = *(const f32x4 *)(lsep + qq * 32 + e4 * 8);
+          f32x4 bv = {bb.mid, bb.mid, bb.mid, bb.mid};
+          if (mixed) bv = *(const f32x4 *)(u + (qq * 32 + e4 * 8) * 16);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int e = e4 * 4 + j;
+            const float pr = fast_exp2(__builtin_fmaf(s[e], c, bv[j] - ls[j]));
+            s[e] = pr;
+            dp[e] = pr * dp[e];  // dS
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const bf16x8 pb = pack_k(s, j), sb = pack_k(dp, j);
+#pragma unroll
+          for (int dt = 0; dt < 2; ++dt) {
+            dv[dt] = MFMA32(frag_t(gt, qq * 32 + j * 16, dt * 32, lane), pb, dv[dt]);
+            dk[dt] = MFMA32(frag_t(qt, qq * 32 + j * 16, dt * 32, lane), sb, dk[dt]);
+          }
+        }
+      }
+    };
+    Item it{0, p0};
+    issue(it, qs0, gs0, w0);
+    while (it.g < a.G) {
+      Item n1 = next(it);
+      step(n1, qs0, gs0, w0, rt0, qs1, gs1, w1);
+      it = n1;
+      if (it.g >= a.G) break;
+      n1 = next(it);
+      step(n1, qs1, gs1, w1, rt1, qs0, gs0, w0);
+      it = n1;
+    }
+  }
+  const bool live = key < len, store = key < a.Skv;
+  put_row((bf16_t *)a.dK.p + b * a.dK.seq + hk * a.dK.head + (int64_t)key * a.dK.tok, dk, a.scale, live,
+          store, lane);
+  put_row((bf16_t *)a.dV.p + b * a.dV.seq + hk * a.dV.head + (int64_t)key * a.dV.tok, dv, 1.f, live, store,
+          lane);
+}
+
+// ---------------------------------------------------------------------------
+// The bias by distance, and the sum of the table gradient's partials
+// ---------------------------------------------------------------------------
+// out[h][d + seq] = log2(e) table[h][bucket(d)], -inf where the bucket is -1; then
+// the same by descending distance, out[h][2 seq + f] = out[h][2 seq - f] (distance
+// seq - f).  Entry 0 of either (distance -seq, seq) is never used: -inf.
+__global__ __launch_bounds__(256) void relpos_bias_kernel(RelposBiasArgs a) {
+  const int e = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y;
+  if (e >= 2 * a.seq) return;
+  const int id = a.bucket[e];
+  const float v = id < 0 ? -INFINITY : a.table[(int64_t)h * a.nbucket + id] * kLog2e;
+  float *o = a.out + (int64_t)h * 4 * a.seq;
+  o[e] = v;
+  o[2 * (int64_t)a.seq + (e ? 2 * a.seq - e : 0)] = v;
+}
+
+// dtable[h][c]: partials [B][H][ntile][nbucket] added over sequences and block
+// rows in a fixed order.  A workgroup takes 64 buckets of a head, 16 threads a
+// bucket.
+__global__ __launch_bounds__(1024) void relpos_dtable_kernel(const float *P, int B, int H, int ntile,
+                                                             int nbucket, float *dtable) {
+  __shared__ float red[1024];
+  const int cc = threadIdx.x & 63, part = threadIdx.x >> 6;
+  const int c = blockIdx.x * 64 + cc, h = blockIdx.y;
+  const int64_t rows = (int64_t)B * ntile;
+  float s = 0.f;
+  if (c < nbucket)
+    for (int64_t r = part; r < rows; r += 16) {
+      const int64_t b = r / ntile, t = r % ntile;
+      s += P[((b * H + h) * ntile + t) * nbucket + c];
+    }
+  red[threadIdx.x] = s;
+  __syncthreads();
+  if (part || c >= nbucket) return;
+  for (int p = 1; p < 16; ++p) s += red[p * 64 + cc];
+  dtable[(int64_t)h * nbucket + c] = s;
+}
+
+}  // namespace
+
+hipError_t launch_relpos_fwd(const RelposArgs &a, hipStream_t s) {
+  const int64_t grid = (int64_t)a.B * a.H * a.ntile;
+  if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
+  launch_kernel(relpos_fwd_kernel, dim3((unsigned)grid), dim3(128), s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_relpos_bwd_dq(const RelposArgs &a, hipStream_t s) {
+  const int64_t grid = (int64_t)a.B * a.H * a.ntile;
+  if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
+  launch_kernel(relpos_bwd_dq_kernel, dim3((unsigned)grid), dim3(128), s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_relpos_bwd_dkv(const RelposArgs &a, hipStream_t s) {
+  const int64_t grid = (int64_t)a.B * a.Hkv * a.ntile;
+  if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
+  launch_kernel(relpos_bwd_dkv_kernel, dim3((unsigned)grid), dim3(128), s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_relpos_dtable(const RelposArgs &a, float *dtable, hipStream_t s) {
+  launch_kernel(relpos_dtable_kernel, dim3((unsigned)((a.nbucket + 63) / 64), (unsigned)a.H), dim3(1024), s,
+                (const float *)a.partials, a.B, a.H, a.ntile, a.nbucket, dtable);
+  return hipGetLastError();
+}
+
+hipError_t launch_relpos_bias(const RelposBiasArgs &a, int H, hipStream_t s) {
+  launch_kernel(relpos_bias_kernel, dim3((unsigned)((2 * (int64_t)a.seq + 255) / 256), (unsigned)H),
+                dim3(256), s, a);
+  return hipGetLastError();
+}
+
+}  // namespace pf

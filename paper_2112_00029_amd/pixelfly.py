@@ -75,6 +75,12 @@ class pf_linear_plan(ctypes.Structure):
                                                        ("tn_tile", _i32), ("tn_shared", _i32)]
 
 
+class pf_attn_tensor(ctypes.Structure):
+    _fields_ = [("data", _p), ("seq", _i64), ("head", _i64), ("token", _i64)]
+
+
+_rows_p = ctypes.POINTER(pf_attn_tensor)
+
 _SIGS = {
     "pf_layout_create": (_i32, [_i64, _i64, _i32, _i32, ctypes.POINTER(_p)]),
     "pf_layout_create_from_mask": (_i32, [_i32, _i32, _i32, _p, ctypes.POINTER(_p)]),
@@ -116,6 +122,20 @@ _SIGS = {
     "pf_attn_workspace_bytes": (_sz, [_i32, _i32, _i32]),
     "pf_attn_bwd_noalloc": (_i32, [_p, _i32, _i32, _i32, _i32, _f32, _p, _p, _p, _p, _p, _p, _p,
                                    _p, _p, _p]),
+    "pf_relpos_create": (_i32, [_i64, _i32, _p, ctypes.POINTER(_p)]),
+    "pf_relpos_create_log": (_i32, [_i64, _i32, _i64, _i32, ctypes.POINTER(_p)]),
+    "pf_relpos_buckets_get": (_i32, [_p, ctypes.POINTER(ctypes.POINTER(_i32)), ctypes.POINTER(_i64),
+                                     ctypes.POINTER(_i32)]),
+    "pf_relpos_upload": (_i32, [_p, _p]),
+    "pf_relpos_destroy": (None, [_p]),
+    "pf_relpos_bias_floats": (_sz, [_p]),
+    "pf_relpos_bias": (_i32, [_p, _i32, _p, _p, _p]),
+    "pf_attn_relpos_fwd": (_i32, [_p, _p, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _rows_p, _rows_p,
+                                  _rows_p, _p, _rows_p, _p, _p, _p, _p, _sz, _p]),
+    "pf_attn_relpos_bwd": (_i32, [_p, _p, _i32, _i32, _i32, _i32, _i32, _f32, _rows_p, _rows_p,
+                                  _rows_p, _p, _rows_p, _p, _rows_p, _rows_p, _rows_p, _rows_p, _p, _p,
+                                  _p, _sz, _p]),
+    "pf_attn_relpos_workspace_bytes": (_sz, [_p, _p, _i32, _i32, _i32]),
     "pf_dense_gemm": (_i32, [_i32, _i32, _i64, _i64, _i64, _p, _p, _p, _p, _sz, _p]),
     "pf_dense_workspace_bytes": (_sz, [_i32, _i32, _i64, _i64, _i64]),
     "pf_timing_begin": (_i32, [_i32]),
@@ -407,6 +427,110 @@ def pf_attn_bwd_noalloc(layout, B, H, S, d, scale, Q, K, V, O, lse, dO, dQ, dK, 
 
 def pf_attn_workspace_bytes(B, H, S) -> int:
     return int(_lib.pf_attn_workspace_bytes(B, H, S))
+
+
+class Relpos:
+    """Owner of a pf_relpos* (destroyed with the object)."""
+
+    def __init__(self, handle: int):
+        self.handle = handle
+
+    def __del__(self):
+        h, self.handle = getattr(self, "handle", None), None
+        if h and _lib is not None:
+            _lib.pf_relpos_destroy(h)
+
+
+def pf_relpos_create(seq: int, n_buckets: int, bucket) -> Relpos:
+    """bucket: 2 seq - 1 integers, the bucket of key - query = -(seq - 1) ..
+    seq - 1 (-1: not attended)."""
+    m = np.ascontiguousarray(bucket, dtype=np.int32)
+    if m.shape != (max(2 * seq - 1, 0),):
+        raise ValueError(f"bucket shape {m.shape} != ({2 * seq - 1},)")
+    h = _p()
+    _check(_lib.pf_relpos_create(seq, n_buckets, m.ctypes.data_as(_p), ctypes.byref(h)))
+    return Relpos(h.value)
+
+
+def pf_relpos_create_log(seq: int, n_buckets: int, max_distance: int, bidirectional: bool) -> Relpos:
+    h = _p()
+    _check(_lib.pf_relpos_create_log(seq, n_buckets, max_distance, int(bool(bidirectional)),
+                                     ctypes.byref(h)))
+    return Relpos(h.value)
+
+
+def pf_relpos_buckets_get(relpos: Relpos) -> tuple:
+    """(bucket map as pf_relpos_create takes it, n_buckets); a copy."""
+    b, seq, n = ctypes.POINTER(_i32)(), _i64(), _i32()
+    _check(_lib.pf_relpos_buckets_get(relpos.handle, ctypes.byref(b), ctypes.byref(seq), ctypes.byref(n)))
+    return np.ctypeslib.as_array(b, shape=(2 * seq.value - 1,)).copy(), n.value
+
+
+def pf_relpos_upload(relpos: Relpos, stream=None) -> None:
+    _check(_lib.pf_relpos_upload(relpos.handle, _stream(stream)))
+
+
+def pf_relpos_destroy(relpos: Relpos) -> None:
+    h, relpos.handle = relpos.handle, None
+    if h:
+        _lib.pf_relpos_destroy(h)
+
+
+def pf_relpos_bias_floats(relpos: Relpos) -> int:
+    return int(_lib.pf_relpos_bias_floats(relpos.handle))
+
+
+def pf_relpos_bias(relpos, H, table, bias, stream=None) -> None:
+    """table: H x n_buckets float32, bias: H x pf_relpos_bias_floats float32."""
+    _check(_lib.pf_relpos_bias(relpos.handle, H, _ptr(table), _ptr(bias), _stream(stream)))
+
+
+def _rows(t, name):
+    """pf_attn_tensor of a (sequences, heads, tokens, 64) bf16 view: any strides
+    but the last, which must be 1."""
+    if t.dim() != 4 or t.dtype != torch.bfloat16 or not t.is_cuda:
+        raise ValueError(f"{name}: expected a 4-d bfloat16 tensor on the GPU")
+    s = t.stride()
+    if s[3] != 1 and t.shape[3] != 1:
+        raise ValueError(f"{name}: the head dim must be contiguous")
+    return pf_attn_tensor(t.data_ptr(), s[0], s[1], max(s[2], 64) if t.shape[2] == 1 else s[2])
+
+
+def _like(t, ref, name):
+    if t.shape != ref.shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(ref.shape)}")
+    return _rows(t, name)
+
+
+def pf_attn_relpos_fwd(layout, relpos, scale, Q, K, V, bias, O, lse, q_start=None, kv_len=None,
+                       workspace=None, ws_bytes=0, stream=None) -> None:
+    """Q, O: (B, H, Sq, 64), K, V: (B, H_kv, Skv, 64) bf16 tensors of any
+    strides with a contiguous last dim; bias: of pf_relpos_bias; lse: (B, H, Sq)
+    float32, contiguous; q_start, kv_len: B int32 on the GPU, or None."""
+    B, H, Sq, d = Q.shape
+    q, k, v, o = _rows(Q, "Q"), _rows(K, "K"), _like(V, K, "V"), _like(O, Q, "O")
+    if K.shape[0] != B or K.shape[3] != d:
+        raise ValueError(f"K: shape {tuple(K.shape)} does not go with Q's {tuple(Q.shape)}")
+    _check(_lib.pf_attn_relpos_fwd(layout.handle, relpos.handle, B, H, K.shape[1], Sq, K.shape[2], d,
+                                   scale, q, k, v, _ptr(bias), o, _ptr(lse), _ptr(q_start),
+                                   _ptr(kv_len), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_attn_relpos_bwd(layout, relpos, scale, Q, K, V, bias, O, lse, dO, dQ, dK, dV, dtable,
+                       kv_len=None, workspace=None, ws_bytes=0, stream=None) -> None:
+    """As pf_attn_relpos_fwd with Sq = Skv; dtable: (H, n_buckets) float32."""
+    B, H, S, d = Q.shape
+    q, k, v, o = _rows(Q, "Q"), _rows(K, "K"), _like(V, K, "V"), _like(O, Q, "O")
+    g, dq, dk, dv = _like(dO, Q, "dO"), _like(dQ, Q, "dQ"), _like(dK, K, "dK"), _like(dV, K, "dV")
+    if K.shape[0] != B or K.shape[2] != S or K.shape[3] != d:
+        raise ValueError(f"K: shape {tuple(K.shape)} does not go with Q's {tuple(Q.shape)}")
+    _check(_lib.pf_attn_relpos_bwd(layout.handle, relpos.handle, B, H, K.shape[1], S, d, scale, q, k, v,
+                                   _ptr(bias), o, _ptr(lse), g, dq, dk, dv, _ptr(dtable),
+                                   _ptr(kv_len), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_attn_relpos_workspace_bytes(layout, relpos, B, H, Sq) -> int:
+    return int(_lib.pf_attn_relpos_workspace_bytes(layout.handle, relpos.handle, B, H, Sq))
 
 
 def pf_dense_gemm(dtype, op, M, N, K, A, B, C, workspace=None, ws_bytes=0, stream=None) -> None:

@@ -1,6 +1,7 @@
 """Argument checks of the operators round the layer's matrices (bias,
-activation and residual; their way back), on the host: every refused call
-enqueues nothing, so plain integers stand in for device addresses."""
+activation and residual; their way back; attention with a relative position
+bias), on the host: every refused call enqueues nothing, so plain integers stand in for device addresses."""
+import numpy as np
 import pytest
 
 from paper_2112_00029_amd import pixelfly as pf
@@ -68,3 +69,153 @@ def test_backward_workspace():
     _refused(pf.PF_ERR_WORKSPACE, "workspace needs", pf.pf_linear_act_bwd, **_bwd(ws_bytes=need - 1, **big))
     _refused(pf.PF_ERR_INVALID_ARG, "workspace is NULL", pf.pf_linear_act_bwd, **_bwd(workspace=None, **big))
     _refused(pf.PF_ERR_INVALID_ARG, "workspace is not", pf.pf_linear_act_bwd, **_bwd(workspace=A + 4, **big))
+
+
+# ---- attention with a relative position bias --------------------------------
+
+def test_log_map_thresholds():
+    """Against the definition in integers, exact powers among them."""
+    for n, reach, both in ((32, 128, True), (16, 128, False), (8, 64, True), (48, 512, True), (2, 5, False),
+                           (4, 9, True), (256, 4096, False), (7, 50, False)):
+        R = pf.pf_relpos_create_log(1024, n, reach, both)
+        got, nb = pf.pf_relpos_buckets_get(R)
+        assert nb == n and got.shape == (2047,)
+        half = n // 2 if both else n
+        e = half // 2
+        want = np.empty(2047, np.int32)
+        for i in range(2047):
+            d = abs(i - 1023)
+            c = d
+            if d >= e:
+                k = 0
+                while k + 1 < half - e and d ** (half - e) >= reach ** (k + 1) * e ** (half - e - k - 1):
+                    k += 1
+                c = e + k
+            c = min(c, half - 1)
+            want[i] = c if i <= 1023 else (half + c if both else -1)
+        assert np.array_equal(got, want), (n, reach, both)
+
+
+def test_plan_refusals():
+    ok = np.zeros(127, np.int32)
+    pf.pf_relpos_create(64, 1, ok)
+    for a in ((63, 1, np.zeros(125, np.int32)), (0, 1, np.zeros(0, np.int32)), (64, 0, ok), (64, 257, ok)):
+        with pytest.raises(pf.PixelflyError) as e:
+            pf.pf_relpos_create(*a)
+        assert e.value.status == pf.PF_ERR_INVALID_ARG
+    for bad in (1, -2):
+        m = ok.copy()
+        m[70] = bad
+        with pytest.raises(pf.PixelflyError) as e:
+            pf.pf_relpos_create(64, 1, m)
+        assert "distance 7" in str(e.value)
+    with pytest.raises(ValueError):
+        pf.pf_relpos_create(64, 1, ok[:-1])
+    for a in ((64, 3, 10, True), (64, 32, 8, True), (64, 1, 10, False), (64, 32, 1 << 40, True)):
+        with pytest.raises(pf.PixelflyError) as e:
+            pf.pf_relpos_create_log(*a)
+        assert e.value.status == pf.PF_ERR_INVALID_ARG
+
+
+class _Attn:
+    """Raw calls with stand-in addresses."""
+
+    def __init__(self):
+        self.L = pf.pf_layout_create_attention(256, 64, 2)
+        self.R = pf.pf_relpos_create_log(256, 32, 128, True)
+        self.keep = []
+
+    def rows(self, **kw):
+        d = dict(data=A, seq=4 * 256 * 64, head=256 * 64, token=64)
+        d.update(kw)
+        r = pf.pf_attn_tensor(d["data"], d["seq"], d["head"], d["token"])
+        self.keep.append(r)
+        return r
+
+    def fwd(self, **kw):
+        d = dict(L=self.L.handle, R=self.R.handle, B=2, H=4, Hkv=2, Sq=250, Skv=250, d=64, scale=0.125,
+                 Q=self.rows(), K=self.rows(), V=self.rows(), bias=A, O=self.rows(), lse=A, q_start=None,
+                 kv_len=None, ws=A, wsb=1 << 30, stream=None)
+        d.update(kw)
+        return pf._lib.pf_attn_relpos_fwd(*d.values())
+
+    def bwd(self, **kw):
+        d = dict(L=self.L.handle, R=self.R.handle, B=2, H=4, Hkv=2, S=250, d=64, scale=0.125)
+        for n in ("Q", "K", "V"):
+            d[n] = self.rows()
+        d["bias"] = A
+        d["O"] = self.rows()
+        d["lse"] = A
+        for n in ("dO", "dQ", "dK", "dV"):
+            d[n] = self.rows()
+        d.update(dtable=A, kv_len=None, ws=A, wsb=1 << 30, stream=None)
+        d.update(kw)
+        return pf._lib.pf_attn_relpos_bwd(*d.values())
+
+
+@pytest.fixture(scope="module")
+def attn():
+    return _Attn()
+
+
+SHARED = [(dict(B=0), -1, "B, H and H_kv"), (dict(Hkv=3), -1, "divide H"), (dict(H=0), -1, "B, H and H_kv"),
+          (dict(d=128), -2, "d = 64"), (dict(scale=0.0), -1, "scale"), (dict(scale=float("nan")), -1, "scale"),
+          (dict(scale=float("inf")), -1, "scale"), (dict(scale=-1.0), -1, "scale"), (dict(bias=None), -1, "bias is NULL"),
+          (dict(bias=A + 4), -1, "bias is not"), (dict(lse=None), -1, "lse is NULL"), (dict(kv_len=A + 2), -1, "kv_len"),
+          (dict(Q=None), -1, "Q is NULL"), (dict(L=None), -1, "layout is NULL"), (dict(R=None), -1, "plan is NULL")]
+ROWS = [(dict(data=None), -1, "is NULL"), (dict(data=A + 8), -1, "16-byte"), (dict(token=60), -1, "multiples of 8"),
+        (dict(token=56), -1, "below 64"), (dict(seq=-64), -1, "negative"), (dict(head=12), -1, "multiples of 8"),
+        (dict(token=1 << 25), -2, "2^31"), (dict(token=1 << 22), -2, "2^31")]
+
+
+@pytest.mark.parametrize("kw,status,text", SHARED)
+def test_attention_refusals(attn, kw, status, text):
+    for call in (attn.fwd, attn.bwd):
+        assert call(**kw) == status and text in pf.pf_last_error(), pf.pf_last_error()
+
+
+@pytest.mark.parametrize("kw,status,text", ROWS)
+def test_attention_tensor_refusals(attn, kw, status, text):
+    for call, names in ((attn.fwd, "Q K V O"), (attn.bwd, "Q K V O dO dQ dK dV")):
+        for n in names.split():
+            assert call(**{n: attn.rows(**kw)}) == status, n
+            assert text in pf.pf_last_error() and pf.pf_last_error().startswith(n), pf.pf_last_error()
+
+
+def test_attention_outputs_may_not_overlap(attn):
+    assert attn.fwd(K=attn.rows(seq=0), V=attn.rows(head=0)) == pf.PF_ERR_STATE
+    for n in ("seq", "head"):
+        assert attn.fwd(O=attn.rows(**{n: 0})) == -1 and "overlap" in pf.pf_last_error()
+        for g in ("dQ", "dK", "dV"):
+            assert attn.bwd(**{g: attn.rows(**{n: 0})}) == -1 and "overlap" in pf.pf_last_error()
+
+
+def test_attention_sizes_layouts_workspace(attn):
+    for kw in (dict(Sq=0), dict(Sq=257), dict(Skv=0), dict(Skv=300)):
+        assert attn.fwd(**kw) == -1 and "Sq and Skv" in pf.pf_last_error()
+    assert attn.fwd(q_start=A + 1) == -1
+    other = pf.pf_layout_create_attention(512, 64, 2)
+    assert attn.fwd(L=other.handle) == -1 and "square" in pf.pf_last_error()
+    rect = pf.pf_layout_create(256, 512, 64, 2)
+    assert attn.bwd(L=rect.handle) == -1
+    b32 = pf.pf_layout_create(256, 256, 32, 2)
+    assert attn.fwd(L=b32.handle) == -2
+    assert attn.fwd() == pf.PF_ERR_STATE and attn.bwd() == pf.PF_ERR_STATE
+    need = pf.pf_attn_relpos_workspace_bytes(attn.L, attn.R, 2, 4, 250)
+    assert need >= 2 * 4 * 250 * 4 and attn.bwd(wsb=need - 1) == pf.PF_ERR_WORKSPACE
+    assert attn.bwd(ws=None) == -1 and attn.bwd(dtable=None) == -1
+    assert pf.pf_attn_relpos_workspace_bytes(attn.L, attn.R, 0, 4, 250) == 0
+    with pytest.raises(pf.PixelflyError):
+        pf.pf_relpos_bias(attn.R, 0, A, A, stream=0)
+    with pytest.raises(pf.PixelflyError) as e:
+        pf.pf_relpos_bias(attn.R, 4, A, A, stream=0)
+    assert e.value.status == pf.PF_ERR_STATE
+
+
+def test_binding_refuses_host_and_odd_tensors(attn):
+    import torch
+    x = torch.zeros((1, 2, 8, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="on the GPU"):
+        pf.pf_attn_relpos_fwd(attn.L, attn.R, 0.125, x, x, x, A, x, A)
+    with pytest.raises(ValueError, match="bfloat16"):
+        pf.pf_attn_relpos_fwd(attn.L, attn.R, 0.125, x.float(), x, x, A, x, A)
