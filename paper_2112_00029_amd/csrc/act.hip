@@ -94,21 +94,21 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
   }
 }
 
-// dbias[c] = sum over the parts, in a fixed order: a workgroup takes 64
-// columns, four threads a column a quarter of the parts each.
+// dbias[c] = sum over the parts, in a fixed order: a workgroup takes 16 columns,
+// 16 threads a column every 16th part each.
 template <typename T>
 __global__ __launch_bounds__(256) void act_dbias_kernel(const float *P, int nparts, int64_t N, T *dbias) {
   __shared__ float red[256];
-  const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-  const int q = threadIdx.x >> 6, per = (nparts + 3) / 4;
+  const int64_t col = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
+  const int q = threadIdx.x >> 4;
   float s = 0.f;
-  if (col < N)
-    for (int p = q * per; p < min(nparts, (q + 1) * per); ++p) s += P[(int64_t)p * N + col];
+#pragma unroll 4
+  for (int p = q; p < nparts; p += 16) s += P[(int64_t)p * N + col];
   red[threadIdx.x] = s;
   __syncthreads();
-  if (q == 0 && col < N)
-    put1(dbias + col, red[threadIdx.x] + red[threadIdx.x + 64] + red[threadIdx.x + 128] +
-                          red[threadIdx.x + 192]);
+  if (q) return;
+  for (int p = 1; p < 16; ++p) s += red[p * 16 + threadIdx.x];
+  put1(dbias + col, s);
 }
 
 }  // namespace
@@ -122,7 +122,7 @@ hipError_t launch_act_bwd(int dtype, const ActBwdArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_act_dbias(int dtype, const ActBwdArgs &a, hipStream_t s) {
-  const int64_t grid = (a.N + 63) / 64;
+  const int64_t grid = a.N / 16;  // N is a multiple of 32
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   if (dtype == 0)
     launch_kernel(act_dbias_kernel<bf16_t>, dim3((unsigned)grid), dim3(256), s,

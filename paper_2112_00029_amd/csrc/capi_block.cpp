@@ -175,8 +175,6 @@ pf::RelposArgs relpos_args(const pf_layout *L, const pf_relpos *R, const RelposD
   a.col_ptr = L->d_col_ptr; a.row_idx = L->d_row_idx;
   a.B = m.B; a.H = m.H; a.Hkv = m.H_kv; a.G = m.H / m.H_kv;
   a.Sq = m.Sq; a.Skv = m.Skv; a.seq = (int)R->seq; a.nb = R->nb;
-  // A chunk starts anywhere in a block.
-  a.ntile = (m.Sq + (q_start ? 63 : 0) + 63) / 64;
   a.nbucket = R->n_buckets;
   a.omin = R->omin; a.omax = R->omax;
   a.scale = m.scale;
@@ -184,6 +182,111 @@ pf::RelposArgs relpos_args(const pf_layout *L, const pf_relpos *R, const RelposD
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+// How a launch over blocks shares them among workgroups: the first nlong of a
+// head's ntile in plong parts, the others in pshort (see pf::RelposArgs).
+struct Parts {
+  int nbh = 0, ntile = 0, nlong = 0, plong = 1, pshort = 1;
+  int64_t slots() const {
+    return (int64_t)nbh * ((plong > 1 ? (int64_t)nlong * plong : 0) +
+                           (pshort > 1 ? (int64_t)(ntile - nlong) * pshort : 0));
+  }
+  int64_t workgroups() const {
+    return (int64_t)nbh * ((int64_t)nlong * plong + (int64_t)(ntile - nlong) * pshort);
+  }
+  void set(pf::RelposArgs &a) const {
+    a.nbh = nbh; a.ntile = ntile; a.nlong = nlong; a.plong = plong; a.pshort = pshort;
+  }
+};
+
+// Blocks (items of a list) per part, where a list is shared at all.
+constexpr int kLongItems = 16;
+// Fewest items of a part of the other blocks, and the workgroups they are split
+// up to.
+constexpr int kShortItems = 4;
+constexpr int64_t kShortWG = 512;
+
+// long_items: list length of the nlong leading blocks, items: of the others.
+Parts choose_parts(int nbh, int ntile, int nlong, int64_t long_items, int64_t items) {
+  Parts p;
+  p.nbh = nbh;
+  p.ntile = ntile;
+  if (nlong > 0 && long_items > kLongItems) {
+    p.nlong = std::min(nlong, ntile);
+    p.plong = (int)((long_items + kLongItems - 1) / kLongItems);
+  }
+  const int64_t wg = (int64_t)nbh * (ntile - p.nlong);
+  if (wg > 0 && wg < kShortWG && items > kLongItems)
+    p.pshort = (int)std::min((kShortWG + wg - 1) / wg, (items + kShortItems - 1) / kShortItems);
+  return p;
+}
+
+// Longest lists of a layout's block rows (or columns) as far as the plan's
+// distances reach: of the leading stripes, and of the rest.
+struct Lists {
+  int nlong;
+  int64_t long_items, items;
+};
+Lists row_lists(const pf_layout *L, const pf_relpos *R, bool columns) {
+  const int64_t nb = L->nb_out, g = std::min<int64_t>(L->global_blocks, nb);
+  // Key block - query block lies in omin .. omax; seen from a column the other
+  // way round.
+  const int64_t lo = columns ? -R->omax : R->omin, hi = columns ? -R->omin : R->omax;
+  auto reach = [&](int64_t last) {  // blocks within lo .. hi of block `last`
+    return std::max<int64_t>(0, std::min(nb - 1, last + hi) - std::max<int64_t>(0, last + lo) + 1);
+  };
+  Lists r{(int)g, g > 0 ? reach(g - 1) : 0, 0};
+  const int64_t most = columns ? L->kmax_bwd : L->kmax_fwd;
+  // With stripes the longest list is theirs: the others' average.
+  r.items = g > 0 && g < nb ? (L->nnzb - g * nb + (nb - g) - 1) / (nb - g) : most;
+  r.items = std::min(r.items, std::max<int64_t>(0, hi - lo + 1));
+  return r;
+}
+
+Parts fwd_parts(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t Sq, bool chunk) {
+  const Lists l = row_lists(L, R, false);
+  // A chunk starts anywhere in a block, and anywhere in its sequence: which of
+  // its tiles are a stripe's is not known here.
+  return choose_parts(B * H, (Sq + (chunk ? 63 : 0) + 63) / 64, chunk ? 0 : l.nlong, l.long_items, l.items);
+}
+Parts dkv_parts(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t Hkv, int32_t S) {
+  const Lists l = row_lists(L, R, true);
+  const int G = H / Hkv;
+  return choose_parts(B * Hkv, (S + 63) / 64, l.nlong, l.long_items * G, l.items * G);
+}
+// Waves per (sequence, key/value head) of the decode kernel.
+Parts decode_parts(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t Hkv) {
+  const Lists l = row_lists(L, R, false);
+  Parts p;
+  p.nbh = B * Hkv;
+  p.ntile = 1;
+  const int64_t want = (2048 + p.nbh - 1) / p.nbh, most = (l.items + 1) / 2;
+  p.pshort = (int)std::max<int64_t>(1, l.items >= 8 ? std::min(want, most) : 1);
+  return p;
+}
+bool use_decode(int32_t Sq, int32_t H, int32_t Hkv) { return Sq == 1 && H / Hkv <= pf::kRelposDecodeRows; }
+
+size_t fwd_slots(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t Hkv, int32_t Sq, bool chunk) {
+  if (use_decode(Sq, H, Hkv))
+    return decode_parts(L, R, B, Hkv).slots() * pf::kRelposDecodeSlot * sizeof(float);
+  return fwd_parts(L, R, B, H, Sq, chunk).slots() * pf::kRelposFwdSlot * sizeof(float);
+}
+// Backward workspace: delta, the bucket sums, slots (first dQ's, then dK and
+// dV's).
+struct BwdPlan {
+  Parts dq, dkv;
+  size_t partials, slots, total;
+};
+BwdPlan bwd_plan(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t Hkv, int32_t S) {
+  BwdPlan p;
+  p.dq = fwd_parts(L, R, B, H, S, false);
+  p.dkv = dkv_parts(L, R, B, H, Hkv, S);
+  p.partials = up256((size_t)B * H * S * sizeof(float));
+  p.slots = p.partials + up256((size_t)p.dq.workgroups() * R->n_buckets * sizeof(float));
+  p.total = p.slots + std::max((size_t)p.dq.slots() * pf::kRelposAccFloats,
+                               (size_t)p.dkv.slots() * 2 * pf::kRelposAccFloats) * sizeof(float);
+  return p;
+}
 
 }  // namespace
 
@@ -286,9 +389,16 @@ pf_status pf_relpos_bias(const pf_relpos *R, int32_t H, const float *table, floa
 }
 
 size_t pf_attn_relpos_workspace_bytes(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t Sq) {
-  if (!L || !R || B < 1 || H < 1 || Sq < 1) return 0;
-  const size_t rows = (size_t)B * H;
-  return up256(rows * Sq * sizeof(float)) + up256(rows * ((Sq + 63) / 64) * R->n_buckets * sizeof(float));
+  if (!L || !R || B < 1 || H < 1 || Sq < 1 || Sq > R->seq || L->n_out != R->seq || L->n_in != R->seq ||
+      (int64_t)B * H > 0x7fffffff / (R->nb + 1))
+    return 0;
+  // For every number of key/value heads, and either form of the forward.
+  size_t need = 0;
+  for (int32_t k = 1; k <= H; ++k)
+    if (H % k == 0)
+      need = std::max({need, fwd_slots(L, R, B, H, k, Sq, false), fwd_slots(L, R, B, H, k, Sq, true),
+                       bwd_plan(L, R, B, H, k, Sq).total});
+  return up256(need);
 }
 
 pf_status pf_attn_relpos_fwd(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t H_kv,
@@ -303,15 +413,25 @@ pf_status pf_attn_relpos_fwd(const pf_layout *L, const pf_relpos *R, int32_t B, 
       (st = check_rows(V, "V", Skv, false, B, H_kv)) != PF_OK || (st = check_rows(O, "O", Sq, true, B, H)) != PF_OK ||
       (st = need_ptr(lse, "lse")) != PF_OK)
     return st;
-  (void)workspace;
-  (void)ws_bytes;
+  const size_t need = fwd_slots(L, R, B, H, H_kv, Sq, q_start != nullptr);
+  if ((st = need_ws(need, workspace, ws_bytes)) != PF_OK) return st;
   if ((st = check_state(L)) != PF_OK || (st = relpos_state(R)) != PF_OK) return st;
   pf::RelposArgs a = relpos_args(L, R, m, bias, q_start, kv_len);
   a.Q = view(Q); a.K = view(K); a.V = view(V); a.Oout = view_out(O);
   a.lse = lse;
+  a.slots = (float *)workspace;
   hipStream_t s = (hipStream_t)stream;
-  Timed t(PF_KERNEL_ATTN_FWD, s);
-  return hip_status(pf::launch_relpos_fwd(a, s), "attention forward kernel");
+  const bool dec = use_decode(Sq, H, H_kv);
+  (dec ? decode_parts(L, R, B, H_kv) : fwd_parts(L, R, B, H, Sq, q_start != nullptr)).set(a);
+  {
+    Timed t(PF_KERNEL_ATTN_FWD, s);
+    st = hip_status(dec ? pf::launch_relpos_decode(a, s) : pf::launch_relpos_fwd(a, s),
+                    "attention forward kernel");
+  }
+  if (st != PF_OK || !need) return st;
+  Timed t(PF_KERNEL_REDUCE, s);
+  return hip_status(dec ? pf::launch_relpos_decode_join(a, s) : pf::launch_relpos_fwd_join(a, s),
+                    "attention forward join");
 }
 
 pf_status pf_attn_relpos_bwd(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t H_kv,
@@ -331,25 +451,32 @@ pf_status pf_attn_relpos_bwd(const pf_layout *L, const pf_relpos *R, int32_t B, 
       (st = check_rows(dV, "dV", S, true, B, H_kv)) != PF_OK || (st = need_ptr(lse, "lse")) != PF_OK ||
       (st = need_ptr(dtable, "dtable")) != PF_OK)
     return st;
-  if ((st = need_ws(pf_attn_relpos_workspace_bytes(L, R, B, H, S), workspace, ws_bytes)) != PF_OK) return st;
+  const BwdPlan p = bwd_plan(L, R, B, H, H_kv, S);
+  if ((st = need_ws(p.total, workspace, ws_bytes)) != PF_OK) return st;
   if ((st = check_state(L)) != PF_OK || (st = relpos_state(R)) != PF_OK) return st;
   pf::RelposArgs a = relpos_args(L, R, m, bias, nullptr, kv_len);
   a.Q = view(Q); a.K = view(K); a.V = view(V); a.O = view(O); a.dO = view(dO);
   a.dQ = view_out(dQ); a.dK = view_out(dK); a.dV = view_out(dV);
   a.lse_in = lse;
   a.delta = (float *)workspace;
-  a.partials = (float *)((char *)workspace + up256((size_t)B * H * S * sizeof(float)));
+  a.partials = (float *)((char *)workspace + p.partials);
+  a.slots = (float *)((char *)workspace + p.slots);
   hipStream_t s = (hipStream_t)stream;
-  {
-    Timed t(PF_KERNEL_ATTN_BWD_DQ, s);
-    if ((st = hip_status(pf::launch_relpos_bwd_dq(a, s), "attention dQ kernel")) != PF_OK) return st;
-  }
-  {
-    Timed t(PF_KERNEL_ATTN_BWD_DKV, s);
-    if ((st = hip_status(pf::launch_relpos_bwd_dkv(a, s), "attention dK/dV kernel")) != PF_OK) return st;
-  }
-  Timed t(PF_KERNEL_REDUCE, s);
-  return hip_status(pf::launch_relpos_dtable(a, dtable, s), "table gradient sum");
+  auto run = [&](pf_kernel_class k, const char *what, auto &&launch) {
+    if (st != PF_OK) return;
+    Timed t(k, s);
+    st = hip_status(launch(), what);
+  };
+  p.dq.set(a);
+  run(PF_KERNEL_ATTN_BWD_DQ, "attention dQ kernel", [&] { return pf::launch_relpos_bwd_dq(a, s); });
+  run(PF_KERNEL_REDUCE, "table gradient sum", [&] { return pf::launch_relpos_dtable(a, dtable, s); });
+  if (p.dq.slots())
+    run(PF_KERNEL_REDUCE, "dQ join", [&] { return pf::launch_relpos_bwd_join(false, a, s); });
+  p.dkv.set(a);
+  run(PF_KERNEL_ATTN_BWD_DKV, "attention dK/dV kernel", [&] { return pf::launch_relpos_bwd_dkv(a, s); });
+  if (p.dkv.slots())
+    run(PF_KERNEL_REDUCE, "dK/dV join", [&] { return pf::launch_relpos_bwd_join(true, a, s); });
+  return st;
 }
 
 }  // extern "C"

@@ -344,14 +344,17 @@ struct RelposArgs {
   float *lse;            // [B][H][Sq]
   const float *lse_in;
   float *delta;          // [B][H][Sq]
-  float *partials;       // [B][H][ntile][nbucket]
+  float *partials;       // a row of nbucket sums per workgroup of the dQ launch
+  float *slots;          // partial results of blocks in several parts
   const int32_t *q_start, *kv_len;  // [B] or null
   const int32_t *info;
   const uint32_t *order;
   const int32_t *row_ptr, *col_idx, *col_ptr, *row_idx;
   int B, H, Hkv, G;      // G = H / Hkv
   int Sq, Skv, seq, nb;  // seq: side of the layout, nb = seq / 64
+  int nbh;               // sequences x heads of the launch
   int ntile;             // 64-row tiles per sequence and head of the launch
+  int nlong, plong, pshort;  // the first nlong of them in plong parts, the others in pshort
   int nbucket;
   int omin, omax;        // block offsets (key - query) that hold an attended distance
   float scale;
@@ -363,9 +366,19 @@ struct RelposBiasArgs {
   int seq, nbucket;
 };
 hipError_t launch_relpos_bias(const RelposBiasArgs &a, int H, hipStream_t s);
+// Each of the launches over blocks, and (when some are in several parts) the
+// one that joins them; floats per slot of a part.
+constexpr int kRelposAccFloats = 2 * 64 * 32, kRelposFwdSlot = kRelposAccFloats + 2 * 128;
 hipError_t launch_relpos_fwd(const RelposArgs &a, hipStream_t s);
+// One query row per sequence: nbh = B Hkv heads in pshort parts each, a wave per
+// part; up to kRelposDecodeRows query heads per key/value head.
+constexpr int kRelposDecodeRows = 32, kRelposDecodeSlot = 64 * 32 + 128;
+hipError_t launch_relpos_decode(const RelposArgs &a, hipStream_t s);
+hipError_t launch_relpos_decode_join(const RelposArgs &a, hipStream_t s);
+hipError_t launch_relpos_fwd_join(const RelposArgs &a, hipStream_t s);
 hipError_t launch_relpos_bwd_dq(const RelposArgs &a, hipStream_t s);
 hipError_t launch_relpos_bwd_dkv(const RelposArgs &a, hipStream_t s);
+hipError_t launch_relpos_bwd_join(bool kv, const RelposArgs &a, hipStream_t s);
 hipError_t launch_relpos_dtable(const RelposArgs &a, float *dtable, hipStream_t s);
 
 // The allocation-free attention backward keeps its row terms in a

@@ -131,6 +131,56 @@ __device__ __forceinline__ void seg_scan(float &sum, int id) {
   seg_step<kRowBcast31, 0xc>(sum, id);
 }
 
+// What a workgroup of a launch over row blocks (a.nbh heads) works on: a part
+// of block blk's list.  Blocks below nlong, the long rows or columns of a mask
+// with global stripes, go first in plong parts, the others in pshort.  A block in
+// several parts leaves fp32 partial results in slot `slot`, which a second launch
+// joins in part order; -1: the block is this workgroup's alone.
+struct Work {
+  int bh, blk, part, parts, slot;
+};
+__device__ __forceinline__ Work find_work(const RelposArgs &a, int L) {
+  Work k;
+  const int lt = a.nbh * a.nlong * a.plong, m = a.ntile - a.nlong;
+  if (L < lt) {
+    const int u = L / a.plong;
+    k = Work{u / a.nlong, u % a.nlong, L - u * a.plong, a.plong, a.plong > 1 ? L : -1};
+  } else {
+    const int r = L - lt, u = r / a.pshort;
+    k = Work{u / m, a.nlong + u % m, r - u * a.pshort, a.pshort,
+             a.pshort > 1 ? r + (a.plong > 1 ? lt : 0) : -1};
+  }
+  return k;
+}
+// The block that workgroup J of a join works on, and its first slot.
+__device__ __forceinline__ Work find_join(const RelposArgs &a, int J) {
+  const int lt = a.nbh * a.nlong * a.plong, nl = a.plong > 1 ? a.nbh * a.nlong : 0;
+  if (J < nl) return Work{J / a.nlong, J % a.nlong, 0, a.plong, J * a.plong};
+  const int u = J - nl, m = a.ntile - a.nlong;
+  return Work{u / m, a.nlong + u % m, 0, a.pshort, u * a.pshort + (a.plong > 1 ? lt : 0)};
+}
+
+// Slot layouts: an accumulator pair of the two waves register-major (16 bytes
+// a lane, a KiB per store), then for the forward the running maximum and sum.
+constexpr int kAccFloats = kRelposAccFloats, kFwdSlot = kRelposFwdSlot;
+__device__ __forceinline__ void put_acc(float *slot, const f32x16 (&o)[2], int w, int lane) {
+  float *q = slot + (w * 64 + lane) * 4;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int dt = i >> 2, e = (i & 3) * 4;
+    *(f32x4 *)(q + i * 512) = f32x4{o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]};
+  }
+}
+__device__ __forceinline__ void add_acc(const float *slot, f32x16 (&o)[2], float scale, int w, int lane) {
+  const float *q = slot + (w * 64 + lane) * 4;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const f32x4 v = *(const f32x4 *)(q + i * 512);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[i >> 2][(i & 3) * 4 + j] += v[j] * scale;
+  }
+}
+
 // First and one past the last position of a row's block list whose column
 // lies in [lo, hi] (columns ascend).
 __device__ __forceinline__ void trim(const int32_t *col, int &p0, int &p1, int lo, int hi) {
@@ -154,9 +204,25 @@ __device__ __forceinline__ void trim(const int32_t *col, int &p0, int &p1, int l
   }
 }
 
+// Part wk.part of the positions [p0, p1).
+__device__ __forceinline__ void take_part(const Work &wk, int &p0, int &p1) {
+  if (wk.parts == 1) return;
+  const int per = (p1 - p0 + wk.parts - 1) / wk.parts;
+  p0 = min(p1, p0 + wk.part * per);
+  p1 = min(p1, p0 + per);
+}
+
 // Tokens of sequence b.
 __device__ __forceinline__ int seq_len(const RelposArgs &a, int b) {
   return a.kv_len ? min(max(ld_meta(a.kv_len + b), 0), a.Skv) : a.Skv;
+}
+
+// The kernel's arguments read again here: those needed after the loop need not
+// occupy scalar registers in it.
+__device__ __forceinline__ const RelposArgs &late_args() {
+  auto *p = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const RelposArgs *)p;
 }
 
 // Bias of a block: what the plan says about its distances (info, see
@@ -170,18 +236,29 @@ struct BlockBias {
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
+// O and lse of row `row` of a sequence's Sq, the first nrow of which hold
+// tokens; l: this lane's keys only.
+__device__ __forceinline__ void fwd_store(const RelposArgs &a, int bh, int row, int nrow,
+                                          const f32x16 (&o)[2], float m, float l, int lane) {
+  l = add_xor32(l);
+  const bool store = row >= 0 && row < a.Sq, live = row < nrow;
+  bf16_t *O = (bf16_t *)a.Oout.p + bh / a.H * a.Oout.seq + bh % a.H * a.Oout.head + (int64_t)row * a.Oout.tok;
+  put_row(O, o, l == 0.f ? 0.f : 1.f / l, live, store, lane);
+  if (lane < 32 && store)
+    a.lse[(int64_t)bh * a.Sq + row] = live ? (m + __log2f(l)) * kLn2 : -INFINITY;
+}
+
 __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   uint8_t *const ks = stage_buf<0, TILE>(), *const vs = stage_buf<1, TILE>();
   uint8_t *const w0 = stage_buf<2, WIN>(), *const w1 = stage_buf<3, WIN>();
 
-  const int bid = xcd_remap(blockIdx.x, gridDim.x);
-  const int bh = bid / a.ntile, tile = bid % a.ntile;
-  const int b = bh / a.H, h = bh % a.H, hk = h / a.G;
+  const Work wk = find_work(a, xcd_remap(blockIdx.x, gridDim.x));
+  const int bh = wk.bh, b = bh / a.H, h = bh % a.H, hk = h / a.G;
   const int len = seq_len(a, b);
   const int start = a.q_start ? min(max(ld_meta(a.q_start + b), 0), a.seq) : 0;
-  const int qb = (start >> 6) + tile;
+  const int qb = (start >> 6) + wk.blk;
   // Row index of this lane's query, and the rows that hold tokens.
   const int row = qb * BQ + w * 32 + (lane & 31) - start;
   const int nrow = min(max(len - start, 0), a.Sq);
@@ -201,6 +278,7 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
     p0 = ld_meta(a.row_ptr + qb);
     p1 = ld_meta(a.row_ptr + qb + 1);
     trim(a.col_idx, p0, p1, qb + a.omin, min(qb + a.omax, (len + BQ - 1) / BQ - 1));
+    take_part(wk, p0, p1);
   }
   f32x16 o[2];
 #pragma unroll
@@ -261,12 +339,12 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
             for (int j = 0; j < 4; ++j) s[kt][e4 * 4 + j] = __builtin_fmaf(s[kt][e4 * 4 + j], c, bv[j]);
           }
         if (tail < BQ) {
-          const int k0 = (lane >> 5) * 4;
+          const int lim = tail - (lane >> 5) * 4;
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (k0 + kt * 32 + (e >> 2) * 8 + (e & 3) >= tail) s[kt][e] = -INFINITY;
+              if (kt * 32 + (e >> 2) * 8 + (e & 3) >= lim) s[kt][e] = -INFINITY;
         }
         cm = 1.f;
         ca = 0.f;
@@ -323,12 +401,220 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
     wait_vm<0>();  // no copy outlives the workgroup
   }
 
+  const RelposArgs &z = late_args();
+  if (wk.slot >= 0) {
+    float *slot = z.slots + (int64_t)wk.slot * kFwdSlot;
+    put_acc(slot, o, w, lane);
+    slot[kAccFloats + w * 128 + lane] = m_run;
+    slot[kAccFloats + w * 128 + 64 + lane] = l_run;
+    return;
+  }
+  fwd_store(z, bh, row, nrow, o, m_run, l_run, lane);
+}
+
+// Join of the forward's parts: each relative to the largest running maximum.
+__global__ __launch_bounds__(128) void relpos_fwd_join_kernel(RelposArgs a) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const Work wk = find_join(a, blockIdx.x);
+  const int b = wk.bh / a.H;
+  const int start = a.q_start ? min(max(ld_meta(a.q_start + b), 0), a.seq) : 0;
+  const int row = ((start >> 6) + wk.blk) * BQ + w * 32 + (lane & 31) - start;
+  if (((start >> 6) + wk.blk) * BQ - start >= a.Sq) return;  // no part has written
+  const float *slot = a.slots + (int64_t)wk.slot * kFwdSlot;
+  const float *ml = slot + kAccFloats + w * 128 + lane;
+  float m = kFloor, l = 0.f;
+  for (int p = 0; p < wk.parts; ++p) m = fmaxf(m, ml[(int64_t)p * kFwdSlot]);
+  f32x16 o[2];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
+  for (int p = 0; p < wk.parts; ++p) {
+    const float s = fast_exp2(ml[(int64_t)p * kFwdSlot] - m);
+    l += ml[(int64_t)p * kFwdSlot + 64] * s;
+    add_acc(slot + (int64_t)p * kFwdSlot, o, s, w, lane);
+  }
+  fwd_store(a, wk.bh, row, min(max(seq_len(a, b) - start, 0), a.Sq), o, m, l, lane);
+}
+
+// ---------------------------------------------------------------------------
+// Forward of one query row per sequence (decoding one token)
+// ---------------------------------------------------------------------------
+// The G query heads of a key/value head are the rows of one tile (G <= 32), so
+// keys and values are read once.  A wave works alone, without barriers, on part of
+// a (sequence, key/value head)'s block list, with tiles of its own; four of them
+// share a workgroup.  The rows differ in head and agree in position: each lane
+// reads its head's bias of its keys from memory (256 bytes a head and block).
+__global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  uint8_t *const ks = stage_buf<0, 4 * TILE>() + w * TILE, *const vs = stage_buf<1, 4 * TILE>() + w * TILE;
+  const int u = xcd_remap(blockIdx.x, gridDim.x) * 4 + w;
+  if (u >= a.nbh * a.pshort) return;
+  const int bhk = u / a.pshort, part = u - bhk * a.pshort;
+  const int b = bhk / a.Hkv, hk = bhk % a.Hkv;
+  const int len = seq_len(a, b);
+  const int pos = a.q_start ? min(max(ld_meta(a.q_start + b), 0), a.seq) : 0, qb = pos >> 6;
+  const int r = lane & 31, h = hk * a.G + r;
+  const bool live = pos < len, mine = r < a.G;
+
+  const bf16_t *K = (const bf16_t *)a.K.p + b * a.K.seq + hk * a.K.head;
+  const bf16_t *V = (const bf16_t *)a.V.p + b * a.V.seq + hk * a.V.head;
+  const uint32_t krb = (uint32_t)(a.K.tok * 2), vrb = (uint32_t)(a.V.tok * 2);
+  const rsrc_t rk = rows_rsrc(K, len, krb), rv = rows_rsrc(V, len, vrb);
+  const float c = a.scale * kLog2e;
+  int p0 = 0, p1 = 0;
+  if (live && qb < a.nb) {
+    p0 = ld_meta(a.row_ptr + qb);
+    p1 = ld_meta(a.row_ptr + qb + 1);
+    trim(a.col_idx, p0, p1, qb + a.omin, min(qb + a.omax, (len + BQ - 1) / BQ - 1));
+    take_part(Work{0, 0, part, a.pshort, 0}, p0, p1);
+  }
+  f32x16 o[2];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
+  float m_run = kFloor, l_run = 0.f;
+  if (p0 < p1) {
+    RowCopy kc, vc;
+    kc.init(lane, 0, krb);
+    vc.init(lane, 0, vrb);
+    auto copy = [&](const RowCopy &rc, rsrc_t rs, uint32_t off, uint8_t *tile) __attribute__((always_inline)) {
+      sfor<8>([&](auto i) __attribute__((always_inline)) {
+        dma16(rs, tile + i * 1024, rc.voff[i & 1] + off + i * rc.step, 0);
+      });
+    };
+    // Bias of this lane's head (rows past G read 0), from key 0's distance on.
+    const rsrc_t rb = make_rsrc(a.bias + (int64_t)hk * a.G * a.bias_ld, (int64_t)a.G * a.bias_ld * 4);
+    const uint32_t boff = (uint32_t)r * (uint32_t)(a.bias_ld * 4) + (uint32_t)(a.seq - pos + (lane >> 5) * 4) * 4u;
+    int col = ld_meta(a.col_idx + p0);
+    copy(kc, rk, (uint32_t)(col * BQ) * krb, ks);
+    bf16x8 qf[4];
+    const bf16_t *Q = (const bf16_t *)a.Q.p + b * a.Q.seq + h * a.Q.head;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (mine) v = *(const u32x4 *)(Q + i * 16 + (lane >> 5) * 8);
+      qf[i] = __builtin_bit_cast(bf16x8, v);
+    }
+    u32x4 bv[8];
+    auto load_bias = [&](int cb) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        bv[i] = __builtin_amdgcn_raw_buffer_load_b128(
+            rb, mine ? (int)(boff + (uint32_t)(cb * BQ + i * 8) * 4u) : 0x7ffffff0, 0, 0);
+    };
+    load_bias(col);
+    copy(vc, rv, (uint32_t)(col * BQ) * vrb, vs);
+    for (int p = p0; p < p1; ++p) {
+      const int cn = ld_meta(a.col_idx + min(p + 1, p1 - 1));
+      // The waits count the copies alone: eight newer ones, whatever the
+      // order of the loads to registers among them.
+      wait_vm<8>();  // K has landed; V may be in flight
+      f32x16 s[2];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[kt][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[kt] = MFMA32(frag_r(ks, kt * 32, i, lane), qf[i], s[kt]);
+      }
+      wait_vm<63>();  // (K's reads have returned)
+      copy(kc, rk, (uint32_t)(cn * BQ) * krb, ks);
+      const int lim = len - col * BQ - (lane >> 5) * 4;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const uint32_t bits = bv[kt * 4 + (e >> 2)][e & 3];
+          s[kt][e] = __builtin_fmaf(s[kt][e], c, __uint_as_float(bits));
+          if (kt * 32 + (e >> 2) * 8 + (e & 3) >= lim) s[kt][e] = -INFINITY;
+        }
+      float bmax = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) bmax = fmaxf(bmax, s[kt][e]);
+      if (__builtin_amdgcn_ballot_w64(bmax > m_run + 8.0f)) {
+        const float m_cand = fmaxf(m_run, max_xor32(bmax));
+        const float alpha = fast_exp2(m_run - m_cand);
+        m_run = m_cand;
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+      }
+      float rs = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = fast_exp2(s[kt][e] - m_run);
+          s[kt][e] = x;
+          rs += x;
+        }
+      l_run += rs;
+      wait_vm<8>();  // V has landed; the next K stays in flight
+      load_bias(cn);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const bf16x8 pb = pack_k(s[kt], j);
+#pragma unroll
+          for (int dt = 0; dt < 2; ++dt)
+            o[dt] = MFMA32(frag_t(vs, kt * 32 + j * 16, dt * 32, lane), pb, o[dt]);
+        }
+      wait_vm<63>();  // (V's reads have returned)
+      copy(vc, rv, (uint32_t)(cn * BQ) * vrb, vs);
+      col = cn;
+    }
+    wait_vm<0>();  // no copy outlives the wave
+  }
+  if (a.pshort > 1) {
+    if (!mine) return;
+    float *slot = a.slots + (int64_t)u * kRelposDecodeSlot;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int dt = i >> 2, e = (i & 3) * 4;
+      *(f32x4 *)(slot + i * 256 + lane * 4) = f32x4{o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]};
+    }
+    slot[2048 + lane] = m_run;
+    slot[2112 + lane] = l_run;
+    return;
+  }
   l_run = add_xor32(l_run);
-  const bool store = row >= 0 && row < a.Sq, live = row < nrow;
-  bf16_t *O = (bf16_t *)a.Oout.p + b * a.Oout.seq + h * a.Oout.head + (int64_t)row * a.Oout.tok;
-  put_row(O, o, l_run == 0.f ? 0.f : 1.f / l_run, live, store, lane);
-  if (lane < 32 && store)
-    a.lse[(int64_t)bh * a.Sq + row] = live ? (m_run + __log2f(l_run)) * kLn2 : -INFINITY;
+  put_row((bf16_t *)a.Oout.p + b * a.Oout.seq + h * a.Oout.head, o, l_run == 0.f ? 0.f : 1.f / l_run, live, mine,
+          lane);
+  if (lane < 32 && mine)
+    a.lse[(int64_t)b * a.H + h] = live ? (m_run + __log2f(l_run)) * kLn2 : -INFINITY;
+}
+
+// Join of the decode kernel's parts: a workgroup per (sequence, key/value head),
+// wave i its rows' 16-byte group i of the accumulators.
+__global__ __launch_bounds__(512) void relpos_decode_join_kernel(RelposArgs a) {
+  const int lane = threadIdx.x & 63, i = threadIdx.x >> 6;
+  const int b = blockIdx.x / a.Hkv, hk = blockIdx.x % a.Hkv;
+  const int r = lane & 31, h = hk * a.G + r;
+  if (r >= a.G) return;
+  const float *slot = a.slots + (int64_t)blockIdx.x * a.pshort * kRelposDecodeSlot;
+  float m = kFloor, l = 0.f;
+#pragma unroll 8
+  for (int p = 0; p < a.pshort; ++p) m = fmaxf(m, slot[(int64_t)p * kRelposDecodeSlot + 2048 + lane]);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int p = 0; p < a.pshort; ++p) {
+    const float *q = slot + (int64_t)p * kRelposDecodeSlot;
+    const float s = fast_exp2(q[2048 + lane] - m);
+    l += q[2112 + lane] * s;
+    const f32x4 v = *(const f32x4 *)(q + i * 256 + lane * 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += v[j] * s;
+  }
+  // The other half of the row's keys sits in lane ^ 32 (both are here or not).
+  l = add_xor32(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  bf16_t *O = (bf16_t *)a.Oout.p + b * a.Oout.seq + h * a.Oout.head + (i >> 2) * 32 + (i & 3) * 8 + (lane >> 5) * 4;
+  *(u32x2 *)O = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
+  if (i == 0 && lane < 32) a.lse[(int64_t)b * a.H + h] = (m + __log2f(l)) * kLn2;
 }
 
 // ---------------------------------------------------------------------------
@@ -346,9 +632,9 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
   __shared__ float diag[2][4 * DPITCH];
   __shared__ float bsum[2][kRelposMaxBuckets];
 
-  const int bid = xcd_remap(blockIdx.x, gridDim.x);
-  const int bh = bid / a.ntile, qb = bid % a.ntile;
-  const int b = bh / a.H, h = bh % a.H, hk = h / a.G;
+  const int L = xcd_remap(blockIdx.x, gridDim.x);
+  const Work wk = find_work(a, L);
+  const int bh = wk.bh, qb = wk.blk, b = bh / a.H, h = bh % a.H, hk = h / a.G;
   const int len = seq_len(a, b);
   const int row = qb * BQ + w * 32 + (lane & 31);
 
@@ -373,6 +659,7 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
     p0 = ld_meta(a.row_ptr + qb);
     p1 = ld_meta(a.row_ptr + qb + 1);
     trim(a.col_idx, p0, p1, qb + a.omin, min(qb + a.omax, (len + BQ - 1) / BQ - 1));
+    take_part(wk, p0, p1);
   }
   f32x16 dq[2];
 #pragma unroll
@@ -391,7 +678,7 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
   }
   delta = add_xor32(delta);
   const bool live = row < len, store = row < a.Sq;
-  if (lane < 32 && store) a.delta[(int64_t)bh * a.Sq + row] = delta;
+  if (lane < 32 && store && wk.part == 0) a.delta[(int64_t)bh * a.Sq + row] = delta;
   // Rows without a token or without a key: probability 0 everywhere.
   const float lse = live ? a.lse_in[(int64_t)bh * a.Sq + row] : -INFINITY;
   const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
@@ -463,10 +750,10 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
             for (int j = 0; j < 4; ++j) s[e4 * 4 + j] = __builtin_fmaf(s[e4 * 4 + j], c, bv[j]);
           }
           if (tail < BQ) {
-            const int k0 = (lane >> 5) * 4 + kt * 32;
+            const int lim = tail - (lane >> 5) * 4 - kt * 32;
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (k0 + (e >> 2) * 8 + (e & 3) >= tail) s[e] = -INFINITY;
+              if ((e >> 2) * 8 + (e & 3) >= lim) s[e] = -INFINITY;
           }
           cm = 1.f;
           ca = -lse2;
@@ -545,18 +832,21 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
     flush();
     wait_vm<0>();  // no copy outlives the workgroup
   }
-  put_row((bf16_t *)a.dQ.p + b * a.dQ.seq + h * a.dQ.head + (int64_t)row * a.dQ.tok, dq, a.scale, live,
-          store, lane);
+  const RelposArgs &z = late_args();
+  if (wk.slot >= 0) put_acc(z.slots + (int64_t)wk.slot * kAccFloats, dq, w, lane);
+  else
+    put_row((bf16_t *)z.dQ.p + b * z.dQ.seq + h * z.dQ.head + (int64_t)row * z.dQ.tok, dq, z.scale, live,
+            store, lane);
   __syncthreads();
-  float *P = a.partials + ((int64_t)bh * a.ntile + qb) * a.nbucket;
-  for (int i = threadIdx.x; i < a.nbucket; i += 128) P[i] = bsum[0][i] + bsum[1][i];
+  float *P = z.partials + (int64_t)L * z.nbucket;
+  for (int i = threadIdx.x; i < z.nbucket; i += 128) P[i] = bsum[0][i] + bsum[1][i];
 }
 
 // ---------------------------------------------------------------------------
 // Backward, pass 2: dK and dV (a key block of one key/value head; its G query
 // heads and their kept query blocks one after another)
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(128) void relpos_bwd_dkv_kernel(RelposArgs a) {
+__global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   uint8_t *const qs0 = stage_buf<0, TILE>(), *const gs0 = stage_buf<1, TILE>();
@@ -565,9 +855,8 @@ __global__ __launch_bounds__(128) void relpos_bwd_dkv_kernel(RelposArgs a) {
   // Row terms of the 64 queries: lse (log2 units), then -delta.
   __shared__ __attribute__((aligned(16))) float rt0[2 * BQ], rt1[2 * BQ];
 
-  const int bid = xcd_remap(blockIdx.x, gridDim.x);
-  const int bhk = bid / a.ntile, kb = bid % a.ntile;
-  const int b = bhk / a.Hkv, hk = bhk % a.Hkv;
+  const Work wk = find_work(a, xcd_remap(blockIdx.x, gridDim.x));
+  const int kb = wk.blk, b = wk.bh / a.Hkv, hk = wk.bh % a.Hkv;
   const int len = seq_len(a, b);
   const int key = kb * BQ + w * 32 + (lane & 31);
 
@@ -587,7 +876,10 @@ __global__ __launch_bounds__(128) void relpos_bwd_dkv_kernel(RelposArgs a) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) dk[0][e] = dk[1][e] = dv[0][e] = dv[1][e] = 0.f;
 
-  if (p0 < p1) {
+  // This part of the column's items: (query head of the group, position).
+  int i0 = 0, i1 = (p1 - p0) * a.G;
+  take_part(wk, i0, i1);
+  if (i0 < i1) {
     const rsrc_t rk = rows_rsrc(K, len, krb), rv = rows_rsrc(V, len, vrb);
     RowCopy qc, gc;
     qc.init(lane, w, qrb);
@@ -598,7 +890,6 @@ __global__ __launch_bounds__(128) void relpos_bwd_dkv_kernel(RelposArgs a) {
       kf[i] = frag_b(rk, key, krb, i, lane);
       vf[i] = frag_b(rv, key, vrb, i, lane);
     }
-    // Work item: query head g of the group, position p of the column's list.
     struct Item {
       int g, p;
     };
@@ -623,7 +914,7 @@ __global__ __launch_bounds__(128) void relpos_bwd_dkv_kernel(RelposArgs a) {
       rt = w == 0 ? (x == -INFINITY ? INFINITY : x * kLog2e) : -x;
     };
     const int unit = 64 + (lane >> 5) * 4 - (w * 32 + (lane & 31));
-    auto step = [&](Item nx, uint8_t *qt, uint8_t *gt, const uint8_t *wc, float (&rc)[2 * BQ],
+    auto step = [&](bool more, Item nx, uint8_t *qt, uint8_t *gt, const uint8_t *wc, float (&rc)[2 * BQ],
                     uint8_t *qn, uint8_t *gn, uint8_t *wn) __attribute__((always_inline)) {
       wait_vm<0>();
       // The stage's row terms were last read two blocks ago, before the
@@ -632,7 +923,7 @@ __global__ __launch_bounds__(128) void relpos_bwd_dkv_kernel(RelposArgs a) {
       const BlockBias bb = bf;
       wait_vm<0>();
       barrier();
-      if (nx.g < a.G) issue(nx, qn, gn, wn);
+      if (more) issue(nx, qn, gn, wn);
       const bool mixed = bb.info >= kRelposMixed;
       const float *lsep = &rc[(lane >> 5) * 4], *delp = lsep + BQ;
       const uint8_t *u = wc + unit * 16;
@@ -676,23 +967,49 @@ __global__ __launch_bounds__(128) void relpos_bwd_dkv_kernel(RelposArgs a) {
         }
       }
     };
-    Item it{0, p0};
+    Item it{i0 / (p1 - p0), p0 + i0 % (p1 - p0)};
     issue(it, qs0, gs0, w0);
-    while (it.g < a.G) {
-      Item n1 = next(it);
-      step(n1, qs0, gs0, w0, rt0, qs1, gs1, w1);
-      it = n1;
-      if (it.g >= a.G) break;
-      n1 = next(it);
-      step(n1, qs1, gs1, w1, rt1, qs0, gs0, w0);
-      it = n1;
+    for (int i = i0; i < i1; i += 2) {
+      it = next(it);
+      step(i + 1 < i1, it, qs0, gs0, w0, rt0, qs1, gs1, w1);
+      if (i + 1 < i1) {
+        it = next(it);
+        step(i + 2 < i1, it, qs1, gs1, w1, rt1, qs0, gs0, w0);
+      }
     }
+  }
+  if (wk.slot >= 0) {
+    float *slot = a.slots + (int64_t)wk.slot * (2 * kAccFloats);
+    put_acc(slot, dk, w, lane);
+    put_acc(slot + kAccFloats, dv, w, lane);
+    return;
   }
   const bool live = key < len, store = key < a.Skv;
   put_row((bf16_t *)a.dK.p + b * a.dK.seq + hk * a.dK.head + (int64_t)key * a.dK.tok, dk, a.scale, live,
           store, lane);
   put_row((bf16_t *)a.dV.p + b * a.dV.seq + hk * a.dV.head + (int64_t)key * a.dV.tok, dv, 1.f, live, store,
           lane);
+}
+
+// Sums of the parts' dQ (KV false) or dK and dV, in part order.
+template <bool KV>
+__global__ __launch_bounds__(128) void relpos_bwd_join_kernel(RelposArgs a) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const Work wk = find_join(a, blockIdx.x);
+  const int heads = KV ? a.Hkv : a.H, b = wk.bh / heads, h = wk.bh % heads;
+  const int row = wk.blk * BQ + w * 32 + (lane & 31);
+  const bool live = row < seq_len(a, b), store = row < a.Sq;
+  sfor<KV ? 2 : 1>([&](auto k) __attribute__((always_inline)) {
+    constexpr int SLOT = (KV ? 2 : 1) * kAccFloats;
+    const float *slot = a.slots + (int64_t)wk.slot * SLOT + k * kAccFloats;
+    f32x16 o[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
+    for (int p = 0; p < wk.parts; ++p) add_acc(slot + (int64_t)p * SLOT, o, 1.f, w, lane);
+    const RowViewOut &g = !KV ? a.dQ : k == 0 ? a.dK : a.dV;
+    put_row((bf16_t *)g.p + b * g.seq + h * g.head + (int64_t)row * g.tok, o, KV && k == 1 ? 1.f : a.scale,
+            live, store, lane);
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -711,54 +1028,80 @@ __global__ __launch_bounds__(256) void relpos_bias_kernel(RelposBiasArgs a) {
   o[2 * (int64_t)a.seq + (e ? 2 * a.seq - e : 0)] = v;
 }
 
-// dtable[h][c]: partials [B][H][ntile][nbucket] added over sequences and block
-// rows in a fixed order.  A workgroup takes 64 buckets of a head, 16 threads a
-// bucket.
-__global__ __launch_bounds__(1024) void relpos_dtable_kernel(const float *P, int B, int H, int ntile,
+// dtable[h][c]: the dQ launch's partials, one row of nbucket sums per
+// workgroup, added over sequences, block rows and parts in a fixed order: a head's
+// rows are `nl` consecutive ones per sequence among the long blocks', then ns
+// among the others'.  A workgroup takes 32 buckets of a head, 32 threads a bucket.
+__global__ __launch_bounds__(1024) void relpos_dtable_kernel(const float *P, int B, int H, int nl, int ns,
                                                              int nbucket, float *dtable) {
   __shared__ float red[1024];
-  const int cc = threadIdx.x & 63, part = threadIdx.x >> 6;
-  const int c = blockIdx.x * 64 + cc, h = blockIdx.y;
-  const int64_t rows = (int64_t)B * ntile;
+  const int cc = threadIdx.x & 31, part = threadIdx.x >> 5;
+  const int c = blockIdx.x * 32 + cc, h = blockIdx.y;
   float s = 0.f;
   if (c < nbucket)
-    for (int64_t r = part; r < rows; r += 16) {
-      const int64_t b = r / ntile, t = r % ntile;
-      s += P[((b * H + h) * ntile + t) * nbucket + c];
+    for (int b = 0; b < B; ++b) {
+      const int64_t bh = (int64_t)b * H + h;
+      const float *p = P + bh * nl * nbucket + c;
+      for (int r = part; r < nl; r += 32) s += p[(int64_t)r * nbucket];
+      p = P + ((int64_t)B * H * nl + bh * ns) * nbucket + c;
+#pragma unroll 4
+      for (int r = part; r < ns; r += 32) s += p[(int64_t)r * nbucket];
     }
   red[threadIdx.x] = s;
   __syncthreads();
   if (part || c >= nbucket) return;
-  for (int p = 1; p < 16; ++p) s += red[p * 64 + cc];
+  for (int p = 1; p < 32; ++p) s += red[p * 32 + cc];
   dtable[(int64_t)h * nbucket + c] = s;
 }
 
 }  // namespace
 
+namespace {
+int64_t parts_grid(const RelposArgs &a) {
+  return (int64_t)a.nbh * ((int64_t)a.nlong * a.plong + (int64_t)(a.ntile - a.nlong) * a.pshort);
+}
+int64_t join_grid(const RelposArgs &a) {
+  return (int64_t)a.nbh * ((a.plong > 1 ? a.nlong : 0) + (a.pshort > 1 ? a.ntile - a.nlong : 0));
+}
+template <typename F>
+hipError_t go(F kernel, int64_t grid, const RelposArgs &a, hipStream_t s) {
+  if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
+  launch_kernel(kernel, dim3((unsigned)grid), dim3(128), s, a);
+  return hipGetLastError();
+}
+}  // namespace
+
 hipError_t launch_relpos_fwd(const RelposArgs &a, hipStream_t s) {
-  const int64_t grid = (int64_t)a.B * a.H * a.ntile;
-  if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  launch_kernel(relpos_fwd_kernel, dim3((unsigned)grid), dim3(128), s, a);
+  return go(relpos_fwd_kernel, parts_grid(a), a, s);
+}
+hipError_t launch_relpos_fwd_join(const RelposArgs &a, hipStream_t s) {
+  return go(relpos_fwd_join_kernel, join_grid(a), a, s);
+}
+hipError_t launch_relpos_decode(const RelposArgs &a, hipStream_t s) {
+  const int64_t units = (int64_t)a.nbh * a.pshort, grid = (units + 3) / 4;
+  if (units <= 0 || units > 0x7fffffff || a.G > kRelposDecodeRows) return hipErrorInvalidValue;
+  launch_kernel(relpos_decode_kernel, dim3((unsigned)grid), dim3(256), s, a);
   return hipGetLastError();
 }
-
+hipError_t launch_relpos_decode_join(const RelposArgs &a, hipStream_t s) {
+  launch_kernel(relpos_decode_join_kernel, dim3((unsigned)a.nbh), dim3(512), s, a);
+  return hipGetLastError();
+}
 hipError_t launch_relpos_bwd_dq(const RelposArgs &a, hipStream_t s) {
-  const int64_t grid = (int64_t)a.B * a.H * a.ntile;
-  if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  launch_kernel(relpos_bwd_dq_kernel, dim3((unsigned)grid), dim3(128), s, a);
-  return hipGetLastError();
+  return go(relpos_bwd_dq_kernel, parts_grid(a), a, s);
 }
-
 hipError_t launch_relpos_bwd_dkv(const RelposArgs &a, hipStream_t s) {
-  const int64_t grid = (int64_t)a.B * a.Hkv * a.ntile;
-  if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  launch_kernel(relpos_bwd_dkv_kernel, dim3((unsigned)grid), dim3(128), s, a);
-  return hipGetLastError();
+  return go(relpos_bwd_dkv_kernel, parts_grid(a), a, s);
+}
+hipError_t launch_relpos_bwd_join(bool kv, const RelposArgs &a, hipStream_t s) {
+  return kv ? go(relpos_bwd_join_kernel<true>, join_grid(a), a, s)
+            : go(relpos_bwd_join_kernel<false>, join_grid(a), a, s);
 }
 
 hipError_t launch_relpos_dtable(const RelposArgs &a, float *dtable, hipStream_t s) {
-  launch_kernel(relpos_dtable_kernel, dim3((unsigned)((a.nbucket + 63) / 64), (unsigned)a.H), dim3(1024), s,
-                (const float *)a.partials, a.B, a.H, a.ntile, a.nbucket, dtable);
+  launch_kernel(relpos_dtable_kernel, dim3((unsigned)((a.nbucket + 31) / 32), (unsigned)a.H), dim3(1024), s,
+                (const float *)a.partials, a.B, a.H, a.nlong * a.plong, (a.ntile - a.nlong) * a.pshort,
+                a.nbucket, dtable);
   return hipGetLastError();
 }
 

@@ -211,6 +211,41 @@ def test_whole_sequences(name):
     _case(*CASES[name]).check()
 
 
+# Lists shared by several workgroups and joined: few blocks of long lists, long
+# columns and rows of stripes, grouped heads; parts that get nothing.
+SPLIT = {
+    "all_kept_1300": (1, 2, 2, 1300, "log", 0), "causal_1411": (1, 4, 1, 1411, "clipc", 0, [1300], True),
+    "stripe_1700": (2, 4, 2, 1700, "log", 2, [1700, 900], True, 1), "stripe_causal_1700": (1, 4, 1, 1700, "logc", 4, None, False, 2),
+    "grouped_1100": (1, 8, 1, 1100, "log", 2), "short_lens_1300": (2, 2, 1, 1300, "clip", 0, [20, 0]),
+    "all_stripes_1216": (1, 2, 2, 1216, "log", 1, None, False, 19),
+}
+
+
+@pytest.mark.parametrize("name", SPLIT)
+def test_lists_in_parts(name):
+    print(f"[relpos] {name} {SPLIT[name]}", flush=True)
+    _case(*SPLIT[name]).check()
+
+
+@pytest.mark.parametrize("H,Hkv,kind,ms,glob", [(8, 2, "logc", 0, 0), (4, 4, "clip", 0, 0), (32, 1, "log", 0, 0),
+                                                (33, 1, "logc", 0, 0), (3, 3, "log", 4, 1), (40, 1, "log", 4, 0)])
+def test_one_row_against_long_caches(H, Hkv, kind, ms, glob):
+    lens = [1500, 1, 64, 65, 777, 1024, 0, 3]
+    starts = [1499, 0, 63, 64, 776, 700, 5, 2]
+    c = _case(8, H, Hkv, 1500, kind, ms, lens=lens, Sq=1, starts=starts, tm=True, glob=glob)
+    c.check_fwd(*c.fwd())
+    # Without q_start the one row is the first.
+    c.dstarts = c.starts = None
+    c.check_fwd(*c.fwd())
+
+
+@pytest.mark.parametrize("rows", [2, 64, 130])
+def test_few_rows_against_long_caches(rows):
+    lens = [1500, 140, 200]
+    c = _case(3, 4, 2, 1500, "logc", 0, lens=lens, Sq=rows, starts=[1500 - rows, 140 - rows, 10])
+    c.check_fwd(*c.fwd())
+
+
 def test_long_sequence():
     c = _case(1, 2, 1, 4096, "log", 64)
     c.check()
