@@ -554,7 +554,7 @@ typedef struct {
  * Q, O: B sequences x H heads x Sq rows; K, V: B x H_kv heads x Skv tokens, query
  * head h reading key/value head h / (H / H_kv); bf16, d = 64, layout square with
  * b = 64 and the plan's seq as its side; Sq and Skv any in 1 .. seq.  lse:
- * [B][H][Sq] fp32.  scale > 0.
+ * [B][H][Sq] fp32.  scale in 2^-40 .. 2^40.
  *
  * q_start, kv_len: B int32 each in device memory, or NULL.  Row i of sequence n
  * stands at position q_start[n] + i (NULL: i) and key j at position j; the tokens of

@@ -4,7 +4,6 @@
 // see include/pixelfly.h for the contract.
 #include "capi.h"
 
-#include <cmath>
 #include <new>
 
 #include "relpos.h"
@@ -153,8 +152,9 @@ pf_status check_relpos(const pf_layout *L, const pf_relpos *R, const RelposDims 
   if (m.Sq < 1 || m.Sq > R->seq || m.Skv < 1 || m.Skv > R->seq)
     return fail(PF_ERR_INVALID_ARG, "Sq and Skv must be in 1 .. the layout's side");
   if ((int64_t)m.B * m.H > 0x7fffffff / (R->nb + 1)) return fail(PF_ERR_INVALID_ARG, "too many blocks");
-  if (!(m.scale > 0.f) || !std::isfinite(m.scale))
-    return fail(PF_ERR_INVALID_ARG, "scale must be positive and finite");
+  // The bias enters the products in units of the unscaled score.
+  if (!(m.scale >= 0x1p-40f && m.scale <= 0x1p40f))
+    return fail(PF_ERR_INVALID_ARG, "scale must be in 2^-40 .. 2^40");
   if ((st = need_ptr(bias, "bias")) != PF_OK) return st;
   if (((uintptr_t)q_start | (uintptr_t)kv_len) & 3)
     return fail(PF_ERR_INVALID_ARG, "q_start or kv_len is not 4-byte aligned");

@@ -51,20 +51,24 @@ __device__ __forceinline__ rsrc_t rows_rsrc(const bf16_t *p, int n, uint32_t row
 // TileCopy of attn_kernels.hip with a row stride.  All of the address is in the
 // lane offset, which the range check sees.
 struct RowCopy {
-  uint32_t voff[2], step;
+  uint32_t row, chunk;  // this lane's in the first window
   int w4;
-  __device__ __forceinline__ void init(int lane, int w, uint32_t row_bytes) {
+  __device__ __forceinline__ void init(int lane, int w) {
     const int x = (((lane >> 4) & 1) << 2) | (((lane >> 5) & 1) << 1);
     w4 = w * 4;
-#pragma unroll
-    for (int o = 0; o < 2; ++o)
-      voff[o] = (uint32_t)(w4 * 8 + (lane >> 3)) * row_bytes + (uint32_t)(((lane & 7) ^ x ^ o) << 4);
-    step = 8 * row_bytes;
+    row = (uint32_t)(w4 * 8 + (lane >> 3));
+    chunk = (uint32_t)(((lane & 7) ^ x) << 4);
   }
-  // off: byte offset of the tile's first row.
-  __device__ __forceinline__ void issue(rsrc_t r, uint32_t off, uint8_t *tile) const {
-    sfor<4>([&](auto i) __attribute__((always_inline)) {
-      dma16(r, tile + (w4 + i) * 1024, voff[i & 1] + off + i * step, 0);
+  // off: byte offset of the tile's first row; NW windows of 8 rows.
+  template <int NW = 4>
+  __device__ __forceinline__ void issue(rsrc_t r, uint32_t off, uint32_t row_bytes, uint8_t *tile) const {
+    // The lane offsets are formed anew each time: kept over the loop they
+    // would take the registers of four waves per SIMD.
+    uint32_t q = row, ch = chunk;
+    asm volatile("" : "+v"(q), "+v"(ch));
+    const uint32_t v = q * row_bytes + off;
+    sfor<NW>([&](auto i) __attribute__((always_inline)) {
+      dma16(r, tile + (w4 + i) * 1024, v + (ch ^ (i & 1) * 16) + i * 8 * row_bytes, 0);
     });
   }
 };
@@ -82,25 +86,30 @@ __device__ __forceinline__ bf16x8 frag_b(rsrc_t r, int row, uint32_t row_bytes, 
   return __builtin_bit_cast(bf16x8, v);
 }
 
-// Row l % 32's 64 columns (two transposed accumulators) times scale, or zeros
-// where !live, to dst when `store`.
+// Registers 8 p .. 8 p + 7 of accumulator dt (g = 2 dt + p): 16 columns of row
+// l % 32, times scale, or zeros where !live, to dst when `store`: the halves swap
+// registers so that each lane stores 16 bytes.
+__device__ __forceinline__ void put_eight(bf16_t *dst, int g, f32x4 lo, f32x4 hi, float scale, bool live,
+                                          bool store, int lane) {
+  const uint32_t x0 = pack2(lo[0] * scale, lo[1] * scale), x1 = pack2(lo[2] * scale, lo[3] * scale);
+  const uint32_t y0 = pack2(hi[0] * scale, hi[1] * scale), y1 = pack2(hi[2] * scale, hi[3] * scale);
+  const auto s0 = __builtin_amdgcn_permlane32_swap(x0, y0, false, false);
+  const auto s1 = __builtin_amdgcn_permlane32_swap(x1, y1, false, false);
+  u32x4 v = {s0[0], s1[0], s0[1], s1[1]};
+  if (!live) v = u32x4{0u, 0u, 0u, 0u};
+  if (store) *(u32x4 *)(dst + g * 16 + (lane >> 5) * 8) = v;
+}
+
+// Row l % 32's 64 columns: two transposed accumulators.
 __device__ __forceinline__ void put_row(bf16_t *dst, const f32x16 (&o)[2], float scale, bool live,
                                         bool store, int lane) {
 #pragma unroll
-  for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const int e = 8 * p;
-      const uint32_t x0 = pack2(o[dt][e] * scale, o[dt][e + 1] * scale);
-      const uint32_t x1 = pack2(o[dt][e + 2] * scale, o[dt][e + 3] * scale);
-      const uint32_t y0 = pack2(o[dt][e + 4] * scale, o[dt][e + 5] * scale);
-      const uint32_t y1 = pack2(o[dt][e + 6] * scale, o[dt][e + 7] * scale);
-      const auto s0 = __builtin_amdgcn_permlane32_swap(x0, y0, false, false);
-      const auto s1 = __builtin_amdgcn_permlane32_swap(x1, y1, false, false);
-      u32x4 v = {s0[0], s1[0], s0[1], s1[1]};
-      if (!live) v = u32x4{0u, 0u, 0u, 0u};
-      if (store) *(u32x4 *)(dst + dt * 32 + p * 16 + (lane >> 5) * 8) = v;
-    }
+  for (int g = 0; g < 4; ++g) {
+    const f32x16 &v = o[g >> 1];
+    const int e = 8 * (g & 1);
+    put_eight(dst, g, f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}, f32x4{v[e + 4], v[e + 5], v[e + 6], v[e + 7]},
+              scale, live, store, lane);
+  }
 }
 
 // x of another lane by a DPP control; lanes without a source read 0.
@@ -233,6 +242,39 @@ struct BlockBias {
   float mid;
 };
 
+// Scores are taken out of the accumulators into scalars before a branch changes
+// them: as vectors, the two sides' 16 registers would be joined by copies (21
+// spilled registers in the forward, 73 -> 90 us).
+struct Scores {
+  float v[16];
+  __device__ __forceinline__ void take(const f32x16 &s) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = s[e];
+  }
+  // In log2 units with a mixed block's bias, v c + b; u: the lane's first unit.
+  __device__ __forceinline__ void add_window(float c, const uint8_t *u) {
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      const f32x4 b = *(const f32x4 *)(u + e4 * 128);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[e4 * 4 + j] = __builtin_fmaf(v[e4 * 4 + j], c, b[j]);
+    }
+  }
+  // Keys from `lim` on (counted from the lane's first) do not exist.
+  __device__ __forceinline__ void cut(int lim) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if ((e >> 2) * 8 + (e & 3) >= lim) v[e] = -INFINITY;
+  }
+  // Entries 8 j .. 8 j + 7 as a bf16 K-operand.
+  __device__ __forceinline__ bf16x8 pack(int j) const {
+    bf16x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (__bf16)v[8 * j + e];
+    return r;
+  }
+};
+
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
@@ -286,15 +328,14 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
   float m_run = kFloor, l_run = 0.f;  // l_run: this lane's keys only
 
   if (p0 < p1) {
-    RowCopy kc, vc;
-    kc.init(lane, w, krb);
-    vc.init(lane, w, vrb);
+    RowCopy cp;
+    cp.init(lane, w);
     auto block_bias = [&](int col) __attribute__((always_inline)) {
       const int d = col - qb;
       return BlockBias{ld_meta(a.info + d + a.nb - 1), ld_meta(bias + d * BQ + a.seq)};
     };
     auto issue_k = [&](int col, uint8_t *win) __attribute__((always_inline)) {
-      kc.issue(rk, (uint32_t)(col * BQ) * krb, ks);
+      cp.issue(rk, (uint32_t)(col * BQ) * krb, krb, ks);
       copy_window(rb, ((col - qb) * BQ + a.seq - BQ) * 4, win, lane, w);
     };
     int ccur = ld_meta(a.col_idx + p0);
@@ -309,51 +350,42 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
 
     // Unit of this lane's first key in the window: key - query + 64.
     const int unit = 64 + (lane >> 5) * 4 - (w * 32 + (lane & 31));
-    f32x16 s[2];
-    auto step = [&](int p, const uint8_t *wc, uint8_t *wn) __attribute__((always_inline)) {
+    Scores s[2];
+    auto step = [&](int p, const uint8_t *win, uint8_t *wnext) __attribute__((always_inline)) {
       wait_vm<0>();  // this wave's K and window have landed,
       barrier();     // every wave's have, and the last block's V is read
-      vc.issue(rv, (uint32_t)(ccur * BQ) * vrb, vs);
+      cp.issue(rv, (uint32_t)(ccur * BQ) * vrb, vrb, vs);
       const BlockBias bn = block_bias(cn);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
+        f32x16 acc;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[kt][e] = 0.f;
+        for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[kt] = MFMA32(frag_r(ks, kt * 32, i, lane), qf[i], s[kt]);
+        for (int i = 0; i < 4; ++i) acc = MFMA32(frag_r(ks, kt * 32, i, lane), qf[i], acc);
+        s[kt].take(acc);
       }
       wait_vm<4>();  // (no wait: the four V copies may be in flight)
       barrier();     // every wave has read K
-      issue_k(cn, wn);
+      issue_k(cn, wnext);
       // Scores in log2 units: s cm + ca.
       float cm = c, ca = bb.mid;
-      const int tail = len - ccur * BQ;  // keys of the block that exist
-      if (bb.info >= kRelposMixed || tail < BQ) {
-        const uint8_t *u = wc + unit * 16;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int e4 = 0; e4 < 4; ++e4) {
-            const f32x4 bv = *(const f32x4 *)(u + (kt * 32 + e4 * 8) * 16);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[kt][e4 * 4 + j] = __builtin_fmaf(s[kt][e4 * 4 + j], c, bv[j]);
-          }
-        if (tail < BQ) {
-          const int lim = tail - (lane >> 5) * 4;
-#pragma unroll
-          for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (kt * 32 + (e >> 2) * 8 + (e & 3) >= lim) s[kt][e] = -INFINITY;
-        }
+      if (bb.info >= kRelposMixed) {
+        s[0].add_window(c, win + unit * 16);
+        s[1].add_window(c, win + unit * 16 + 512);
         cm = 1.f;
         ca = 0.f;
+      }
+      const int left = len - ccur * BQ;  // keys from the block's first on
+      if (left < BQ) {
+        s[0].cut(left - (lane >> 5) * 4);
+        s[1].cut(left - (lane >> 5) * 4 - 32);
       }
       float bmax = -INFINITY;
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) bmax = fmaxf(bmax, s[kt][e]);
+        for (int e = 0; e < 16; ++e) bmax = fmaxf(bmax, s[kt].v[e]);
       // The reference m_run (the same in both lanes of a query) moves only when
       // some lane's maximum grew by more than 8 (log2 units): until then the
       // probabilities stay below 2^8.
@@ -374,8 +406,8 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float x = fast_exp2(__builtin_fmaf(s[kt][e], cm, off));
-          s[kt][e] = x;
+          const float x = fast_exp2(__builtin_fmaf(s[kt].v[e], cm, off));
+          s[kt].v[e] = x;
           rs += x;
         }
       l_run += rs;
@@ -388,12 +420,13 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const bf16x8 pb = pack_k(s[kt], j);
+          const bf16x8 pb = s[kt].pack(j);
 #pragma unroll
           for (int dt = 0; dt < 2; ++dt)
             o[dt] = MFMA32(frag_t(vs, kt * 32 + j * 16, dt * 32, lane), pb, o[dt]);
         }
     };
+    // Two windows in turn: a block's is read after the next one's copy has begun.
     for (int p = p0; p < p1; p += 2) {
       step(p, w0, w1);
       if (p + 1 < p1) step(p + 1, w1, w0);
@@ -473,19 +506,13 @@ __global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
   for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
   float m_run = kFloor, l_run = 0.f;
   if (p0 < p1) {
-    RowCopy kc, vc;
-    kc.init(lane, 0, krb);
-    vc.init(lane, 0, vrb);
-    auto copy = [&](const RowCopy &rc, rsrc_t rs, uint32_t off, uint8_t *tile) __attribute__((always_inline)) {
-      sfor<8>([&](auto i) __attribute__((always_inline)) {
-        dma16(rs, tile + i * 1024, rc.voff[i & 1] + off + i * rc.step, 0);
-      });
-    };
+    RowCopy cp;
+    cp.init(lane, 0);
     // Bias of this lane's head (rows past G read 0), from key 0's distance on.
     const rsrc_t rb = make_rsrc(a.bias + (int64_t)hk * a.G * a.bias_ld, (int64_t)a.G * a.bias_ld * 4);
     const uint32_t boff = (uint32_t)r * (uint32_t)(a.bias_ld * 4) + (uint32_t)(a.seq - pos + (lane >> 5) * 4) * 4u;
     int col = ld_meta(a.col_idx + p0);
-    copy(kc, rk, (uint32_t)(col * BQ) * krb, ks);
+    cp.issue<8>(rk, (uint32_t)(col * BQ) * krb, krb, ks);
     bf16x8 qf[4];
     const bf16_t *Q = (const bf16_t *)a.Q.p + b * a.Q.seq + h * a.Q.head;
 #pragma unroll
@@ -502,7 +529,7 @@ __global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
             rb, mine ? (int)(boff + (uint32_t)(cb * BQ + i * 8) * 4u) : 0x7ffffff0, 0, 0);
     };
     load_bias(col);
-    copy(vc, rv, (uint32_t)(col * BQ) * vrb, vs);
+    cp.issue<8>(rv, (uint32_t)(col * BQ) * vrb, vrb, vs);
     for (int p = p0; p < p1; ++p) {
       const int cn = ld_meta(a.col_idx + min(p + 1, p1 - 1));
       // The waits count the copies alone: eight newer ones, whatever the
@@ -517,7 +544,7 @@ __global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
         for (int i = 0; i < 4; ++i) s[kt] = MFMA32(frag_r(ks, kt * 32, i, lane), qf[i], s[kt]);
       }
       wait_vm<63>();  // (K's reads have returned)
-      copy(kc, rk, (uint32_t)(cn * BQ) * krb, ks);
+      cp.issue<8>(rk, (uint32_t)(cn * BQ) * krb, krb, ks);
       const int lim = len - col * BQ - (lane >> 5) * 4;
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
@@ -564,7 +591,7 @@ __global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
             o[dt] = MFMA32(frag_t(vs, kt * 32 + j * 16, dt * 32, lane), pb, o[dt]);
         }
       wait_vm<63>();  // (V's reads have returned)
-      copy(vc, rv, (uint32_t)(cn * BQ) * vrb, vs);
+      cp.issue<8>(rv, (uint32_t)(cn * BQ) * vrb, vrb, vs);
       col = cn;
     }
     wait_vm<0>();  // no copy outlives the wave
@@ -588,33 +615,50 @@ __global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
     a.lse[(int64_t)b * a.H + h] = live ? (m_run + __log2f(l_run)) * kLn2 : -INFINITY;
 }
 
-// Join of the decode kernel's parts: a workgroup per (sequence, key/value head),
-// wave i its rows' 16-byte group i of the accumulators.
-__global__ __launch_bounds__(512) void relpos_decode_join_kernel(RelposArgs a) {
-  const int lane = threadIdx.x & 63, i = threadIdx.x >> 6;
-  const int b = blockIdx.x / a.Hkv, hk = blockIdx.x % a.Hkv;
-  const int r = lane & 31, h = hk * a.G + r;
-  if (r >= a.G) return;
-  const float *slot = a.slots + (int64_t)blockIdx.x * a.pshort * kRelposDecodeSlot;
+// Join of the decode kernel's parts, a workgroup per (sequence, query head):
+// 16 threads across the row's columns, four each, 16 threads down the parts; each
+// runs through its parts online, then the 16 are added through LDS in order.
+__global__ __launch_bounds__(256) void relpos_decode_join_kernel(RelposArgs a) {
+  __shared__ float mx[16], red[16][16 * 5];
+  const int cg = threadIdx.x & 15, q = threadIdx.x >> 4;
+  const int b = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / a.G, r = h - hk * a.G;
+  // Columns 4 cg ..: accumulator group i of lane r (+ 32 for the odd fours).
+  const int i = (cg >> 3) * 4 + ((cg & 7) >> 1), lane = r + (cg & 1) * 32;
+  const float *slot = a.slots + ((int64_t)b * a.Hkv + hk) * a.pshort * kRelposDecodeSlot;
   float m = kFloor, l = 0.f;
-#pragma unroll 8
-  for (int p = 0; p < a.pshort; ++p) m = fmaxf(m, slot[(int64_t)p * kRelposDecodeSlot + 2048 + lane]);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int p = 0; p < a.pshort; ++p) {
-    const float *q = slot + (int64_t)p * kRelposDecodeSlot;
-    const float s = fast_exp2(q[2048 + lane] - m);
-    l += q[2112 + lane] * s;
-    const f32x4 v = *(const f32x4 *)(q + i * 256 + lane * 4);
+#pragma unroll 2
+  for (int p = q; p < a.pshort; p += 16) {
+    const float *s = slot + (int64_t)p * kRelposDecodeSlot;
+    const float mp = s[2048 + r], lp = s[2112 + r] + s[2112 + 32 + r];
+    const f32x4 v = *(const f32x4 *)(s + i * 256 + lane * 4);
+    const float mn = fmaxf(m, mp), x = fast_exp2(m - mn), y = fast_exp2(mp - mn);
+    l = l * x + lp * y;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] += v[j] * s;
+    for (int j = 0; j < 4; ++j) o[j] = o[j] * x + v[j] * y;
+    m = mn;
   }
-  // The other half of the row's keys sits in lane ^ 32 (both are here or not).
-  l = add_xor32(l);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  bf16_t *O = (bf16_t *)a.Oout.p + b * a.Oout.seq + h * a.Oout.head + (i >> 2) * 32 + (i & 3) * 8 + (lane >> 5) * 4;
-  *(u32x2 *)O = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
-  if (i == 0 && lane < 32) a.lse[(int64_t)b * a.H + h] = (m + __log2f(l)) * kLn2;
+  if (cg == 0) mx[q] = m;
+  __syncthreads();
+  float top = mx[0];
+#pragma unroll
+  for (int k = 1; k < 16; ++k) top = fmaxf(top, mx[k]);
+  const float x = fast_exp2(m - top);
+  float *mine = &red[q][cg * 5];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) mine[j] = o[j] * x;
+  mine[4] = l * x;
+  __syncthreads();
+  if (q) return;
+  float s[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 16; ++k)
+#pragma unroll
+    for (int j = 0; j < 5; ++j) s[j] += red[k][cg * 5 + j];
+  const float inv = s[4] == 0.f ? 0.f : 1.f / s[4];
+  bf16_t *O = (bf16_t *)a.Oout.p + b * a.Oout.seq + h * a.Oout.head + cg * 4;
+  *(u32x2 *)O = u32x2{pack2(s[0] * inv, s[1] * inv), pack2(s[2] * inv, s[3] * inv)};
+  if (cg == 0) a.lse[blockIdx.x] = (top + __log2f(s[4])) * kLn2;
 }
 
 // ---------------------------------------------------------------------------
@@ -626,7 +670,7 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   uint8_t *const ks = stage_buf<0, TILE>(), *const vs = stage_buf<1, TILE>();
-  uint8_t *const w0 = stage_buf<2, WIN>(), *const w1 = stage_buf<3, WIN>();
+  uint8_t *const win = stage_buf<2, WIN>();
   // Per wave: the diagonals of a block by lane row (16 queries, one half of the
   // keys), zero where a row has none; sums per bucket.
   __shared__ float diag[2][4 * DPITCH];
@@ -684,20 +728,19 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
   const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
 
   if (p0 < p1) {
-    RowCopy kc, vc;
-    kc.init(lane, w, krb);
-    vc.init(lane, w, vrb);
+    RowCopy cp;
+    cp.init(lane, w);
     auto block_bias = [&](int col) __attribute__((always_inline)) {
       const int d = col - qb;
       return BlockBias{ld_meta(a.info + d + a.nb - 1), ld_meta(bias + d * BQ + a.seq)};
     };
-    auto issue_k = [&](int col, uint8_t *win) __attribute__((always_inline)) {
-      kc.issue(rk, (uint32_t)(col * BQ) * krb, ks);
+    auto issue_k = [&](int col) __attribute__((always_inline)) {
+      cp.issue(rk, (uint32_t)(col * BQ) * krb, krb, ks);
       copy_window(rb, ((col - qb) * BQ + a.seq - BQ) * 4, win, lane, w);
     };
     int ccur = ld_meta(a.col_idx + p0);
-    vc.issue(rv, (uint32_t)(ccur * BQ) * vrb, vs);
-    issue_k(ccur, w0);
+    cp.issue(rv, (uint32_t)(ccur * BQ) * vrb, vrb, vs);
+    issue_k(ccur);
     BlockBias bb = block_bias(ccur);
     int cn = ld_meta(a.col_idx + min(p0 + 1, p1 - 1));
     const int unit = 64 + (lane >> 5) * 4 - (w * 32 + (lane & 31));
@@ -716,20 +759,11 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
       usum = 0.f;
     };
 
-    f32x16 s, dp;
-    auto scores = [&](int kt) __attribute__((always_inline)) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s = MFMA32(frag_r(ks, kt * 32, i, lane), qf[i], s);
-        dp = MFMA32(frag_r(vs, kt * 32, i, lane), gf[i], dp);
-      }
-    };
-    auto step = [&](int p, const uint8_t *wc, uint8_t *wn) __attribute__((always_inline)) {
+    Scores s;
+    f32x16 dp;
+    for (int p = p0; p < p1; ++p) {
       wait_vm<0>();  // this wave's copies of the block have landed,
       barrier();     // every wave's have
-      const int tail = len - ccur * BQ;
       const bool mixed = bb.info >= kRelposMixed;
       // Order by bucket of a mixed block's distances, two per lane.
       const uint32_t ord = mixed ? a.order[(int64_t)(bb.info - kRelposMixed) * 64 + lane] : 0u;
@@ -737,31 +771,29 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
         flush();
         ucur = bb.info;
       }
-      float acc[5] = {};
+      const BlockBias bn = block_bias(cn);
+      const float cm = mixed ? 1.f : c, ca = (mixed ? 0.f : bb.mid) - lse2;
+      const int left = len - ccur * BQ;  // keys from the block's first on
+      float dsum[5] = {};
+      auto scores = [&](int kt) __attribute__((always_inline)) {
+        f32x16 acc;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] = dp[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          acc = MFMA32(frag_r(ks, kt * 32, i, lane), qf[i], acc);
+          dp = MFMA32(frag_r(vs, kt * 32, i, lane), gf[i], dp);
+        }
+        s.take(acc);
+      };
       auto grads = [&](auto kt_) __attribute__((always_inline)) {
         constexpr int kt = decltype(kt_)::value;
-        float cm = c, ca = bb.mid - lse2;
-        if (mixed || tail < BQ) {
-          const uint8_t *u = wc + unit * 16;
-#pragma unroll
-          for (int e4 = 0; e4 < 4; ++e4) {
-            const f32x4 bv = *(const f32x4 *)(u + (kt * 32 + e4 * 8) * 16);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[e4 * 4 + j] = __builtin_fmaf(s[e4 * 4 + j], c, bv[j]);
-          }
-          if (tail < BQ) {
-            const int lim = tail - (lane >> 5) * 4 - kt * 32;
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if ((e >> 2) * 8 + (e & 3) >= lim) s[e] = -INFINITY;
-          }
-          cm = 1.f;
-          ca = -lse2;
-        }
+        if (mixed) s.add_window(c, win + (unit + kt * 32) * 16);
+        if (left < BQ) s.cut(left - (lane >> 5) * 4 - kt * 32);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float pr = fast_exp2(__builtin_fmaf(s[e], cm, ca));
-          s[e] = pr * (dp[e] - delta);  // dS^T
+          const float pr = fast_exp2(__builtin_fmaf(s.v[e], cm, ca));
+          s.v[e] = pr * (dp[e] - delta);  // dS^T
         }
         if (mixed) {
           // Key 16 a + j + 4 (l / 32) of this half, query lane x of its 16:
@@ -770,35 +802,34 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
             constexpr int e = decltype(ee)::value;
             constexpr int j = ((e >> 2) & 1) * 8 + (e & 3), m = kt * 2 + (e >> 3);
             if constexpr (j == 0) {
-              acc[m] += s[e];
+              dsum[m] += s.v[e];
             } else {
-              acc[m] += dpp0<kRowShl + j>(s[e]);
-              acc[m + 1] += dpp0<kRowShr + 16 - j>(s[e]);
+              dsum[m] += dpp0<kRowShl + j>(s.v[e]);
+              dsum[m + 1] += dpp0<kRowShr + 16 - j>(s.v[e]);
             }
           });
         } else {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) usum += s[e];
+          for (int e = 0; e < 16; ++e) usum += s.v[e];
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const bf16x8 d = pack_k(s, j);
+          const bf16x8 d = s.pack(j);
 #pragma unroll
           for (int dt = 0; dt < 2; ++dt)
             dq[dt] = MFMA32(frag_t(ks, kt * 32 + j * 16, dt * 32, lane), d, dq[dt]);
         }
       };
-      const BlockBias bn = block_bias(cn);
       scores(0);
       grads(std::integral_constant<int, 0>{});
       scores(1);
       wait_vm<0>();
       barrier();  // every wave has read V
-      vc.issue(rv, (uint32_t)(cn * BQ) * vrb, vs);
+      cp.issue(rv, (uint32_t)(cn * BQ) * vrb, vrb, vs);
       grads(std::integral_constant<int, 1>{});
       if (mixed) {
 #pragma unroll
-        for (int m = 0; m < 5; ++m) dg[16 * m] = acc[m];
+        for (int m = 0; m < 5; ++m) dg[16 * m] = dsum[m];
         const int o0 = ord & 127, o1 = (ord >> 8) & 127, i0 = (ord >> 16) & 255, i1 = ord >> 24;
         const float *dd = diag[w];
         float v0 = 0.f, v1 = 0.f;
@@ -822,12 +853,8 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
       bb = bn;
       cn = ld_meta(a.col_idx + min(p + 2, p1 - 1));
       wait_vm<4>();
-      barrier();  // every wave has read K
-      issue_k(ccur, wn);
-    };
-    for (int p = p0; p < p1; p += 2) {
-      step(p, w0, w1);
-      if (p + 1 < p1) step(p + 1, w1, w0);
+      barrier();  // every wave has read K and the window
+      issue_k(ccur);
     }
     flush();
     wait_vm<0>();  // no copy outlives the workgroup
@@ -852,7 +879,8 @@ __global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
   uint8_t *const qs0 = stage_buf<0, TILE>(), *const gs0 = stage_buf<1, TILE>();
   uint8_t *const qs1 = stage_buf<2, TILE>(), *const gs1 = stage_buf<3, TILE>();
   uint8_t *const w0 = stage_buf<4, WIN>(), *const w1 = stage_buf<5, WIN>();
-  // Row terms of the 64 queries: lse (log2 units), then -delta.
+  // Row terms of the 64 queries: lse (log2 units, less the bias of a block of one
+  // bucket), then -delta.
   __shared__ __attribute__((aligned(16))) float rt0[2 * BQ], rt1[2 * BQ];
 
   const Work wk = find_work(a, xcd_remap(blockIdx.x, gridDim.x));
@@ -864,7 +892,7 @@ __global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
   const bf16_t *V = (const bf16_t *)a.V.p + b * a.V.seq + hk * a.V.head;
   const uint32_t qrb = (uint32_t)(a.Q.tok * 2), krb = (uint32_t)(a.K.tok * 2), vrb = (uint32_t)(a.V.tok * 2);
   const uint32_t grb = (uint32_t)(a.dO.tok * 2);
-  const float c = a.scale * kLog2e;
+  const float c = a.scale * kLog2e, inv_c = 1.f / c;
 
   int p0 = 0, p1 = 0;
   if (len > kb * BQ) {
@@ -881,9 +909,8 @@ __global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
   take_part(wk, i0, i1);
   if (i0 < i1) {
     const rsrc_t rk = rows_rsrc(K, len, krb), rv = rows_rsrc(V, len, vrb);
-    RowCopy qc, gc;
-    qc.init(lane, w, qrb);
-    gc.init(lane, w, grb);
+    RowCopy cp;
+    cp.init(lane, w);
     bf16x8 kf[4], vf[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -896,22 +923,21 @@ __global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
     auto next = [&](Item it) __attribute__((always_inline)) {
       return it.p + 1 < p1 ? Item{it.g, it.p + 1} : Item{it.g + 1, p0};
     };
-    float rt = 0.f;  // row term of the block in flight (wave 0: lse, wave 1: -delta)
-    BlockBias bf{0, 0.f};  // its bias
+    float rt = 0.f;  // row term of the block in flight (wave 0: lse, wave 1: delta)
+    BlockBias bf{0, 0.f};  // the bias of the block in flight
     auto issue = [&](Item it, uint8_t *qt, uint8_t *gt, uint8_t *win) __attribute__((always_inline)) {
       const int h = hk * a.G + it.g, qb = ld_meta(a.row_idx + it.p);
       const bf16_t *Q = (const bf16_t *)a.Q.p + b * a.Q.seq + h * a.Q.head;
       const bf16_t *dO = (const bf16_t *)a.dO.p + b * a.dO.seq + h * a.dO.head;
-      qc.issue(rows_rsrc(Q, len, qrb), (uint32_t)(qb * BQ) * qrb, qt);
-      gc.issue(rows_rsrc(dO, len, grb), (uint32_t)(qb * BQ) * grb, gt);
+      cp.issue(rows_rsrc(Q, len, qrb), (uint32_t)(qb * BQ) * qrb, qrb, qt);
+      cp.issue(rows_rsrc(dO, len, grb), (uint32_t)(qb * BQ) * grb, grb, gt);
       // The head's bias by descending distance: by query - key.
       const float *rev = a.bias + (int64_t)h * a.bias_ld + 2 * (int64_t)a.seq;
       copy_window(make_rsrc(rev, (int64_t)a.seq * 8), ((qb - kb) * BQ + a.seq - BQ) * 4, win, lane, w);
       bf = BlockBias{ld_meta(a.info + (kb - qb) + a.nb - 1), ld_meta(rev + (qb - kb) * BQ + a.seq)};
       const int q = qb * BQ + lane;
       const float *src = (w == 0 ? a.lse_in : a.delta) + (int64_t)(b * a.H + h) * a.Sq;
-      float x = q < len ? src[q] : (w == 0 ? -INFINITY : 0.f);
-      rt = w == 0 ? (x == -INFINITY ? INFINITY : x * kLog2e) : -x;
+      rt = q < len ? src[q] : (w == 0 ? -INFINITY : 0.f);
     };
     const int unit = 64 + (lane >> 5) * 4 - (w * 32 + (lane & 31));
     auto step = [&](bool more, Item nx, uint8_t *qt, uint8_t *gt, const uint8_t *wc, float (&rc)[2 * BQ],
@@ -919,19 +945,30 @@ __global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
       wait_vm<0>();
       // The stage's row terms were last read two blocks ago, before the
       // previous barrier.
-      rc[w * BQ + lane] = rt;
-      const BlockBias bb = bf;
+      const bool mixed = bf.info >= kRelposMixed;
+      rc[w * BQ + lane] = w ? -rt : rt == -INFINITY ? INFINITY : rt * kLog2e - (mixed ? 0.f : bf.mid);
       wait_vm<0>();
       barrier();
       if (more) issue(nx, qn, gn, wn);
-      const bool mixed = bb.info >= kRelposMixed;
       const float *lsep = &rc[(lane >> 5) * 4], *delp = lsep + BQ;
-      const uint8_t *u = wc + unit * 16;
 #pragma unroll
       for (int qq = 0; qq < 2; ++qq) {
-        // S[query][key], dP[query][key] of 32 queries x this wave's 32 keys;
-        // dP starts at -delta.
-        f32x16 s = {}, dp;
+        // S[query][key], dP[query][key] of 32 queries x this wave's 32 keys; dP
+        // starts at -delta.
+        f32x16 s, dp;
+        // A mixed block's scores start at their bias, in units of the unscaled
+        // score: what follows is the same for every block.
+        if (mixed) {
+#pragma unroll
+          for (int e4 = 0; e4 < 4; ++e4) {
+            const f32x4 bv = *(const f32x4 *)(wc + (unit + qq * 32 + e4 * 8) * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[e4 * 4 + j] = bv[j] * inv_c;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] = 0.f;
+        }
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
           const f32x4 de = *(const f32x4 *)(delp + qq * 32 + e4 * 8);
@@ -946,12 +983,10 @@ __global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
           const f32x4 ls = *(const f32x4 *)(lsep + qq * 32 + e4 * 8);
-          f32x4 bv = {bb.mid, bb.mid, bb.mid, bb.mid};
-          if (mixed) bv = *(const f32x4 *)(u + (qq * 32 + e4 * 8) * 16);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int e = e4 * 4 + j;
-            const float pr = fast_exp2(__builtin_fmaf(s[e], c, bv[j] - ls[j]));
+            const float pr = fast_exp2(__builtin_fmaf(s[e], c, -ls[j]));
             s[e] = pr;
             dp[e] = pr * dp[e];  // dS
           }
@@ -991,25 +1026,28 @@ __global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
           lane);
 }
 
-// Sums of the parts' dQ (KV false) or dK and dV, in part order.
+// Sums of the parts' dQ (KV false) or dK and dV, in part order: four workgroups
+// per block and tensor, eight accumulator registers each.
 template <bool KV>
 __global__ __launch_bounds__(128) void relpos_bwd_join_kernel(RelposArgs a) {
+  constexpr int GROUPS = KV ? 8 : 4, SLOT = (KV ? 2 : 1) * kAccFloats;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const Work wk = find_join(a, blockIdx.x);
+  const Work wk = find_join(a, blockIdx.x / GROUPS);
+  const int kv = blockIdx.x % GROUPS / 4, g = blockIdx.x % 4;
   const int heads = KV ? a.Hkv : a.H, b = wk.bh / heads, h = wk.bh % heads;
   const int row = wk.blk * BQ + w * 32 + (lane & 31);
   const bool live = row < seq_len(a, b), store = row < a.Sq;
-  sfor<KV ? 2 : 1>([&](auto k) __attribute__((always_inline)) {
-    constexpr int SLOT = (KV ? 2 : 1) * kAccFloats;
-    const float *slot = a.slots + (int64_t)wk.slot * SLOT + k * kAccFloats;
-    f32x16 o[2];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
-    for (int p = 0; p < wk.parts; ++p) add_acc(slot + (int64_t)p * SLOT, o, 1.f, w, lane);
-    const RowViewOut &g = !KV ? a.dQ : k == 0 ? a.dK : a.dV;
-    put_row((bf16_t *)g.p + b * g.seq + h * g.head + (int64_t)row * g.tok, o, KV && k == 1 ? 1.f : a.scale,
-            live, store, lane);
-  });
+  const float *slot = a.slots + (int64_t)wk.slot * SLOT + kv * kAccFloats + g * 1024 + (w * 64 + lane) * 4;
+  f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+#pragma unroll 4
+  for (int p = 0; p < wk.parts; ++p) {
+    lo += *(const f32x4 *)(slot + (int64_t)p * SLOT);
+    hi += *(const f32x4 *)(slot + (int64_t)p * SLOT + 512);
+  }
+  const RowViewOut &t = !KV ? a.dQ : kv == 0 ? a.dK : a.dV;
+  const float scale = KV && kv == 1 ? 1.f : a.scale;
+  bf16_t *dst = (bf16_t *)t.p + b * t.seq + h * t.head + (int64_t)row * t.tok;
+  put_eight(dst, g, lo, hi, scale, live, store, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -1084,7 +1122,7 @@ hipError_t launch_relpos_decode(const RelposArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 hipError_t launch_relpos_decode_join(const RelposArgs &a, hipStream_t s) {
-  launch_kernel(relpos_decode_join_kernel, dim3((unsigned)a.nbh), dim3(512), s, a);
+  launch_kernel(relpos_decode_join_kernel, dim3((unsigned)(a.B * a.H)), dim3(256), s, a);
   return hipGetLastError();
 }
 hipError_t launch_relpos_bwd_dq(const RelposArgs &a, hipStream_t s) {
@@ -1094,8 +1132,8 @@ hipError_t launch_relpos_bwd_dkv(const RelposArgs &a, hipStream_t s) {
   return go(relpos_bwd_dkv_kernel, parts_grid(a), a, s);
 }
 hipError_t launch_relpos_bwd_join(bool kv, const RelposArgs &a, hipStream_t s) {
-  return kv ? go(relpos_bwd_join_kernel<true>, join_grid(a), a, s)
-            : go(relpos_bwd_join_kernel<false>, join_grid(a), a, s);
+  return kv ? go(relpos_bwd_join_kernel<true>, 8 * join_grid(a), a, s)
+            : go(relpos_bwd_join_kernel<false>, 4 * join_grid(a), a, s);
 }
 
 hipError_t launch_relpos_dtable(const RelposArgs &a, float *dtable, hipStream_t s) {
