@@ -199,25 +199,33 @@ struct Parts {
   }
 };
 
-// Blocks (items of a list) per part, where a list is shared at all.
-constexpr int kLongItems = 16;
-// Fewest items of a part of the other blocks, and the workgroups they are split
-// up to.
-constexpr int kShortItems = 4;
-constexpr int64_t kShortWG = 512;
+// Blocks (items) per part of the long lists: 8 x 12 x 4096 with a stripe, lists of
+// 64 in parts of 16 / 12 / 8, backward 377 / 347 / 328 us, forward 133 / 129 / 121.
+constexpr int kLongItems = 8;
+// The other lists are split where their blocks make fewer workgroups than `fill`, in
+// parts of at least `least` items.  Rows (forward and dQ): 512 and 4; 12 heads x
+// 2048, every block kept, 384 workgroups: two parts 35.4 us, three 38.1.  dK and
+// dV, whose slots are twice as large: 1024 and 16; 4 x 4 x 2048 causal, four query
+// heads each (512 workgroups, up to 128 items): one part 325 us, two 234; 4 x 4 x 1511
+// (368, 24 items on average): two 68, three 77.
+constexpr int kShortItems = 16;  // lists up to here stay whole
+struct Split {
+  int64_t fill, least;
+};
+constexpr Split kRowSplit{512, 4}, kColSplit{1024, 16};
 
 // long_items: list length of the nlong leading blocks, items: of the others.
-Parts choose_parts(int nbh, int ntile, int nlong, int64_t long_items, int64_t items) {
+Parts choose_parts(int nbh, int ntile, int nlong, int64_t long_items, int64_t items, const Split &s) {
   Parts p;
   p.nbh = nbh;
   p.ntile = ntile;
-  if (nlong > 0 && long_items > kLongItems) {
+  if (nlong > 0 && long_items > kShortItems) {
     p.nlong = std::min(nlong, ntile);
     p.plong = (int)((long_items + kLongItems - 1) / kLongItems);
   }
   const int64_t wg = (int64_t)nbh * (ntile - p.nlong);
-  if (wg > 0 && wg < kShortWG && items > kLongItems)
-    p.pshort = (int)std::min((kShortWG + wg - 1) / wg, (items + kShortItems - 1) / kShortItems);
+  if (wg > 0 && wg < s.fill && items > kShortItems)
+    p.pshort = (int)std::min((s.fill + wg - 1) / wg, (items + s.least - 1) / s.least);
   return p;
 }
 
@@ -247,21 +255,25 @@ Parts fwd_parts(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, in
   const Lists l = row_lists(L, R, false);
   // A chunk starts anywhere in a block, and anywhere in its sequence: which of
   // its tiles are a stripe's is not known here.
-  return choose_parts(B * H, (Sq + (chunk ? 63 : 0) + 63) / 64, chunk ? 0 : l.nlong, l.long_items, l.items);
+  return choose_parts(B * H, (Sq + (chunk ? 63 : 0) + 63) / 64, chunk ? 0 : l.nlong, l.long_items, l.items,
+                      kRowSplit);
 }
 Parts dkv_parts(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t Hkv, int32_t S) {
   const Lists l = row_lists(L, R, true);
   const int G = H / Hkv;
-  return choose_parts(B * Hkv, (S + 63) / 64, l.nlong, l.long_items * G, l.items * G);
+  return choose_parts(B * Hkv, (S + 63) / 64, l.nlong, l.long_items * G, l.items * G, kColSplit);
 }
-// Waves per (sequence, key/value head) of the decode kernel.
+// Waves per (sequence, key/value head) of the decode kernel: lists of eight blocks
+// or more are split up to 1024 waves in all, at least two blocks each (16 x 4 heads of
+// 4096 keys: one wave 68 us, 1024 in all 16.6, 2048 19.2; 12 heads of 1000 keys: one
+// 20.7, eight 12.3; seven blocks in two parts 12.3 against 11.7 in one).
 Parts decode_parts(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t Hkv) {
   const Lists l = row_lists(L, R, false);
   Parts p;
   p.nbh = B * Hkv;
   p.ntile = 1;
-  const int64_t want = (2048 + p.nbh - 1) / p.nbh, most = (l.items + 1) / 2;
-  p.pshort = (int)std::max<int64_t>(1, l.items >= 8 ? std::min(want, most) : 1);
+  if (l.items >= 8)
+    p.pshort = (int)std::max<int64_t>(1, std::min<int64_t>((1024 + p.nbh - 1) / p.nbh, (l.items + 1) / 2));
   return p;
 }
 bool use_decode(int32_t Sq, int32_t H, int32_t Hkv) { return Sq == 1 && H / Hkv <= pf::kRelposDecodeRows; }

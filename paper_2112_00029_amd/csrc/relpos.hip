@@ -445,27 +445,40 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
   fwd_store(z, bh, row, nrow, o, m_run, l_run, lane);
 }
 
-// Join of the forward's parts: each relative to the largest running maximum.
+// Join of the forward's parts in order, online: four workgroups per block, eight
+// accumulator registers each.
 __global__ __launch_bounds__(128) void relpos_fwd_join_kernel(RelposArgs a) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const Work wk = find_join(a, blockIdx.x);
-  const int b = wk.bh / a.H;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = blockIdx.x & 3;
+  const Work wk = find_join(a, blockIdx.x >> 2);
+  const int b = wk.bh / a.H, h = wk.bh % a.H;
   const int start = a.q_start ? min(max(ld_meta(a.q_start + b), 0), a.seq) : 0;
-  const int row = ((start >> 6) + wk.blk) * BQ + w * 32 + (lane & 31) - start;
-  if (((start >> 6) + wk.blk) * BQ - start >= a.Sq) return;  // no part has written
+  const int first = ((start >> 6) + wk.blk) * BQ - start;
+  if (first >= a.Sq) return;  // no part has written
+  const int row = first + w * 32 + (lane & 31);
   const float *slot = a.slots + (int64_t)wk.slot * kFwdSlot;
-  const float *ml = slot + kAccFloats + w * 128 + lane;
+  const float *ml = slot + kAccFloats + w * 128 + lane, *acc = slot + g * 1024 + (w * 64 + lane) * 4;
   float m = kFloor, l = 0.f;
-  for (int p = 0; p < wk.parts; ++p) m = fmaxf(m, ml[(int64_t)p * kFwdSlot]);
-  f32x16 o[2];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
+  f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+#pragma unroll 4
   for (int p = 0; p < wk.parts; ++p) {
-    const float s = fast_exp2(ml[(int64_t)p * kFwdSlot] - m);
-    l += ml[(int64_t)p * kFwdSlot + 64] * s;
-    add_acc(slot + (int64_t)p * kFwdSlot, o, s, w, lane);
+    const int64_t at = (int64_t)p * kFwdSlot;
+    const float mp = ml[at], lp = ml[at + 64];
+    const f32x4 u = *(const f32x4 *)(acc + at), v = *(const f32x4 *)(acc + at + 512);
+    const float mn = fmaxf(m, mp), x = fast_exp2(m - mn), y = fast_exp2(mp - mn);
+    l = l * x + lp * y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      lo[j] = lo[j] * x + u[j] * y;
+      hi[j] = hi[j] * x + v[j] * y;
+    }
+    m = mn;
   }
-  fwd_store(a, wk.bh, row, min(max(seq_len(a, b) - start, 0), a.Sq), o, m, l, lane);
+  l = add_xor32(l);
+  const bool store = row >= 0 && row < a.Sq, live = row < min(max(seq_len(a, b) - start, 0), a.Sq);
+  bf16_t *O = (bf16_t *)a.Oout.p + b * a.Oout.seq + h * a.Oout.head + (int64_t)row * a.Oout.tok;
+  put_eight(O, g, lo, hi, l == 0.f ? 0.f : 1.f / l, live, store, lane);
+  if (g == 0 && lane < 32 && store)
+    a.lse[(int64_t)wk.bh * a.Sq + row] = live ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -1113,7 +1126,7 @@ hipError_t launch_relpos_fwd(const RelposArgs &a, hipStream_t s) {
   return go(relpos_fwd_kernel, parts_grid(a), a, s);
 }
 hipError_t launch_relpos_fwd_join(const RelposArgs &a, hipStream_t s) {
-  return go(relpos_fwd_join_kernel, join_grid(a), a, s);
+  return go(relpos_fwd_join_kernel, 4 * join_grid(a), a, s);
 }
 hipError_t launch_relpos_decode(const RelposArgs &a, hipStream_t s) {
   const int64_t units = (int64_t)a.nbh * a.pshort, grid = (units + 3) / 4;
