@@ -191,6 +191,9 @@ struct Parts {
     return (int64_t)nbh * ((plong > 1 ? (int64_t)nlong * plong : 0) +
                            (pshort > 1 ? (int64_t)(ntile - nlong) * pshort : 0));
   }
+  // Every launch's workgroups and slots fit 31 bits (a join takes up to eight
+  // workgroups a block).
+  bool fits() const { return workgroups() <= 0x7fffffff / 8; }
   int64_t workgroups() const {
     return (int64_t)nbh * ((int64_t)nlong * plong + (int64_t)(ntile - nlong) * pshort);
   }
@@ -201,7 +204,10 @@ struct Parts {
 
 // Blocks (items) per part of the long lists: 8 x 12 x 4096 with a stripe, lists of
 // 64 in parts of 16 / 12 / 8, backward 377 / 347 / 328 us, forward 133 / 129 / 121.
+// Up to eight workgroups per CU: more long lists than that balance by themselves, and
+// the slots stay below 64 MiB.
 constexpr int kLongItems = 8;
+constexpr int64_t kLongWG = 2048;
 // The other lists are split where their blocks make fewer workgroups than `fill`, in
 // parts of at least `least` items.  Rows (forward and dQ): 512 and 4; 12 heads x
 // 2048, every block kept, 384 workgroups: two parts 35.4 us, three 38.1.  dK and
@@ -221,7 +227,8 @@ Parts choose_parts(int nbh, int ntile, int nlong, int64_t long_items, int64_t it
   p.ntile = ntile;
   if (nlong > 0 && long_items > kShortItems) {
     p.nlong = std::min(nlong, ntile);
-    p.plong = (int)((long_items + kLongItems - 1) / kLongItems);
+    p.plong = (int)std::max<int64_t>(1, std::min((long_items + kLongItems - 1) / kLongItems,
+                                                 kLongWG / ((int64_t)nbh * p.nlong)));
   }
   const int64_t wg = (int64_t)nbh * (ntile - p.nlong);
   if (wg > 0 && wg < s.fill && items > kShortItems)
@@ -425,6 +432,9 @@ pf_status pf_attn_relpos_fwd(const pf_layout *L, const pf_relpos *R, int32_t B, 
       (st = check_rows(V, "V", Skv, false, B, H_kv)) != PF_OK || (st = check_rows(O, "O", Sq, true, B, H)) != PF_OK ||
       (st = need_ptr(lse, "lse")) != PF_OK)
     return st;
+  const bool dec = use_decode(Sq, H, H_kv);
+  const Parts parts = dec ? decode_parts(L, R, B, H_kv) : fwd_parts(L, R, B, H, Sq, q_start != nullptr);
+  if (!parts.fits()) return fail(PF_ERR_UNSUPPORTED, "too many blocks for one launch");
   const size_t need = fwd_slots(L, R, B, H, H_kv, Sq, q_start != nullptr);
   if ((st = need_ws(need, workspace, ws_bytes)) != PF_OK) return st;
   if ((st = check_state(L)) != PF_OK || (st = relpos_state(R)) != PF_OK) return st;
@@ -433,8 +443,7 @@ pf_status pf_attn_relpos_fwd(const pf_layout *L, const pf_relpos *R, int32_t B, 
   a.lse = lse;
   a.slots = (float *)workspace;
   hipStream_t s = (hipStream_t)stream;
-  const bool dec = use_decode(Sq, H, H_kv);
-  (dec ? decode_parts(L, R, B, H_kv) : fwd_parts(L, R, B, H, Sq, q_start != nullptr)).set(a);
+  parts.set(a);
   {
     Timed t(PF_KERNEL_ATTN_FWD, s);
     st = hip_status(dec ? pf::launch_relpos_decode(a, s) : pf::launch_relpos_fwd(a, s),
@@ -464,6 +473,7 @@ pf_status pf_attn_relpos_bwd(const pf_layout *L, const pf_relpos *R, int32_t B, 
       (st = need_ptr(dtable, "dtable")) != PF_OK)
     return st;
   const BwdPlan p = bwd_plan(L, R, B, H, H_kv, S);
+  if (!p.dq.fits() || !p.dkv.fits()) return fail(PF_ERR_UNSUPPORTED, "too many blocks for one launch");
   if ((st = need_ws(p.total, workspace, ws_bytes)) != PF_OK) return st;
   if ((st = check_state(L)) != PF_OK || (st = relpos_state(R)) != PF_OK) return st;
   pf::RelposArgs a = relpos_args(L, R, m, bias, nullptr, kv_len);

@@ -180,16 +180,6 @@ __device__ __forceinline__ void put_acc(float *slot, const f32x16 (&o)[2], int w
     *(f32x4 *)(q + i * 512) = f32x4{o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]};
   }
 }
-__device__ __forceinline__ void add_acc(const float *slot, f32x16 (&o)[2], float scale, int w, int lane) {
-  const float *q = slot + (w * 64 + lane) * 4;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const f32x4 v = *(const f32x4 *)(q + i * 512);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[i >> 2][(i & 3) * 4 + j] += v[j] * scale;
-  }
-}
-
 // First and one past the last position of a row's block list whose column
 // lies in [lo, hi] (columns ascend).
 __device__ __forceinline__ void trim(const int32_t *col, int &p0, int &p1, int lo, int hi) {
@@ -290,6 +280,7 @@ __device__ __forceinline__ void fwd_store(const RelposArgs &a, int bh, int row, 
     a.lse[(int64_t)bh * a.Sq + row] = live ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
+// A workgroup of two waves per 64-row block (or part of its list).
 __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);

@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 
 import numpy as np
 
@@ -75,11 +76,7 @@ class pf_linear_plan(ctypes.Structure):
                                                        ("tn_tile", _i32), ("tn_shared", _i32)]
 
 
-class pf_attn_tensor(ctypes.Structure):
-    _fields_ = [("data", _p), ("seq", _i64), ("head", _i64), ("token", _i64)]
-
-
-_rows_p = ctypes.POINTER(pf_attn_tensor)
+_rows_p = _p  # const pf_attn_tensor *
 
 _SIGS = {
     "pf_layout_create": (_i32, [_i64, _i64, _i32, _i32, ctypes.POINTER(_p)]),
@@ -432,8 +429,9 @@ def pf_attn_workspace_bytes(B, H, S) -> int:
 class Relpos:
     """Owner of a pf_relpos* (destroyed with the object)."""
 
-    def __init__(self, handle: int):
-        self.handle = handle
+    def __init__(self, handle: int, n_buckets: int):
+        self.handle, self.n_buckets = handle, n_buckets
+        self.bias_floats = int(_lib.pf_relpos_bias_floats(handle))  # per head
 
     def __del__(self):
         h, self.handle = getattr(self, "handle", None), None
@@ -449,14 +447,14 @@ def pf_relpos_create(seq: int, n_buckets: int, bucket) -> Relpos:
         raise ValueError(f"bucket shape {m.shape} != ({2 * seq - 1},)")
     h = _p()
     _check(_lib.pf_relpos_create(seq, n_buckets, m.ctypes.data_as(_p), ctypes.byref(h)))
-    return Relpos(h.value)
+    return Relpos(h.value, n_buckets)
 
 
 def pf_relpos_create_log(seq: int, n_buckets: int, max_distance: int, bidirectional: bool) -> Relpos:
     h = _p()
     _check(_lib.pf_relpos_create_log(seq, n_buckets, max_distance, int(bool(bidirectional)),
                                      ctypes.byref(h)))
-    return Relpos(h.value)
+    return Relpos(h.value, n_buckets)
 
 
 def pf_relpos_buckets_get(relpos: Relpos) -> tuple:
@@ -482,24 +480,49 @@ def pf_relpos_bias_floats(relpos: Relpos) -> int:
 
 def pf_relpos_bias(relpos, H, table, bias, stream=None) -> None:
     """table: H x n_buckets float32, bias: H x pf_relpos_bias_floats float32."""
-    _check(_lib.pf_relpos_bias(relpos.handle, H, _ptr(table), _ptr(bias), _stream(stream)))
+    dev, f32 = _device(), torch.float32
+    _check(_lib.pf_relpos_bias(relpos.handle, H, _flat(table, H * relpos.n_buckets, f32, "table", dev),
+                               _flat(bias, H * relpos.bias_floats, f32, "bias", dev), _stream(stream)))
 
 
-def _rows(t, name):
-    """pf_attn_tensor of a (sequences, heads, tokens, 64) bf16 view: any strides
-    but the last, which must be 1."""
-    if t.dim() != 4 or t.dtype != torch.bfloat16 or not t.is_cuda:
-        raise ValueError(f"{name}: expected a 4-d bfloat16 tensor on the GPU")
+# A pf_attn_tensor as bytes: a third of the time a ctypes structure takes.
+_pack_rows = struct.Struct("Pqqq").pack
+
+
+def _rows(t, name, dev):
+    """pf_attn_tensor of a (sequences, heads, tokens, 64) bf16 view on device
+    dev: any strides but the last, which must be 1."""
     s = t.stride()
-    if s[3] != 1 and t.shape[3] != 1:
+    if t.dtype is not torch.bfloat16 or t.get_device() != dev or len(s) != 4:
+        raise ValueError(f"{name}: expected a 4-d bfloat16 tensor on the GPU in use, got {len(s)}-d "
+                         f"{t.dtype} on {t.device}")
+    seq, head, tok, col = s
+    if col != 1 and t.shape[3] != 1:
         raise ValueError(f"{name}: the head dim must be contiguous")
-    return pf_attn_tensor(t.data_ptr(), s[0], s[1], max(s[2], 64) if t.shape[2] == 1 else s[2])
+    if tok < 64 and t.shape[2] == 1:
+        tok = 64
+    return _pack_rows(t.data_ptr(), seq, head, tok)
 
 
-def _like(t, ref, name):
-    if t.shape != ref.shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(ref.shape)}")
-    return _rows(t, name)
+def _flat(t, n, dtype, name, dev):
+    """Address of at least n contiguous elements on device dev; None and
+    integers pass."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name}: expected {n} contiguous {dtype} elements on the GPU in use")
+    return t.data_ptr()
+
+
+def _shapes(want, *pairs):
+    for t, name in pairs:
+        if t.shape != want:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(want)}")
+
+
+def _device():
+    """The current device; -2, which no tensor is on, before the GPU is in use."""
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else -2
 
 
 def pf_attn_relpos_fwd(layout, relpos, scale, Q, K, V, bias, O, lse, q_start=None, kv_len=None,
@@ -507,26 +530,40 @@ def pf_attn_relpos_fwd(layout, relpos, scale, Q, K, V, bias, O, lse, q_start=Non
     """Q, O: (B, H, Sq, 64), K, V: (B, H_kv, Skv, 64) bf16 tensors of any
     strides with a contiguous last dim; bias: of pf_relpos_bias; lse: (B, H, Sq)
     float32, contiguous; q_start, kv_len: B int32 on the GPU, or None."""
-    B, H, Sq, d = Q.shape
-    q, k, v, o = _rows(Q, "Q"), _rows(K, "K"), _like(V, K, "V"), _like(O, Q, "O")
-    if K.shape[0] != B or K.shape[3] != d:
-        raise ValueError(f"K: shape {tuple(K.shape)} does not go with Q's {tuple(Q.shape)}")
-    _check(_lib.pf_attn_relpos_fwd(layout.handle, relpos.handle, B, H, K.shape[1], Sq, K.shape[2], d,
-                                   scale, q, k, v, _ptr(bias), o, _ptr(lse), _ptr(q_start),
-                                   _ptr(kv_len), _ptr(workspace), ws_bytes, _stream(stream)))
+    dev, f32, i32 = _device(), torch.float32, torch.int32
+    q, k, v, o = _rows(Q, "Q", dev), _rows(K, "K", dev), _rows(V, "V", dev), _rows(O, "O", dev)
+    sq, sk = Q.shape, K.shape
+    (B, H, Sq, d), (Bk, Hk, Skv, dk) = sq, sk
+    if Bk != B or dk != d:
+        raise ValueError(f"K: shape {tuple(sk)} does not go with Q's {tuple(sq)}")
+    _shapes(sk, (V, "V"))
+    _shapes(sq, (O, "O"))
+    _check(_lib.pf_attn_relpos_fwd(layout.handle, relpos.handle, B, H, Hk, Sq, Skv, d, scale, q, k, v,
+                                   _flat(bias, H * relpos.bias_floats, f32, "bias", dev), o,
+                                   _flat(lse, B * H * Sq, f32, "lse", dev),
+                                   _flat(q_start, B, i32, "q_start", dev),
+                                   _flat(kv_len, B, i32, "kv_len", dev), _ptr(workspace), ws_bytes,
+                                   _stream(stream)))
 
 
 def pf_attn_relpos_bwd(layout, relpos, scale, Q, K, V, bias, O, lse, dO, dQ, dK, dV, dtable,
                        kv_len=None, workspace=None, ws_bytes=0, stream=None) -> None:
     """As pf_attn_relpos_fwd with Sq = Skv; dtable: (H, n_buckets) float32."""
+    dev, f32 = _device(), torch.float32
+    q, k, v, o = _rows(Q, "Q", dev), _rows(K, "K", dev), _rows(V, "V", dev), _rows(O, "O", dev)
+    g, dq = _rows(dO, "dO", dev), _rows(dQ, "dQ", dev)
+    dk, dv = _rows(dK, "dK", dev), _rows(dV, "dV", dev)
     B, H, S, d = Q.shape
-    q, k, v, o = _rows(Q, "Q"), _rows(K, "K"), _like(V, K, "V"), _like(O, Q, "O")
-    g, dq, dk, dv = _like(dO, Q, "dO"), _like(dQ, Q, "dQ"), _like(dK, K, "dK"), _like(dV, K, "dV")
     if K.shape[0] != B or K.shape[2] != S or K.shape[3] != d:
         raise ValueError(f"K: shape {tuple(K.shape)} does not go with Q's {tuple(Q.shape)}")
+    _shapes(K.shape, (V, "V"), (dK, "dK"), (dV, "dV"))
+    _shapes(Q.shape, (O, "O"), (dO, "dO"), (dQ, "dQ"))
     _check(_lib.pf_attn_relpos_bwd(layout.handle, relpos.handle, B, H, K.shape[1], S, d, scale, q, k, v,
-                                   _ptr(bias), o, _ptr(lse), g, dq, dk, dv, _ptr(dtable),
-                                   _ptr(kv_len), _ptr(workspace), ws_bytes, _stream(stream)))
+                                   _flat(bias, H * relpos.bias_floats, f32, "bias", dev), o,
+                                   _flat(lse, B * H * S, f32, "lse", dev), g, dq, dk, dv,
+                                   _flat(dtable, H * relpos.n_buckets, f32, "dtable", dev),
+                                   _flat(kv_len, B, torch.int32, "kv_len", dev), _ptr(workspace),
+                                   ws_bytes, _stream(stream)))
 
 
 def pf_attn_relpos_workspace_bytes(layout, relpos, B, H, Sq) -> int:

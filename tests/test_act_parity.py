@@ -129,6 +129,8 @@ SHAPES = [
     ("bf16", 1000, 1024, 4096, 64, 16, 128), ("bf16", 2100, 1024, 4096, 64, 16, 0),
     ("bf16", 4100, 4096, 1024, 64, 16, 128), ("bf16", 2509, 2048, 8192, 32, 32, 64),
     ("bf16", 2049, 1024, 4096, 128, 8, 256), ("bf16", 8200, 512, 512, 128, 2, 128),
+    # Output tiles that are not full: 13 and 37 block rows.
+    ("bf16", 3000, 512, 832, 64, 4, 64), ("bf16", 2100, 512, 1184, 32, 4, 32),
 ]
 
 

@@ -449,3 +449,39 @@ def test_repeat_streams_graph():
             want = (oo, ll, *c.bwd(oo, ll))
         for x, y in zip(bufs, want):
             assert t.equal(x, y), i
+
+
+def test_binding_checks_tensors():
+    c = _case(1, 2, 2, 64, "log", 1)
+    t, o = c.t, c.q.clone()
+    lse = t.empty((1, 2, 64), device="cuda")
+    call = lambda **k: c.pf.pf_attn_relpos_fwd(c.L, c.R, c.scale, k.get("q", c.q), k.get("k", c.k), c.v,
+                                               k.get("bias", c.bias), o, k.get("lse", lse), k.get("st"), k.get("n"))
+    call()
+    for k, bad in (("q", c.q.float()), ("k", c.k[:, :, :32]), ("bias", c.bias[:1]), ("bias", c.bias.double()),
+                   ("lse", lse[:, :1]), ("st", t.zeros(1, dtype=t.int64, device="cuda")),
+                   ("n", t.zeros(1, dtype=t.int32)), ("n", t.zeros(0, dtype=t.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            call(**{k: bad})
+    with pytest.raises(ValueError, match="contiguous"):
+        call(q=c.q.transpose(2, 3))
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each: the bits of the calls one by one."""
+    a, b = _case(2, 4, 2, 500, "log", 4, lens=[500, 300]), _case(1, 4, 1, 1411, "clipc", 0, [1300], True)
+    t = a.t
+    want = []
+    for c in (a, b):
+        o, lse = c.fwd()
+        want.append((o, lse, *c.bwd(o, lse)))
+    t.cuda.synchronize()
+    streams, got = [t.cuda.Stream(), t.cuda.Stream()], [None, None]
+    for _ in range(3):
+        for i, c in enumerate((a, b)):
+            with t.cuda.stream(streams[i]):
+                o, lse = c.fwd()
+                got[i] = (o, lse, *c.bwd(o, lse))
+        t.cuda.synchronize()
+        for x, y in zip(want[0] + want[1], got[0] + got[1]):
+            assert t.equal(x, y)
