@@ -322,7 +322,8 @@ pf_status pf_linear_fwd(const pf_layout *layout, pf_dtype dtype, int64_t T,
 /* Activations of pf_linear_fwd_act; s(y) = 1 / (1 + exp(-y)). */
 typedef enum {
   PF_ACT_NONE = 0,
-  PF_ACT_GELU = 1,      /* exact (erf) GELU, as PF_EPI_GELU                       */
+  PF_ACT_GELU = 1,      /* exact (erf) GELU, z Phi(z); bf16: within 3e-5 of it
+                           before rounding                                        */
   PF_ACT_GELU_TANH = 2, /* z s(2 sqrt(2 / pi) (z + 0.044715 z^3)): the tanh form  */
   PF_ACT_SILU = 3,      /* z s(z)                                                 */
   PF_ACT_RELU = 4

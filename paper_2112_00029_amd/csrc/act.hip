@@ -1,13 +1,19 @@
 // Backward of the layer's epilogue: dY_pre = dY o act'(Y_pre) and the bias
 // gradient, its column sums, in one pass over T x N.
 //
-// HBM-bound: every element is read twice and written once (read once for
-// PF_ACT_NONE) with ten to thirty VALU instructions on it.  A thread owns one
-// 16-byte column chunk and walks down the rows of its workgroup's part, eight
-// fp32 sums (four for fp32 data) in registers; a workgroup is `cw` chunks wide and
-// 256 / cw rows tall, its rows' sums are added through LDS in row order, and
-// the parts of the token range leave one fp32 row of N sums each, which a second
-// launch adds in part order.  Deterministic: no atomics.
+// Every element is read twice and written once (read once for PF_ACT_NONE) with
+// ten to thirty VALU instructions on it.  A thread owns one 16-byte column chunk and
+// walks down the rows of its workgroup's part, eight fp32 sums (four for fp32 data) in
+// registers; a workgroup is `cw` chunks wide and 256 / cw rows tall, its rows' sums are
+// added through LDS in row order, and the parts of the token range leave one fp32 row
+// of N sums each, which a second launch adds in part order.  Deterministic: no
+// atomics.  16384 x 16384 GELU: 309 us, 5.2 TB/s (a large copy: 4.86), bound by
+// memory; 2100 x 4096: 10.7 + 3.9 us, one round of workgroups and a second launch.
+// Measured and not kept: two rows per step (319 -> 363 us).
+//
+// dY_pre goes past the caches when it is larger than they are (256 MiB): 16384 x 16384
+// 319 -> 309 us, with the backward-data that reads it next 942 -> 936; smaller ones
+// stay for that call (8192 x 4096 both calls 97 us, streamed 101; 2100 x 4096 51, 53).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -34,23 +40,22 @@ __device__ __forceinline__ void get16(const bf16_t *p, float (&v)[8]) {
     v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ void put16(float *p, const float (&v)[4]) {
-  *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
-}
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)lo) |
          ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16);
 }
-__device__ __forceinline__ void put16(bf16_t *p, const float (&v)[8]) {
-  *(u32x4 *)p = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                      pack_bf16x2(v[6], v[7])};
+__device__ __forceinline__ f32x4 words(const float (&v)[4]) { return f32x4{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ u32x4 words(const float (&v)[8]) {
+  return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+               pack_bf16x2(v[6], v[7])};
 }
 __device__ __forceinline__ void put1(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put1(bf16_t *p, float v) {
   *p = __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-template <typename T>
+// STREAM: a variant, not a branch, whose two stores the compiler would join.
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
   constexpr int V = 16 / sizeof(T);
   __shared__ float red[256 * V];
@@ -73,7 +78,10 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
         float z[V];
         get16(Z + t * a.N, z);
         act_grad_apply<T>(a.act, d, z);
-        put16(dZ + t * a.N, d);
+        const auto x = words(d);
+        auto *p = (decltype(words(d)) *)(dZ + t * a.N);
+        if constexpr (STREAM) __builtin_nontemporal_store(x, p);
+        else *p = x;
       }
 #pragma unroll
       for (int e = 0; e < V; ++e) sum[e] += d[e];
@@ -116,8 +124,9 @@ __global__ __launch_bounds__(256) void act_dbias_kernel(const float *P, int npar
 hipError_t launch_act_bwd(int dtype, const ActBwdArgs &a, hipStream_t s) {
   const int64_t grid = (int64_t)a.groups * a.nparts;
   if (grid <= 0 || grid > 0x7fffffff || a.cw < 1 || a.cw > 64 || 256 % a.cw) return hipErrorInvalidValue;
-  if (dtype == 0) launch_kernel(act_bwd_kernel<bf16_t>, dim3((unsigned)grid), dim3(256), s, a);
-  else launch_kernel(act_bwd_kernel<float>, dim3((unsigned)grid), dim3(256), s, a);
+  auto go = [&](auto kernel) { launch_kernel(kernel, dim3((unsigned)grid), dim3(256), s, a); };
+  if (dtype == 0) a.stream ? go(act_bwd_kernel<bf16_t, true>) : go(act_bwd_kernel<bf16_t, false>);
+  else a.stream ? go(act_bwd_kernel<float, true>) : go(act_bwd_kernel<float, false>);
   return hipGetLastError();
 }
 

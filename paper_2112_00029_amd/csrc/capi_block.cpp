@@ -79,6 +79,7 @@ pf_status pf_linear_act_bwd(pf_dtype dtype, int64_t T, int64_t N, pf_activation 
   a.partials = need ? (float *)workspace : nullptr;
   a.T = T; a.N = N; a.rows_per_part = p.rows;
   a.act = (int)act; a.cw = p.cw; a.groups = p.groups; a.nparts = p.nparts;
+  a.stream = T * N * (dtype == PF_BF16 ? 2 : 4) >= (int64_t)256 << 20;
   {
     Timed t(PF_KERNEL_GELU_BWD, s);
     if ((st = hip_status(pf::launch_act_bwd((int)dtype, a, s), "activation backward kernel")) != PF_OK)

@@ -15,7 +15,6 @@
 
 #include <hip/hip_runtime.h>
 
-#include "pf_gelu.h"
 #include "pf_internal.h"
 
 namespace pf {
@@ -45,17 +44,12 @@ __device__ __forceinline__ float sigmoid2(float y2) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y2));
 }
 
-// GELU for bf16 results: max(x, 0) - |x| Phi(-|x|), the tail as exp2 of a polynomial:
-// log2 Phi(-a) is smooth, and one of degree 7 (fitted here over a <= 7 to the largest
-// error, its leading coefficient negative: the tail goes on falling beyond) leaves the
-// tail within 1.2e-5 of itself where |gelu| > 1e-10: a three-hundredth of half a bf16
-// step, on either side of zero.  The epilogue has nothing to overlap with, so its
-// instructions are time: 16384 x 4096 -> 16384 with pre-activations 801 us with
-// pf_gelu.h's form (6e-8 of the CDF, 30 issue slots), 771 with a reciprocal and a
-// polynomial of degree 4 (21), 697 - 719 so (15; boxes differ).
-__device__ __forceinline__ float gelu_bf16(float x) {
-  // Keeps a * tail finite (one instruction; fminf quiets NaNs first).
-  const float a = fabsf(__builtin_amdgcn_fmed3f(x, -1e4f, 1e4f));
+// Phi(-a), a >= 0, for bf16 results: the exponential of a polynomial.  log2 Phi(-a)
+// is smooth: one of degree 7 (fitted here over a <= 7 to the largest error, its
+// leading coefficient negative, so that the tail goes on falling beyond) leaves it
+// within 1.2e-5 of itself up to a = 7, a three-hundredth of half a bf16 step; past 7
+// it is below 1.3e-12 and the fit falls faster than it does.
+__device__ __forceinline__ float normal_tail_bf16(float a) {
   float q = -1.58825458e-06f;
   q = __builtin_fmaf(q, a, 5.61542814e-05f);
   q = __builtin_fmaf(q, a, -0.00088322388f);
@@ -64,7 +58,24 @@ __device__ __forceinline__ float gelu_bf16(float x) {
   q = __builtin_fmaf(q, a, -0.458964258f);
   q = __builtin_fmaf(q, a, -1.15103567f);
   q = __builtin_fmaf(q, a, -1.00001395f);
-  return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(q), x < 0.f ? 0.f : x);
+  return __builtin_amdgcn_exp2f(q);
+}
+// GELU for bf16 results: max(x, 0) - |x| Phi(-|x|).  The epilogue has nothing to
+// overlap with, so its instructions are time: 16384 x 4096 -> 16384 with
+// pre-activations 801 us with pf_gelu.h's form (6e-8 of the CDF, 30 issue slots), 771
+// with a reciprocal and a polynomial of degree 4 (21), 697 - 719 so (15; boxes
+// differ).
+__device__ __forceinline__ float gelu_bf16(float x) {
+  // Keeps a * tail finite (one instruction; fminf quiets NaNs first).
+  const float a = fabsf(__builtin_amdgcn_fmed3f(x, -1e4f, 1e4f));
+  return __builtin_fmaf(-a, normal_tail_bf16(a), x < 0.f ? 0.f : x);
+}
+// Its derivative, Phi(x) + x phi(x), within 7e-6: the way back of 16384 x 16384 takes
+// 319 us so (memory), 334 with pf_gelu.h's form (82 % of the issue slots).
+__device__ __forceinline__ float gelu_grad_bf16(float x) {
+  const float tail = normal_tail_bf16(fabsf(x));
+  const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752f);
+  return __builtin_fmaf(x * 0.39894228040143268f, e, x < 0.f ? tail : 1.0f - tail);
 }
 
 template <typename T>
@@ -74,7 +85,7 @@ __device__ __forceinline__ float act_gelu(float x) {
 }
 template <typename T>
 __device__ __forceinline__ float act_gelu_grad(float x) {
-  if constexpr (sizeof(T) == 2) return gelu_grad_fast(x);
+  if constexpr (sizeof(T) == 2) return gelu_grad_bf16(x);
   else {
     const float cdf = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
     return cdf + x * (0.39894228040143268f * expf(-0.5f * x * x));

@@ -315,6 +315,7 @@ struct ActBwdArgs {
   float *partials;
   int64_t T, N, rows_per_part;
   int act, cw, groups, nparts;
+  int stream;  // store dZ past the caches
 };
 hipError_t launch_act_bwd(int dtype, const ActBwdArgs &a, hipStream_t s);
 hipError_t launch_act_dbias(int dtype, const ActBwdArgs &a, hipStream_t s);

@@ -10,11 +10,12 @@
 //  * The bias depends on key - query alone, so a 64 x 64 block needs 127 values
 //    of its head, which relpos_bias_kernel has laid out by distance, in log2 units.
 //    Most blocks lie in one bucket (beyond the largest distance every block
-//    does): there the bias is one scalar, added in the fma that scales the score, at
-//    no cost.  For the others the block's 128-value window goes to LDS as 128 units of
-//    16 bytes, unit W holding values W .. W + 3: a lane's four consecutive keys are
-//    then one aligned ds_read_b128 whatever its row, free of bank conflicts, and the
-//    eight reads of a block differ by immediates.
+//    does): there the bias is one scalar, added in the fma that scales the score
+//    (dK/dV: taken off the row's log-sum), at no cost.  For the others ("mixed") the
+//    block's 128-value window goes to LDS as 128 units of 16 bytes, unit W holding
+//    values W .. W + 3: a lane's four consecutive keys are then one aligned
+//    ds_read_b128 whatever its row, free of bank conflicts, and the eight reads of a
+//    block differ by immediates.
 //  * A pair whose bucket is -1 has bias -inf: probability 0.  Blocks wholly
 //    outside the attended distances, and key blocks past a sequence's length, are
 //    cut off a row's block list before the loop; the running maximum starts at a
@@ -30,6 +31,24 @@
 //    VALU instructions per 64 scores and no LDS.  The diagonals then go to the
 //    plan's order by bucket and a segmented scan over the wave leaves one sum per
 //    bucket.  No atomics; every sum has a fixed order.
+//  * Lists of very different length (a stripe's rows and columns; grouped heads; few
+//    blocks of long lists) are shared by several workgroups and joined in order.
+//
+// Rounded to fewer bits: P before P V and P^T dO, dS before its products (bf16, the
+// matrix cores' input; sums and the table gradient take them in fp32), and the
+// outputs.
+//
+// 8 x 12 x 4096, 7 blocks per row, 3 of them mixed (without a bias, attn_kernels.hip,
+// same box): forward 72 (65) us, VALU 51 % of cycles, MFMA 24 %, LDS 15 %; dQ with the
+// table gradient 121 - 126 (97), VALU 51 / MFMA 24 / LDS 17 %, three waves per SIMD
+// where 24 KiB of LDS and 150 registers leave room, not four; dK/dV 129 - 135 (115),
+// VALU 41 / MFMA 30 / LDS 24 %.  Like those kernels they are bound by the serial S ->
+// softmax -> product chain of few waves and the vector unit's part of it.
+// Measured and not kept: mixed scores that start at their bias in the accumulator, with
+// every block on one path (forward 78 at three waves, dQ 124 - 129 against 119 - 122;
+// dK/dV keeps it: 135 -> 128); a loop body per kind of block (51 - 61 registers
+// spilled); one window instead of two for the forward (76 us); the lane offsets of the
+// copies kept over the loop (24 registers spilled, 90 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -107,8 +126,8 @@ __device__ __forceinline__ void put_row(bf16_t *dst, const f32x16 (&o)[2], float
   for (int g = 0; g < 4; ++g) {
     const f32x16 &v = o[g >> 1];
     const int e = 8 * (g & 1);
-    put_eight(dst, g, f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}, f32x4{v[e + 4], v[e + 5], v[e + 6], v[e + 7]},
-              scale, live, store, lane);
+    put_eight(dst, g, f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]},
+              f32x4{v[e + 4], v[e + 5], v[e + 6], v[e + 7]}, scale, live, store, lane);
   }
 }
 
@@ -480,6 +499,9 @@ __global__ __launch_bounds__(128) void relpos_fwd_join_kernel(RelposArgs a) {
 // a (sequence, key/value head)'s block list, with tiles of its own; four of them
 // share a workgroup.  The rows differ in head and agree in position: each lane
 // reads its head's bias of its keys from memory (256 bytes a head and block).
+// 16 sequences of up to 4096 keys, 16 query on 4 key/value heads: 12.5 us (40 MB, 3.2
+// TB/s) and 4.1 for the join; on the kernel above, a wave's 64 rows nearly empty and
+// every key read four times, 67 us.  Bound by the latency of a wave's four blocks.
 __global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -514,7 +536,8 @@ __global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
     cp.init(lane, 0);
     // Bias of this lane's head (rows past G read 0), from key 0's distance on.
     const rsrc_t rb = make_rsrc(a.bias + (int64_t)hk * a.G * a.bias_ld, (int64_t)a.G * a.bias_ld * 4);
-    const uint32_t boff = (uint32_t)r * (uint32_t)(a.bias_ld * 4) + (uint32_t)(a.seq - pos + (lane >> 5) * 4) * 4u;
+    const uint32_t boff =
+        (uint32_t)r * (uint32_t)(a.bias_ld * 4) + (uint32_t)(a.seq - pos + (lane >> 5) * 4) * 4u;
     int col = ld_meta(a.col_idx + p0);
     cp.issue<8>(rk, (uint32_t)(col * BQ) * krb, krb, ks);
     bf16x8 qf[4];
@@ -613,8 +636,8 @@ __global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
     return;
   }
   l_run = add_xor32(l_run);
-  put_row((bf16_t *)a.Oout.p + b * a.Oout.seq + h * a.Oout.head, o, l_run == 0.f ? 0.f : 1.f / l_run, live, mine,
-          lane);
+  put_row((bf16_t *)a.Oout.p + b * a.Oout.seq + h * a.Oout.head, o, l_run == 0.f ? 0.f : 1.f / l_run,
+          live, mine, lane);
   if (lane < 32 && mine)
     a.lse[(int64_t)b * a.H + h] = live ? (m_run + __log2f(l_run)) * kLn2 : -INFINITY;
 }
