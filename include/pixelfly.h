@@ -327,6 +327,8 @@ typedef enum {
   PF_ACT_GELU_TANH = 2, /* z s(2 sqrt(2 / pi) (z + 0.044715 z^3)): the tanh form  */
   PF_ACT_SILU = 3,      /* z s(z)                                                 */
   PF_ACT_RELU = 4
+  /* z finite: at an infinity, where a formula has inf 0, the value or its
+     derivative may be NaN. */
 } pf_activation;
 
 /*
@@ -544,7 +546,10 @@ pf_status pf_relpos_bias(const pf_relpos *relpos, int32_t H, const float *table,
 
 /* Rows of 64 contiguous bf16 elements: sequence, head and token strides in
  * elements (multiples of 8; token stride 64 or more).  Sequences or heads of an
- * input may share memory (stride 0), those of an output may not. */
+ * input may share memory (stride 0).  No two rows of an output may: taken by
+ * ascending stride, tokens, heads and sequences each step past all that the
+ * smaller ones cover (INVALID_ARG otherwise).  Outputs overlap no input and no
+ * other output. */
 typedef struct {
   void *data;
   int64_t seq, head, token;

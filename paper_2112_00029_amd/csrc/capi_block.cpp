@@ -130,8 +130,21 @@ pf_status check_rows(const pf_attn_tensor *t, const char *name, int64_t rows, bo
     return fail(PF_ERR_INVALID_ARG, n + ": token stride below 64, or a negative stride");
   if (t->token > kMaxToken || (rows + 64) * t->token * 2 > 0x7fffffff)
     return fail(PF_ERR_UNSUPPORTED, n + ": a head's rows of one sequence span 2^31 bytes or more");
-  if (out && ((B > 1 && t->seq < 64) || (heads > 1 && t->head < 64)))
-    return fail(PF_ERR_INVALID_ARG, n + " is written: its sequences and heads must not overlap");
+  if (out) {
+    // Rows of different tokens, heads or sequences must not meet: by ascending
+    // stride, each dimension steps past all that the smaller ones cover.
+    struct Dim {
+      int64_t stride, n;
+    } dim[3] = {{t->token, rows}, {t->head, heads}, {t->seq, B}};
+    std::sort(dim, dim + 3, [](const Dim &x, const Dim &y) { return x.stride < y.stride; });
+    __int128 span = 64;
+    for (const Dim &x : dim) {
+      if (x.n == 1) continue;
+      if (x.stride < span)
+        return fail(PF_ERR_INVALID_ARG, n + " is written: its tokens, heads and sequences must not overlap");
+      span += (__int128)x.stride * (x.n - 1);
+    }
+  }
   return PF_OK;
 }
 
@@ -409,7 +422,7 @@ pf_status pf_relpos_bias(const pf_relpos *R, int32_t H, const float *table, floa
 }
 
 size_t pf_attn_relpos_workspace_bytes(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t Sq) {
-  if (!L || !R || B < 1 || H < 1 || Sq < 1 || Sq > R->seq || L->n_out != R->seq || L->n_in != R->seq ||
+  if (!L || !R || B < 1 || H < 1 || H > 65535 || Sq < 1 || Sq > R->seq || L->n_out != R->seq || L->n_in != R->seq ||
       (int64_t)B * H > 0x7fffffff / (R->nb + 1))
     return 0;
   // For every number of key/value heads, and either form of the forward.

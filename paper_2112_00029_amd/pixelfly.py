@@ -499,7 +499,13 @@ def _rows(t, name, dev):
     seq, head, tok, col = s
     if col != 1 and t.shape[3] != 1:
         raise ValueError(f"{name}: the head dim must be contiguous")
-    if tok < 64 and t.shape[2] == 1:
+    # Strides of one sequence, head or token are never used: any will do.
+    B, H, n, _ = t.shape
+    if B == 1:
+        seq = 0
+    if H == 1:
+        head = 0
+    if n == 1:
         tok = 64
     return _pack_rows(t.data_ptr(), seq, head, tok)
 

@@ -189,6 +189,28 @@ def test_attention_outputs_may_not_overlap(attn):
             assert attn.bwd(**{g: attn.rows(**{n: 0})}) == -1 and "overlap" in pf.pf_last_error()
 
 
+@pytest.mark.parametrize("kw", [dict(head=64), dict(head=249 * 64), dict(seq=64), dict(token=128, head=64),
+                                dict(token=4 * 64, head=64, seq=249 * 4 * 64), dict(seq=3 * 256 * 64)])
+def test_attention_output_rows_may_not_meet(attn, kw):
+    for n in ("O", "dQ"):
+        call = attn.fwd if n == "O" else attn.bwd
+        assert call(**{n: attn.rows(**kw)}) == -1 and "overlap" in pf.pf_last_error()
+    assert attn.fwd(Q=attn.rows(**kw)) == pf.PF_ERR_STATE
+
+
+@pytest.mark.parametrize("kw", [dict(head=250 * 64), dict(token=4 * 64, head=64, seq=250 * 4 * 64),
+                                dict(token=24 * 64, head=128, seq=250 * 24 * 64), dict(seq=64, head=128, token=512),
+                                dict(seq=1 << 62)])
+def test_attention_output_orders(attn, kw):
+    assert attn.fwd(O=attn.rows(**kw)) == pf.PF_ERR_STATE
+    assert attn.bwd(dQ=attn.rows(**kw)) == pf.PF_ERR_STATE
+
+
+def test_attention_workspace_of_refused_heads(attn):
+    assert pf.pf_attn_relpos_workspace_bytes(attn.L, attn.R, 1, 65535, 64) > 0
+    assert pf.pf_attn_relpos_workspace_bytes(attn.L, attn.R, 1, 65536, 64) == 0
+
+
 def test_attention_sizes_layouts_workspace(attn):
     for kw in (dict(Sq=0), dict(Sq=257), dict(Skv=0), dict(Skv=300)):
         assert attn.fwd(**kw) == -1 and "Sq and Skv" in pf.pf_last_error()

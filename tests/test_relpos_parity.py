@@ -340,6 +340,18 @@ def test_strides_of_one_projection():
     assert (grad[:, S:] == 7).all() and (grad[:, :, H + 2 * Hk:] == 7).all()
 
 
+def test_strides_of_single_dimensions():
+    """Strides of a dimension of one (any number, as views have them) do not
+    matter."""
+    c = _case(1, 1, 1, 1, "log", 0)
+    odd = lambda x: c.t.as_strided(x, (1, 1, 1, D), (3, 5, 7, 1))
+    o, lse = c.fwd()
+    o2 = c.t.empty_like(o)
+    c.q, c.k, c.v = odd(c.q), odd(c.k), odd(c.v)
+    _, lse2 = c.fwd(o=odd(o2))
+    assert c.t.equal(o, o2) and c.t.equal(lse, lse2)
+
+
 def test_broadcast_keys_and_values():
     """One sequence's keys and values for the whole batch (stride 0)."""
     c = _case(3, 2, 2, 200, "log", 0)
