@@ -1049,7 +1049,11 @@ struct FwdEpi {
   int act;
   const void *residual;
 };
-FwdEpi plain_epi(pf_epilogue epi) { return FwdEpi{(int)epi, nullptr, pf::kActNone, nullptr}; }
+// (-1, refused by check_fwd_epi: no pf_epilogue; kEpiAct is none either.)
+FwdEpi plain_epi(pf_epilogue epi) {
+  const bool known = epi == PF_EPI_NONE || epi == PF_EPI_GELU;
+  return FwdEpi{known ? (int)epi : -1, nullptr, pf::kActNone, nullptr};
+}
 
 pf_status check_fwd_epi(const FwdEpi &e, const void *Y_pre) {
   pf_status st;
@@ -1061,7 +1065,7 @@ pf_status check_fwd_epi(const FwdEpi &e, const void *Y_pre) {
       return fail(PF_ERR_INVALID_ARG, "Y_pre given without an activation");
     return Y_pre ? need_ptr(Y_pre, "Y_pre") : PF_OK;
   }
-  if (e.epi != PF_EPI_NONE && e.epi != PF_EPI_GELU) return fail(PF_ERR_INVALID_ARG, "bad epilogue");
+  if (e.epi < 0) return fail(PF_ERR_INVALID_ARG, "bad epilogue");
   if (e.epi == PF_EPI_GELU && (st = need_ptr(Y_pre, "Y_pre")) != PF_OK) return st;
   if (e.epi == PF_EPI_NONE && Y_pre) return fail(PF_ERR_INVALID_ARG, "Y_pre given without GELU epilogue");
   return PF_OK;

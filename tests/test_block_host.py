@@ -45,6 +45,16 @@ def test_forward_state_and_gamma(layout):
     _refused(pf.PF_ERR_INVALID_ARG, "gamma", pf.pf_linear_fwd_act_mixed, *a[:4], float("nan"), *a[4:])
 
 
+@pytest.mark.parametrize("epi", [-1, 2, 3])
+def test_other_epilogues_of_the_plain_forward(layout, epi):
+    a = (layout, "bf16", 8, 64)
+    b = (A, A, A, A, A, A, epi)
+    for y_pre in (None, A):
+        _refused(pf.PF_ERR_INVALID_ARG, "bad epilogue", pf.pf_linear_fwd, *a, *b, y_pre)
+        _refused(pf.PF_ERR_INVALID_ARG, "bad epilogue", pf.pf_linear_fwd_mixed, *a, 0.5, *b, y_pre)
+        _refused(pf.PF_ERR_INVALID_ARG, "bad epilogue", pf.pf_linear_bwd_data, *a, A, A, A, A, A, A, epi, y_pre)
+
+
 def _bwd(**kw):
     d = dict(dtype="bf16", T=64, N=512, act=pf.PF_ACT_SILU, dY=A, Y_pre=A, dY_pre=A, dbias=A, workspace=A,
              ws_bytes=1 << 30)
