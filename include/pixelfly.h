@@ -650,7 +650,7 @@ typedef enum {
   PF_KERNEL_GELU_BWD = 6,       /* standalone GELU backward, pf_linear_act_bwd */
   PF_KERNEL_ATTN_FWD = 7,
   PF_KERNEL_ATTN_BWD_DQ = 8,    /* dQ (and the row terms delta) */
-  PF_KERNEL_ATTN_BWD_DKV = 9,   /* dK, dV */
+  PF_KERNEL_ATTN_BWD_DKV = 9,   /* dK, dV (and the sums of dtable) */
   PF_KERNEL_DENSE = 10,         /* dense comparator GEMM */
   PF_KERNEL_BUTTERFLY = 11,     /* product-form butterfly (forward, backward-data) */
   PF_KERNEL_COUNT = 12

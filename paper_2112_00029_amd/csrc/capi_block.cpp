@@ -505,9 +505,13 @@ pf_status pf_attn_relpos_bwd(const pf_layout *L, const pf_relpos *R, int32_t B, 
   };
   p.dq.set(a);
   run(PF_KERNEL_ATTN_BWD_DQ, "attention dQ kernel", [&] { return pf::launch_relpos_bwd_dq(a, s); });
-  run(PF_KERNEL_REDUCE, "table gradient sum", [&] { return pf::launch_relpos_dtable(a, dtable, s); });
   if (p.dq.slots())
     run(PF_KERNEL_REDUCE, "dQ join", [&] { return pf::launch_relpos_bwd_join(false, a, s); });
+  // The dQ launch's partials: whole rounds of the 8 XCDs.
+  a.dtable = dtable;
+  a.tab_wg = (H * ((R->n_buckets + pf::kRelposTabCols - 1) / pf::kRelposTabCols) + 7) / 8 * 8;
+  a.tab_nl = p.dq.nlong * p.dq.plong;
+  a.tab_ns = (p.dq.ntile - p.dq.nlong) * p.dq.pshort;
   p.dkv.set(a);
   run(PF_KERNEL_ATTN_BWD_DKV, "attention dK/dV kernel", [&] { return pf::launch_relpos_bwd_dkv(a, s); });
   if (p.dkv.slots())

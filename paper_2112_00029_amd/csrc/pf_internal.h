@@ -337,6 +337,7 @@ constexpr int kRelposMaxBuckets = 256;
 // distances 2 l and 2 l + 1 of the block's 128 (key - query + 64) in ascending
 // order of bucket: position, position << 8, bucket << 16, bucket << 24.
 constexpr int kRelposMixed = 256;
+constexpr int kRelposTabCols = 16;  // buckets per workgroup of the table gradient
 struct RelposArgs {
   RowView Q, K, V, O, dO;
   RowViewOut Oout, dQ, dK, dV;
@@ -346,6 +347,9 @@ struct RelposArgs {
   const float *lse_in;
   float *delta;          // [B][H][Sq]
   float *partials;       // a row of nbucket sums per workgroup of the dQ launch
+  float *dtable;         // [H][nbucket]; the dK/dV launch's first tab_wg workgroups (a multiple
+                         // of 8) write it from the partials: tab_nl and tab_ns rows per
+                         // sequence and head
   float *slots;          // partial results of blocks in several parts
   const int32_t *q_start, *kv_len;  // [B] or null
   const int32_t *info;
@@ -357,6 +361,7 @@ struct RelposArgs {
   int ntile;             // 64-row tiles per sequence and head of the launch
   int nlong, plong, pshort;  // the first nlong of them in plong parts, the others in pshort
   int nbucket;
+  int tab_wg, tab_nl, tab_ns;
   int omin, omax;        // block offsets (key - query) that hold an attended distance
   float scale;
 };
@@ -380,7 +385,6 @@ hipError_t launch_relpos_fwd_join(const RelposArgs &a, hipStream_t s);
 hipError_t launch_relpos_bwd_dq(const RelposArgs &a, hipStream_t s);
 hipError_t launch_relpos_bwd_dkv(const RelposArgs &a, hipStream_t s);
 hipError_t launch_relpos_bwd_join(bool kv, const RelposArgs &a, hipStream_t s);
-hipError_t launch_relpos_dtable(const RelposArgs &a, float *dtable, hipStream_t s);
 
 // The allocation-free attention backward keeps its row terms in a
 // file-scope device array of kAttnScratchRows floats (16 MiB per GPU);

@@ -900,6 +900,36 @@ __global__ __launch_bounds__(128, 3) void relpos_bwd_dq_kernel(RelposArgs a) {
 // Backward, pass 2: dK and dV (a key block of one key/value head; its G query
 // heads and their kept query blocks one after another)
 // ---------------------------------------------------------------------------
+// dtable[h][c]: the dQ launch's partials, one row of nbucket sums per workgroup,
+// added over sequences, block rows and parts in a fixed order: a head's rows are
+// tab_nl consecutive ones per sequence among the long blocks', then tab_ns among the
+// others'.  A workgroup takes kRelposTabCols buckets of a head, eight threads a bucket.
+__device__ __forceinline__ void table_sums(const RelposArgs &a, int t, float *red) {
+  constexpr int C = kRelposTabCols, PARTS = 128 / C;
+  const int nb = a.nbucket, nc = (nb + C - 1) / C, h = t / nc;
+  if (h >= a.H) return;
+  const int cc = threadIdx.x % C, part = threadIdx.x / C, c = t % nc * C + cc;
+  float s = 0.f;
+  auto add = [&](const float *p, int n) {  // n rows per sequence
+    const int total = a.B * n;
+#pragma unroll 8
+    for (int i = part; i < total; i += PARTS) {
+      const int b = i / n, r = i - b * n;
+      s += p[(((int64_t)b * a.H + h) * n + r) * nb];
+    }
+  };
+  if (c < nb) {
+    add(a.partials + c, a.tab_nl);
+    add(a.partials + (int64_t)a.B * a.H * a.tab_nl * nb + c, a.tab_ns);
+  }
+  red[threadIdx.x] = s;
+  __syncthreads();
+  if (part || c >= nb) return;
+#pragma unroll
+  for (int p = 1; p < PARTS; ++p) s += red[p * C + cc];
+  a.dtable[(int64_t)h * nb + c] = s;
+}
+
 __global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -910,7 +940,13 @@ __global__ __launch_bounds__(128, 2) void relpos_bwd_dkv_kernel(RelposArgs a) {
   // bucket), then -delta.
   __shared__ __attribute__((aligned(16))) float rt0[2 * BQ], rt1[2 * BQ];
 
-  const Work wk = find_work(a, xcd_remap(blockIdx.x, gridDim.x));
+  // The first workgroups add up the table gradient, beside the others' work (in a
+  // launch of its own: 4 x 16 x 1511 both passes 65.3 -> 62.5 us without it).
+  if ((int)blockIdx.x < a.tab_wg) {
+    table_sums(a, blockIdx.x, rt0);
+    return;
+  }
+  const Work wk = find_work(a, xcd_remap(blockIdx.x - a.tab_wg, gridDim.x - a.tab_wg));
   const int kb = wk.blk, b = wk.bh / a.Hkv, hk = wk.bh % a.Hkv;
   const int len = seq_len(a, b);
   const int key = kb * BQ + w * 32 + (lane & 31);
@@ -1078,7 +1114,7 @@ __global__ __launch_bounds__(128) void relpos_bwd_join_kernel(RelposArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// The bias by distance, and the sum of the table gradient's partials
+// The bias by distance
 // ---------------------------------------------------------------------------
 // out[h][d + seq] = log2(e) table[h][bucket(d)], -inf where the bucket is -1; then
 // the same by descending distance, out[h][2 seq + f] = out[h][2 seq - f] (distance
@@ -1091,32 +1127,6 @@ __global__ __launch_bounds__(256) void relpos_bias_kernel(RelposBiasArgs a) {
   float *o = a.out + (int64_t)h * 4 * a.seq;
   o[e] = v;
   o[2 * (int64_t)a.seq + (e ? 2 * a.seq - e : 0)] = v;
-}
-
-// dtable[h][c]: the dQ launch's partials, one row of nbucket sums per
-// workgroup, added over sequences, block rows and parts in a fixed order: a head's
-// rows are `nl` consecutive ones per sequence among the long blocks', then ns
-// among the others'.  A workgroup takes 32 buckets of a head, 32 threads a bucket.
-__global__ __launch_bounds__(1024) void relpos_dtable_kernel(const float *P, int B, int H, int nl, int ns,
-                                                             int nbucket, float *dtable) {
-  __shared__ float red[1024];
-  const int cc = threadIdx.x & 31, part = threadIdx.x >> 5;
-  const int c = blockIdx.x * 32 + cc, h = blockIdx.y;
-  float s = 0.f;
-  if (c < nbucket)
-    for (int b = 0; b < B; ++b) {
-      const int64_t bh = (int64_t)b * H + h;
-      const float *p = P + bh * nl * nbucket + c;
-      for (int r = part; r < nl; r += 32) s += p[(int64_t)r * nbucket];
-      p = P + ((int64_t)B * H * nl + bh * ns) * nbucket + c;
-#pragma unroll 4
-      for (int r = part; r < ns; r += 32) s += p[(int64_t)r * nbucket];
-    }
-  red[threadIdx.x] = s;
-  __syncthreads();
-  if (part || c >= nbucket) return;
-  for (int p = 1; p < 32; ++p) s += red[p * 32 + cc];
-  dtable[(int64_t)h * nbucket + c] = s;
 }
 
 }  // namespace
@@ -1156,18 +1166,11 @@ hipError_t launch_relpos_bwd_dq(const RelposArgs &a, hipStream_t s) {
   return go(relpos_bwd_dq_kernel, parts_grid(a), a, s);
 }
 hipError_t launch_relpos_bwd_dkv(const RelposArgs &a, hipStream_t s) {
-  return go(relpos_bwd_dkv_kernel, parts_grid(a), a, s);
+  return go(relpos_bwd_dkv_kernel, a.tab_wg + parts_grid(a), a, s);
 }
 hipError_t launch_relpos_bwd_join(bool kv, const RelposArgs &a, hipStream_t s) {
   return kv ? go(relpos_bwd_join_kernel<true>, 8 * join_grid(a), a, s)
             : go(relpos_bwd_join_kernel<false>, 4 * join_grid(a), a, s);
-}
-
-hipError_t launch_relpos_dtable(const RelposArgs &a, float *dtable, hipStream_t s) {
-  launch_kernel(relpos_dtable_kernel, dim3((unsigned)((a.nbucket + 31) / 32), (unsigned)a.H), dim3(1024), s,
-                (const float *)a.partials, a.B, a.H, a.nlong * a.plong, (a.ntile - a.nlong) * a.pshort,
-                a.nbucket, dtable);
-  return hipGetLastError();
 }
 
 hipError_t launch_relpos_bias(const RelposBiasArgs &a, int H, hipStream_t s) {
