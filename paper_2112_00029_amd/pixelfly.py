@@ -153,10 +153,13 @@ def header_functions() -> list[str]:
 
 
 def _ptr(x):
-    if x is None or isinstance(x, int):
+    if x is None or type(x) is int:
         return x
-    if hasattr(x, "data_ptr"):
+    try:
         return x.data_ptr()
+    except AttributeError:
+        if isinstance(x, int):
+            return x
     raise TypeError(f"expected a tensor, int address or None, got {type(x)}")
 
 
@@ -164,6 +167,13 @@ def _ptr(x):
 # call of the smallest products waits for the host: 3.7 -> 0.4 us of 9.1 / 5.7 us
 # for an attention forward of one block).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) if torch else None
+# The same of an initialised runtime's current device (torch.cuda.current_device
+# initialises it first).
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) if torch else None
+
+
+def _current_device() -> int:
+    return _raw_device() if _raw_device is not None else torch.cuda.current_device()
 
 
 def _stream(s):
@@ -172,7 +182,7 @@ def _stream(s):
         if torch is None or not torch.cuda.is_initialized():
             return None
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(s, int):
         return s
@@ -482,7 +492,7 @@ def pf_relpos_bias(relpos, H, table, bias, stream=None) -> None:
     """table: H x n_buckets float32, bias: H x pf_relpos_bias_floats float32."""
     dev, f32 = _device(), torch.float32
     _check(_lib.pf_relpos_bias(relpos.handle, H, _flat(table, H * relpos.n_buckets, f32, "table", dev),
-                               _flat(bias, H * relpos.bias_floats, f32, "bias", dev), _stream(stream)))
+                               _flat(bias, H * relpos.bias_floats, f32, "bias", dev), _stream_on(stream, dev)))
 
 
 # A pf_attn_tensor as bytes: a third of the time a ctypes structure takes.
@@ -499,14 +509,10 @@ def _rows(t, name, dev):
     seq, head, tok, col = s
     if col != 1 and t.shape[3] != 1:
         raise ValueError(f"{name}: the head dim must be contiguous")
-    # Strides of one sequence, head or token are never used: any will do.
-    B, H, n, _ = t.shape
-    if B == 1:
-        seq = 0
-    if H == 1:
-        head = 0
-    if n == 1:
-        tok = 64
+    if (seq | head | tok) & 7 or tok < 64:
+        # Strides of one sequence, head or token are never used: any will do.
+        B, H, n, _ = t.shape
+        seq, head, tok = seq if B > 1 else 0, head if H > 1 else 0, tok if n > 1 else 64
     return _pack_rows(t.data_ptr(), seq, head, tok)
 
 
@@ -528,7 +534,12 @@ def _shapes(want, *pairs):
 
 def _device():
     """The current device; -2, which no tensor is on, before the GPU is in use."""
-    return torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    return _current_device() if torch.cuda.is_initialized() else -2
+
+
+def _stream_on(s, dev):
+    """_stream, with the current device at hand (-2: none)."""
+    return _raw_stream(dev) if s is None and dev >= 0 and _raw_stream is not None else _stream(s)
 
 
 def pf_attn_relpos_fwd(layout, relpos, scale, Q, K, V, bias, O, lse, q_start=None, kv_len=None,
@@ -549,7 +560,7 @@ def pf_attn_relpos_fwd(layout, relpos, scale, Q, K, V, bias, O, lse, q_start=Non
                                    _flat(lse, B * H * Sq, f32, "lse", dev),
                                    _flat(q_start, B, i32, "q_start", dev),
                                    _flat(kv_len, B, i32, "kv_len", dev), _ptr(workspace), ws_bytes,
-                                   _stream(stream)))
+                                   _stream_on(stream, dev)))
 
 
 def pf_attn_relpos_bwd(layout, relpos, scale, Q, K, V, bias, O, lse, dO, dQ, dK, dV, dtable,
@@ -559,17 +570,18 @@ def pf_attn_relpos_bwd(layout, relpos, scale, Q, K, V, bias, O, lse, dO, dQ, dK,
     q, k, v, o = _rows(Q, "Q", dev), _rows(K, "K", dev), _rows(V, "V", dev), _rows(O, "O", dev)
     g, dq = _rows(dO, "dO", dev), _rows(dQ, "dQ", dev)
     dk, dv = _rows(dK, "dK", dev), _rows(dV, "dV", dev)
-    B, H, S, d = Q.shape
-    if K.shape[0] != B or K.shape[2] != S or K.shape[3] != d:
-        raise ValueError(f"K: shape {tuple(K.shape)} does not go with Q's {tuple(Q.shape)}")
-    _shapes(K.shape, (V, "V"), (dK, "dK"), (dV, "dV"))
-    _shapes(Q.shape, (O, "O"), (dO, "dO"), (dQ, "dQ"))
-    _check(_lib.pf_attn_relpos_bwd(layout.handle, relpos.handle, B, H, K.shape[1], S, d, scale, q, k, v,
+    sq, sk = Q.shape, K.shape
+    (B, H, S, d), (Bk, Hk, Sk, d_k) = sq, sk
+    if Bk != B or Sk != S or d_k != d:
+        raise ValueError(f"K: shape {tuple(sk)} does not go with Q's {tuple(sq)}")
+    _shapes(sk, (V, "V"), (dK, "dK"), (dV, "dV"))
+    _shapes(sq, (O, "O"), (dO, "dO"), (dQ, "dQ"))
+    _check(_lib.pf_attn_relpos_bwd(layout.handle, relpos.handle, B, H, Hk, S, d, scale, q, k, v,
                                    _flat(bias, H * relpos.bias_floats, f32, "bias", dev), o,
                                    _flat(lse, B * H * S, f32, "lse", dev), g, dq, dk, dv,
                                    _flat(dtable, H * relpos.n_buckets, f32, "dtable", dev),
                                    _flat(kv_len, B, torch.int32, "kv_len", dev), _ptr(workspace),
-                                   ws_bytes, _stream(stream)))
+                                   ws_bytes, _stream_on(stream, dev)))
 
 
 def pf_attn_relpos_workspace_bytes(layout, relpos, B, H, Sq) -> int:
