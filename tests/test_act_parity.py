@@ -274,6 +274,43 @@ def test_backward_past_the_caches(dtype, T, N):
     assert (bad <= 0).all() and not db.isnan().any(), float(bad.max())
 
 
+def test_outputs_past_2_to_31_elements():
+    """131100 x 16448: the first and last rows forward (in place on the
+    residual) against the formulas, the last rows back against a call of their own."""
+    t = torch_cuda()
+    from paper_2112_00029_amd import pixelfly as pf
+    T, K, N, b, tail = 131100, 128, 16448, 64, 300
+    L = pf.pf_layout_create(N, K, b, 1)
+    pf.pf_layout_upload(L)
+    g = t.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *s: t.randn(s, generator=g, device="cuda", dtype=t.float32).bfloat16()
+    x, w, bias = rnd(T, K), rnd(N // b, b, b).mul_(0.125), rnd(N)
+    y = t.full((T, N), 0.25, dtype=t.bfloat16, device="cuda")
+    z = t.empty((T, N), dtype=t.bfloat16, device="cuda")
+    assert y.numel() > 1 << 31
+    need = pf.pf_workspace_bytes(L, T, 0, "bf16")
+    ws = t.empty((max(need, 256),), dtype=t.uint8, device="cuda")
+    print("[act] forward past 2^31 elements", flush=True)
+    pf.pf_linear_fwd_act(L, "bf16", T, 0, x, w, None, None, bias, pf.PF_ACT_SILU, y, y, z, None, ws, need)
+    # Block row i keeps block column i mod 2 alone.
+    col = (t.arange(N // b, device="cuda") % (K // b))
+    for rows in (slice(0, tail), slice(T - tail, T)):
+        xs = x[rows].double().view(tail, K // b, b)[:, col]
+        exact = (xs[:, :, None, :] * w.double()[None]).sum(-1).view(tail, N) + bias.double()
+        mag = (xs.abs()[:, :, None, :] * w.double().abs()[None]).sum(-1).view(tail, N) + bias.double().abs()
+        tol = 68 * 2.0 ** -24 * mag
+        u = 2.0 ** -8
+        assert ((z[rows].double() - exact).abs() <= u * exact.abs() + (1 + u) * tol).all()
+        out = 0.25 + exact * t.sigmoid(exact)
+        own = 1e-6 * (1 + exact.abs())
+        assert ((y[rows].double() - out).abs() <= u * out.abs() + (1 + u) * (LIP * tol + own)).all()
+    print("[act] back past 2^31 elements", flush=True)
+    keep = z[-tail:].clone()
+    dz, db = _bwd(t, pf, "bf16", T, N, "silu", y, z, alias=z)
+    part, _ = _bwd(t, pf, "bf16", tail, N, "silu", y[-tail:].contiguous(), keep)
+    assert t.equal(dz[-tail:], part)
+
+
 def test_backward_extreme_pre_activations():
     """Far tails of either sign, zeros, the largest finite values: finite
     derivatives with the limits 0 and 1; NaN stays NaN (ReLU: 0)."""

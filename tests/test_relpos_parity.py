@@ -340,6 +340,33 @@ def test_strides_of_one_projection():
     assert (grad[:, S:] == 7).all() and (grad[:, :, H + 2 * Hk:] == 7).all()
 
 
+def test_offsets_past_32_bits():
+    """Sequences 2^32 and heads 2^31 elements apart, of inputs and outputs: the
+    bits of the separate tensors (whole sequences, and one row of each)."""
+    for rows, starts in ((None, None), (1, [269, 99])):
+        c = _case(2, 2, 2, 270, "log", 2, lens=[270, 100], Sq=rows, starts=starts)
+        t = c.t
+        if rows is None:
+            big = t.empty((1 << 32) + (1 << 31) + (1 << 24), dtype=t.bfloat16, device="cuda")
+        n = [0]
+        def far(x):
+            v = t.as_strided(big, tuple(x.shape), (1 << 32, 1 << 31, D, 1), n[0])
+            n[0] += 1 << 20
+            return v.copy_(x)
+        o, lse = c.fwd()
+        nan = t.full_like(o, float("nan"))
+        q, k, v, o2 = far(c.q), far(c.k), far(c.v), far(nan)
+        _, lse2 = c.fwd(q=q, k=k, v=v, o=o2)
+        assert t.equal(o, o2) and t.equal(lse, lse2)
+        if rows is None:
+            grads = c.bwd(o, lse)
+            far_grads = far(nan), far(nan), far(nan), t.empty_like(grads[3])
+            c.pf.pf_attn_relpos_bwd(c.L, c.R, c.scale, q, k, v, c.bias, o2, lse2, far(c.do), *far_grads, c.dlens,
+                                    c.ws, c.wsb)
+            for x, y in zip(grads, far_grads):
+                assert t.equal(x, y)
+
+
 def test_strides_of_single_dimensions():
     """Strides of a dimension of one (any number, as views have them) do not
     matter."""
