@@ -491,7 +491,7 @@ __global__ __launch_bounds__(128) void relpos_fwd_join_kernel(RelposArgs a) {
 // a (sequence, key/value head)'s block list, with tiles of its own; four of them
 // share a workgroup.  The rows differ in head and agree in position: each lane
 // reads its head's bias of its keys from memory (256 bytes a head and block).
-// 16 sequences of up to 4096 keys, 16 query on 4 key/value heads: 12.0 us (40 MB, 3.4
+// 16 sequences of up to 4096 keys, 16 query on 4 key/value heads: 12.4 us (40 MB, 3.3
 // TB/s) and 4.1 for the join; on the kernel above, a wave's 64 rows nearly empty and
 // every key read four times, 67 us.  Bound by the latency of a wave's four blocks.
 __global__ __launch_bounds__(256, 2) void relpos_decode_kernel(RelposArgs a) {
