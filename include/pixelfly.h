@@ -572,6 +572,9 @@ typedef struct {
  * -inf; so do rows at positions past their sequence's tokens.  Memory of tokens
  * past kv_len is not used, whatever it holds.  (A NaN or infinity in an attended
  * block's K or V spreads to rows of that block, masked pairs included.)
+ * Scores are fp32: S is off by at most about 2^-18 (scale sum_d |q_d k_d| + |bias|), and P
+ * by as much of itself.  O and lse are those of the rounded scores, however
+ * large, as long as these are finite and above about -1e30.
  * Needs pf_attn_relpos_workspace_bytes of workspace (0: may be NULL).
  * Errors: INVALID_ARG, UNSUPPORTED, STATE, WORKSPACE, HIP.
  */
@@ -591,7 +594,10 @@ pf_status pf_attn_relpos_fwd(const pf_layout *layout, const pf_relpos *relpos, i
  * dK and dV of a key/value head are sums over its query heads.  dtable: H x
  * n_buckets fp32, written whole (zeros for buckets no pair has).  Gradients of
  * rows past kv_len are zero.  Every sum has a fixed order: repeat calls agree
- * bitwise.  Needs pf_attn_relpos_workspace_bytes(layout, relpos, B, H, S).
+ * bitwise.  P comes from lse, which is rounded itself: beside the scores' error it is off
+ * by at most 20 x 2^-24 |lse| of itself, so the gradients keep bf16's precision up
+ * to |lse| of about 2^10, have no digits left at 2^19 and may be infinite or NaN past
+ * 2^26.  Needs pf_attn_relpos_workspace_bytes(layout, relpos, B, H, S).
  * Errors: INVALID_ARG, UNSUPPORTED, STATE, WORKSPACE, HIP.
  */
 pf_status pf_attn_relpos_bwd(const pf_layout *layout, const pf_relpos *relpos, int32_t B, int32_t H,

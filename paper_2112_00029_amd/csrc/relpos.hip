@@ -60,6 +60,12 @@ namespace {
 
 constexpr int WIN = 128 * 16;        // bytes of a bias window in LDS
 constexpr float kFloor = -1e30f;     // running maximum before any key (log2 units)
+// Running maximum from which the forward rounds a one-bucket block's scores before
+// it takes the maximum off.  Below, one fma does both: the maximum is a rounded
+// score, the fma's own is not, and the largest key's exponent is off zero by up to 2^-24
+// of it: here 2^-12 of a probability, an eighth of its rounding to bf16; at scores of 2^31
+// (where it was measured: NaN, and rows of zeros) past the exponential's range.
+constexpr float kLarge = 4096.f;
 
 // Token rows [0, n) of a head: range-checked, 16 bytes at a time.
 __device__ __forceinline__ rsrc_t rows_rsrc(const bf16_t *p, int n, uint32_t row_bytes) {
@@ -328,6 +334,7 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
   float m_run = kFloor, l_run = 0.f;  // l_run: this lane's keys only
+  bool large = false;  // some row's m_run is beyond kLarge
 
   if (p0 < p1) {
     RowCopy cp;
@@ -396,11 +403,22 @@ __global__ __launch_bounds__(128, 4) void relpos_fwd_kernel(RelposArgs a) {
         const float m_cand = fmaxf(m_run, max_xor32(bm));
         const float alpha = fast_exp2(m_run - m_cand);
         m_run = m_cand;
+        large = __builtin_amdgcn_ballot_w64(fabsf(m_run) > kLarge && m_run > kFloor) != 0;
         l_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+      }
+      // Beyond kLarge the scores are rounded before the maximum is taken off, as
+      // the maximum was.
+      if (large && bb.info < kRelposMixed) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[kt].v[e] = __builtin_fmaf(s[kt].v[e], cm, ca);
+        cm = 1.f;
+        ca = 0.f;
       }
       const float off = ca - m_run;
       float rs = 0.f;
