@@ -1,5 +1,5 @@
 """Position-bias attention over the range of scales that the calls accept, with
-large scores.
+large scores, and its table gradient against differences that can fail.
 
 Tolerances, pair by pair (u = 2^-8, half a step of bf16; e = 2^-24, of fp32; every
 input is exact), in units of the natural score S = scale q.k + bias:
@@ -159,3 +159,68 @@ def test_large_scores(scale, rows):
             want = (top[:, 0] + t.log(num))[some]
             assert ((lse[b, h].double()[some] - want).abs() <= 8 * E32 * want.abs()).all(), (b, h)
             assert (lse[b, h][~some] == -float("inf")).all()
+
+
+def _row_terms(c, h, o):
+    """Head h of sequence 0: P, dP, the exact delta, the kernel's (from its O),
+    pairs, buckets, relative error of P."""
+    t = c.t
+    s, live, cell, hk, n, err = c.pairs(0, h)
+    p = t.nan_to_num(t.softmax(s, -1))
+    do, v = c.do[0, h].double(), c.v[0, hk].double()
+    dp = do @ v.t()
+    return p, dp, (p * dp).sum(-1, keepdim=True), (do * o[0, h].double()).sum(-1, keepdim=True), live, cell, n, err
+
+
+@pytest.mark.parametrize("kind,wide", [("clip", 0), ("clip", 40), ("log", 7), ("log", 15)])
+def test_table_gradient_against_differences(kind, wide):
+    """dtable by central differences of <dO, O> in float64 over the table, at each
+    head's largest entries and at a bucket of many distances, along whose part of O the
+    rows' dO lean, so that its entry is large too.
+
+    delta takes O as it is stored: what its rounding moves dtable by, the sum over rows of
+    P(bucket) (delta - <dO, O stored>), is computed and taken off, so that the bound is the
+    fp32 part alone: P E (|dP| + |delta|), 64 e of the sums in dP and delta, n e of the sum.
+    In one entry x the rows' O is linear in a logistic function of x, whose third
+    derivative is at most its first: differences of step h are off by h^2 / 6 of the rows'
+    absolute terms.  Bound and correction are at most 2 % of every entry checked: a dtable
+    of zeros, one without delta, scaled or of the wrong bucket fails."""
+    m, n = (clip_map(192, 20), 41) if kind == "clip" else (log_map(192, 16, 64, True), 16)
+    c = Scaled(1, 2, 1, 190, m, n, butterfly(3, 4), [177], scale=0.125, seed=2)
+    t = c.t
+    o, lse = c.fwd()
+    for hd in range(2):
+        p, _, _, _, live, cell, _, _ = _row_terms(c, hd, o)
+        v, mine = c.v[0, 0].double(), t.where(live & (cell == wide), p, 0.0)
+        lean = mine @ v / mine.sum(-1, keepdim=True).clamp(min=1e-9) - p @ v
+        c.do[0, hd] += (8 * lean / lean.norm(dim=-1, keepdim=True).clamp(min=1e-9)).bfloat16()
+    _, _, _, dt = c.bwd(o, lse)
+    tab, h = c.table.double(), 1e-3
+    for hd in range(2):
+        p, dp, delta, stored, live, cell, nk, err = _row_terms(c, hd, o)
+        do, v = c.do[0, hd].double(), c.v[0, 0].double()
+
+        def loss():
+            s = c.head(0, hd)[0]
+            return float((t.nan_to_num(t.softmax(s, -1)) @ v * do).sum())
+
+        sums = lambda x: t.zeros(n, dtype=t.float64, device="cuda").index_add_(0, cell[live], x[live])
+        exact = sums(p * (dp - delta))
+        eds = p * (err * (dp.abs() + delta.abs()) + 64 * E32 * (do.abs() @ v.abs().t()
+                                                              + (do.abs() * (p @ v.abs())).sum(-1, keepdim=True)))
+        tol = sums(eds + nk * E32 * (p * (dp - stored)).abs())
+        for cc in {wide, *exact.abs().argsort(descending=True)[:3].tolist()}:
+            vals = []
+            for sg in (1, -1):
+                c.table = tab.clone()
+                c.table[hd, cc] += sg * h
+                vals.append(loss())
+            c.table = tab
+            num = (vals[0] - vals[1]) / (2 * h)
+            mine = t.where(live & (cell == cc), p, 0.0)
+            moved = float((mine * (delta - stored)).sum())
+            bound = float(tol[cc]) + h * h / 6 * 1.01 * float((mine * (dp - delta)).sum(-1).abs().sum())
+            got = float(dt[hd, cc])
+            print(f"  head {hd} bucket {cc}: {got:.6f}, differences {num:.6f}, of the stored O {moved:.6f}, bound {bound:.1e}")
+            assert bound + abs(moved) <= 0.02 * abs(num), (hd, cc)
+            assert abs(got - moved - num) <= bound, (hd, cc, got, moved, num, bound)
