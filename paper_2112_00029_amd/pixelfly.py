@@ -452,7 +452,10 @@ class Relpos:
 def pf_relpos_create(seq: int, n_buckets: int, bucket) -> Relpos:
     """bucket: 2 seq - 1 integers, the bucket of key - query = -(seq - 1) ..
     seq - 1 (-1: not attended)."""
-    m = np.ascontiguousarray(bucket, dtype=np.int32)
+    b = np.asarray(bucket)
+    m = np.ascontiguousarray(b, dtype=np.int32) if b.dtype.kind in "biu" else None
+    if m is None or not np.array_equal(m, b):
+        raise ValueError(f"bucket: expected integers of 32 bits, got {b.dtype}")
     if m.shape != (max(2 * seq - 1, 0),):
         raise ValueError(f"bucket shape {m.shape} != ({2 * seq - 1},)")
     h = _p()
