@@ -10,11 +10,14 @@
 // is needed too, both come from e = exp(-|y|), r = 1 / (1 + e): r and e r, whichever
 // side, so that neither cancels or overflows.
 // bf16 results take the hardware exponential and reciprocal (1 ulp each: far below
-// their own rounding); fp32 results take the library's functions.
+// their own rounding); fp32 results take the library's functions, and for GELU the
+// forms of pf_gelu.h, which keep their digits in the negative tail: x (1 + erf(x / sqrt
+// 2)) / 2 is 4 % off at -5 and zero from -5.6.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
+#include "pf_gelu.h"
 #include "pf_internal.h"
 
 namespace pf {
@@ -81,15 +84,12 @@ __device__ __forceinline__ float gelu_grad_bf16(float x) {
 template <typename T>
 __device__ __forceinline__ float act_gelu(float x) {
   if constexpr (sizeof(T) == 2) return gelu_bf16(x);
-  else return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
+  else return gelu_fast(x);
 }
 template <typename T>
 __device__ __forceinline__ float act_gelu_grad(float x) {
   if constexpr (sizeof(T) == 2) return gelu_grad_bf16(x);
-  else {
-    const float cdf = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
-    return cdf + x * (0.39894228040143268f * expf(-0.5f * x * x));
-  }
+  else return gelu_grad_fast(x);
 }
 template <typename T>
 __device__ __forceinline__ float act_gelu_tanh(float x) {

@@ -1,4 +1,4 @@
-// Exact (erf) GELU and its derivative for kernels with bf16 outputs.
+// Exact (erf) GELU and its derivative, for fp32 and bf16 outputs.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -24,7 +24,9 @@ namespace {
 //   gelu, 2-norm, x from N(0, 1)            3.9e-8 / 3.4e-8 / 3.9e-8
 //   derivative, 2-norm, x from N(0, 1)      6.4e-8 / 3.8e-8 / 4.0e-8
 // The negative tail keeps a relative accuracy where 1 + erf cancels: 7e-7 for x in
-// -3 .. -1.25, then growing with the rounding of x^2 to 3e-6 at -8; 2e-5 at -13.
+// -3 .. -1.25, then growing with the rounding of x^2 to 3e-6 at -8; 2e-5 at -13.  So fp32
+// outputs take it too, and it is cheaper there as well: the way back of 8192 x 8192 174 us
+// with erff, 163 with erfc (18 us more in pf_gelu_bwd, though: 179), 150 so.
 // e: exp(-x^2 / 2).
 __device__ __forceinline__ float normal_cdf(float x, float &e) {
   const float u = x * x;

@@ -42,21 +42,6 @@ __device__ __forceinline__ f32x4 get4(const bf16_t *p) {
 }
 __device__ __forceinline__ f32x4 get4(const float *p) { return *(const f32x4 *)p; }
 
-// fp32 outputs keep the library erff (as in the NT kernels they replace).
-template <typename T>
-__device__ __forceinline__ float gelu_s(float x) {
-  if constexpr (sizeof(T) == 2) return gelu_fast(x);
-  else return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
-}
-template <typename T>
-__device__ __forceinline__ float gelu_grad_s(float x) {
-  if constexpr (sizeof(T) == 2) return gelu_grad_fast(x);
-  else {
-    const float cdf = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
-    return cdf + x * (0.39894228040143268f * __expf(-0.5f * x * x));
-  }
-}
-
 // T: bf16 or float storage.  NH: sub-blocks per step (2 for bf16 blocks of 32,
 // half a 128-byte step each).  BKN: B read as [k][n].  EPI: 0 none, 1 GELU
 // forward, 2 GELU backward, 3 bias, activation and residual (kEpiAct).
@@ -274,10 +259,10 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   if constexpr (EPI == 1) {
     put4((T *)n.C2 + eoff, v);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = gelu_s<T>(v[q]);
+    for (int q = 0; q < 4; ++q) v[q] = gelu_fast(v[q]);
   } else if constexpr (EPI == 2) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] *= gelu_grad_s<T>(aux[q]);
+    for (int q = 0; q < 4; ++q) v[q] *= gelu_grad_fast(aux[q]);
   } else if constexpr (EPI == 3) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] += bz[q];
