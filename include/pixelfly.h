@@ -322,8 +322,11 @@ pf_status pf_linear_fwd(const pf_layout *layout, pf_dtype dtype, int64_t T,
 /* Activations of pf_linear_fwd_act; s(y) = 1 / (1 + exp(-y)). */
 typedef enum {
   PF_ACT_NONE = 0,
-  PF_ACT_GELU = 1,      /* exact (erf) GELU, z Phi(z); bf16: within 3e-5 of it
-                           before rounding                                        */
+  PF_ACT_GELU = 1,      /* exact (erf) GELU, z Phi(z); fp32: within (1.4 z^2 + 34)
+                           2^-24 of itself; bf16: before rounding within 3e-5 of
+                           itself for z >= -7, within 1e-15 (absolute) below, by a
+                           shorter form than PF_EPI_GELU's: the two calls' results
+                           may differ by a bf16 step                              */
   PF_ACT_GELU_TANH = 2, /* z s(2 sqrt(2 / pi) (z + 0.044715 z^3)): the tanh form  */
   PF_ACT_SILU = 3,      /* z s(z)                                                 */
   PF_ACT_RELU = 4
@@ -545,10 +548,12 @@ pf_status pf_relpos_bias(const pf_relpos *relpos, int32_t H, const float *table,
                          void *stream);
 
 /* Rows of 64 contiguous bf16 elements: sequence, head and token strides in
- * elements (multiples of 8; token stride 64 or more).  Sequences or heads of an
- * input may share memory (stride 0).  No two rows of an output may: taken by
- * ascending stride, tokens, heads and sequences each step past all that the
- * smaller ones cover (INVALID_ARG otherwise).  Outputs overlap no input and no
+ * elements (multiples of 8; token stride 64 or more, at most 2^24).  A head's
+ * rows of one sequence, and 64 more, span less than 2^31 bytes (UNSUPPORTED
+ * otherwise); heads and sequences may lie any distance apart.  Sequences or
+ * heads of an input may share memory (stride 0).  No two rows of an output may:
+ * taken by ascending stride, tokens, heads and sequences each step past all that
+ * the smaller ones cover (INVALID_ARG otherwise).  Outputs overlap no input and no
  * other output. */
 typedef struct {
   void *data;
@@ -597,7 +602,9 @@ pf_status pf_attn_relpos_fwd(const pf_layout *layout, const pf_relpos *relpos, i
  * bitwise.  P comes from lse, which is rounded itself: beside the scores' error it is off
  * by at most 20 x 2^-24 |lse| of itself, so the gradients keep bf16's precision up
  * to |lse| of about 2^10, have no digits left at 2^19 and may be infinite or NaN past
- * 2^26.  Needs pf_attn_relpos_workspace_bytes(layout, relpos, B, H, S).
+ * 2^26.  (A NaN or infinity in a row or token of an attended block spreads to the
+ * others of that block, masked pairs included.)
+ * Needs pf_attn_relpos_workspace_bytes(layout, relpos, B, H, S).
  * Errors: INVALID_ARG, UNSUPPORTED, STATE, WORKSPACE, HIP.
  */
 pf_status pf_attn_relpos_bwd(const pf_layout *layout, const pf_relpos *relpos, int32_t B, int32_t H,

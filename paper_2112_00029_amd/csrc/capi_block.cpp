@@ -275,7 +275,9 @@ Lists row_lists(const pf_layout *L, const pf_relpos *R, bool columns) {
 Parts fwd_parts(const pf_layout *L, const pf_relpos *R, int32_t B, int32_t H, int32_t Sq, bool chunk) {
   const Lists l = row_lists(L, R, false);
   // A chunk starts anywhere in a block, and anywhere in its sequence: which of
-  // its tiles are a stripe's is not known here.
+  // its tiles are a stripe's is not known here.  A chunk inside a stripe pays for it (12
+  // heads, the first 64 rows of 4096 with a stripe of one block: 58 us as a chunk, 15 as
+  // the first rows of the sequence).
   return choose_parts(B * H, (Sq + (chunk ? 63 : 0) + 63) / 64, chunk ? 0 : l.nlong, l.long_items, l.items,
                       kRowSplit);
 }

@@ -452,9 +452,10 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
     return;
   }
   // GELU backward (EPI 2): the pre-activations of a pass are loaded before its sums are
-  // staged; so is the residual of EPI 3 (an empty range, zeros, without one).  Rows past M and dead columns read zero (range check), so the loads
-  // need no branch.  (A pass further ahead, in two sets of registers, is no faster: 8192
-  // x 4096 66.4 us so, 66.7 that way.)
+  // staged; so is the residual of EPI 3 (an empty range, zeros, without one).  Rows past
+  // M and dead columns read zero (range check), so the loads need no branch.  (A pass
+  // further ahead, in two sets of registers, is no faster: 8192 x 4096 66.4 us so, 66.7
+  // that way.)
   constexpr int NPASS = TM * (32 / SP), NIT = SP / RPI;
   constexpr bool AUX = EPI >= 2;
   u32x4 ax[AUX ? NIT : 1];
@@ -532,6 +533,12 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
           // but for blocks of 32 (16384 x 4096, b = 128: the output 707 -> 703 us,
           // without pre-activation 653 -> 637, both 682; 8192 tokens, b = 64, both
           // 35.6 -> 33.7; 2509 x 4096, b = 32 the output 89 -> 88, both 91).
+          // With the layer that reads the output next (1024 or 4096 -> four times
+          // that -> back, rank 128, no pre-activation) the output streamed / not:
+          // 16384 x 16384 b = 32 / 64 / 128 921 / 975, 869 / 897, 1111 / 1145 us; 16384
+          // x 4096 218 / 218; 8192 x 4096 126 / 128; 2509 x 16384 167 / 164, 172 / 168,
+          // 223 / 218; 2100 x 4096 b = 32 / 64 59 / 57, 68 / 66.  So outputs that the
+          // caches hold lose up to 4 % in the pair where the call alone gains as much.
           if constexpr (BLK >= 64) __builtin_nontemporal_store(z, (u32x4 *)((bf16_t *)a.C2 + o));
           else *(u32x4 *)((bf16_t *)a.C2 + o) = z;
         }

@@ -69,9 +69,9 @@ struct NTArgs {
   int64_t ldc;
   void *C2;             // GELU forward: pre-activation output
   const void *aux;      // GELU backward: pre-activation input; kEpiAct: residual or null
-  int epi;              // kEpi* below
+  int epi;              // kEpi*
   const void *bias;     // kEpiAct: N elements or null
-  int act;              // kEpiAct: kAct* below
+  int act;              // kEpiAct: kAct*
   int64_t M;            // tokens
   const NTTile *tiles;  // null in dense mode
   int ntiles;           // output column tiles (dense mode: ceil(nblk / G))

@@ -39,11 +39,13 @@
 // outputs.
 //
 // 8 x 12 x 4096, 7 blocks per row, 3 of them mixed (without a bias, attn_kernels.hip,
-// same box): forward 72 (65) us, VALU 51 % of cycles, MFMA 24 %, LDS 15 %; dQ with the
-// table gradient 121 - 126 (97), VALU 51 / MFMA 24 / LDS 17 %, three waves per SIMD
-// where 24 KiB of LDS and 150 registers leave room, not four; dK/dV 129 - 135 (115),
-// VALU 41 / MFMA 30 / LDS 24 %.  Like those kernels they are bound by the serial S ->
-// softmax -> product chain of few waves and the vector unit's part of it.
+// same run; boxes differ by a tenth): forward 79 (72) us, 83 on inputs that change from
+// call to call; dQ with the table gradient 120 (98), three waves per SIMD where 24 KiB
+// of LDS and 150 registers leave room, not four; dK/dV 127 (113), two waves.  Busy
+// cycles of VALU / MFMA / LDS: forward 57 - 58 / 27 - 28 / 16 - 17 %, dQ 50 / 23 / 17 %,
+// dK/dV 40 - 42 / 29 / 23 - 24 %.  No unit is full: a wave's steps S -> softmax ->
+// product of a block depend on one another, and the waves that fit a SIMD do not fill
+// the gaps.
 // Measured and not kept: mixed scores that start at their bias in the accumulator, with
 // every block on one path (forward 78 at three waves, dQ 124 - 129 against 119 - 122;
 // dK/dV keeps it: 135 -> 128); a loop body per kind of block (51 - 61 registers
