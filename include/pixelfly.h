@@ -180,6 +180,23 @@ pf_status pf_layout_create_butterfly(int64_t n, int32_t b, int32_t max_stride,
                                      pf_layout **out);
 
 /*
+ * Layout of a gated layer: two projections of one input, each n_out x n_in on the
+ * mask of pf_layout_create (or of an explicit block mask, as
+ * pf_layout_create_from_mask), as one matrix of 2 n_out rows whose block rows
+ * alternate: block row 2 i is block row i of the gate's projection, 2 i + 1 block
+ * row i of the other factor's.  So U, bias, Z and Wblk hold b rows (columns of Z;
+ * the kept blocks of a block row) of the gate, then the same b of the other factor,
+ * and so on; n_out and nb_out of pf_layout_info_get are the doubled ones.  It serves
+ * pf_linear_gated_fwd, and every other pf_linear call as the 2 n_out x n_in layer it
+ * is: pf_linear_bwd_data and pf_linear_bwd_weight on dZ are the gated layer's.
+ * Host only.  Errors: INVALID_ARG, NOMEM.
+ */
+pf_status pf_layout_create_gated(int64_t n_out, int64_t n_in, int32_t b, int32_t max_stride,
+                                 pf_layout **out);
+pf_status pf_layout_create_gated_from_mask(int32_t nb_out, int32_t nb_in, int32_t b,
+                                           const uint8_t *block_mask, pf_layout **out);
+
+/*
  * One launch: the whole product on T token rows (bf16; b = 32 and
  * max_stride <= 32 in this build, else UNSUPPORTED).  Each workgroup holds a
  * 32-token x (max_stride * 32)-feature tile of the activation in LDS and
@@ -378,6 +395,49 @@ pf_status pf_linear_act_bwd(pf_dtype dtype, int64_t T, int64_t N, pf_activation 
 /* Workspace bytes of pf_linear_act_bwd with dbias (0 on invalid arguments, or
  * when it needs none). */
 size_t pf_linear_act_workspace_bytes(pf_dtype dtype, int64_t T, int64_t N);
+
+/*
+ * Gated layer (the first half of a gated feed-forward block), both projections,
+ * activation and product in one kernel:
+ *     Z = [Zg Zu] = X (M o W)^T + T_lr U^T + bias   (T x 2N, blocks alternating)
+ *     H = act(Zg) o Zu                              (T x N)
+ * on a layout of pf_layout_create_gated (2N = its n_out; INVALID_ARG for another).
+ * bias: 2N elements or NULL.  Z receives the pre-activations for the backward; NULL
+ * keeps none (serving).  PF_ACT_NONE multiplies the two projections.  Sums,
+ * activation and product are fp32, of the unrounded Z; H and Z are rounded once
+ * each.  No buffers may overlap.  The mixed form takes gamma as
+ * pf_linear_fwd_mixed does.  Workspace: pf_workspace_bytes of the layout.
+ * Way back: pf_linear_gated_bwd, then pf_linear_bwd_data and pf_linear_bwd_weight
+ * on the same layout with dZ for their dY.  Everything else as pf_linear_fwd.
+ * Errors: INVALID_ARG, UNSUPPORTED, STATE, WORKSPACE, HIP.
+ */
+pf_status pf_linear_gated_fwd(const pf_layout *layout, pf_dtype dtype, int64_t T, int32_t r,
+                              const void *X, const void *Wblk, const void *U, const void *V,
+                              const void *bias, pf_activation act, void *H, void *Z, void *T_lr,
+                              void *workspace, size_t ws_bytes, void *stream);
+pf_status pf_linear_gated_fwd_mixed(const pf_layout *layout, pf_dtype dtype, int64_t T, int32_t r,
+                                    float gamma, const void *X, const void *Wblk, const void *U,
+                                    const void *V, const void *bias, pf_activation act, void *H,
+                                    void *Z, void *T_lr, void *workspace, size_t ws_bytes,
+                                    void *stream);
+
+/*
+ * Backward of that product, from dH (T x N) and Z (T x 2N, blocks of b columns
+ * alternating; b in {32, 64, 128} dividing N):
+ *     dZg = dH o Zu o act'(Zg),  dZu = dH o act(Zg)   (dZ: T x 2N as Z)
+ *     dbias = column sums of dZ (2N elements of the call's dtype)
+ * in one pass; the sums take the unrounded products, in fp32 and a fixed order.
+ * dbias may be NULL.  dZ may be Z itself; nothing else may overlap.  With dbias
+ * it needs a workspace of pf_linear_gated_workspace_bytes.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ */
+pf_status pf_linear_gated_bwd(pf_dtype dtype, int64_t T, int64_t N, int32_t b, pf_activation act,
+                              const void *dH, const void *Z, void *dZ, void *dbias, void *workspace,
+                              size_t ws_bytes, void *stream);
+
+/* Workspace bytes of pf_linear_gated_bwd with dbias (0 on invalid arguments, or
+ * when it needs none). */
+size_t pf_linear_gated_workspace_bytes(pf_dtype dtype, int64_t T, int64_t N);
 
 /*
  * Backward-data (gradient of the layer w.r.t. its input):
@@ -620,6 +680,87 @@ size_t pf_attn_relpos_workspace_bytes(const pf_layout *layout, const pf_relpos *
                                       int32_t H, int32_t Sq);
 
 /*
+ * Layer normalisation of T rows of N elements (any N in 1 .. 16384), rows ldx (ldy,
+ * ...) >= N elements apart; elements between rows are neither read nor written:
+ *     mean, var of a row,  rstd = 1 / sqrt(var + eps),
+ *     Y = (X - mean) rstd o weight + bias
+ * weight, bias: N elements of the call's dtype or NULL (one; zero).  mean, rstd: T
+ * fp32 each, for the backward; either may be NULL.  Statistics are fp32, of the
+ * whole row in registers: var is the mean of squared differences (a row of equal
+ * elements has var 0 exactly; squares beyond fp32's range give rstd = 0).  Y may be
+ * X itself with the same stride.  A NaN or infinity stays in its row.  Pointers
+ * 16-byte aligned; N and strides that are multiples of 16 bytes are fastest.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+pf_status pf_layernorm_fwd(pf_dtype dtype, int64_t T, int64_t N, float eps, const void *X, int64_t ldx,
+                           const void *weight, const void *bias, void *Y, int64_t ldy, float *mean,
+                           float *rstd, void *stream);
+
+/*
+ * Its gradients, from dY, X and the forward's mean and rstd, with n = (X - mean)
+ * rstd and g = dY o weight:
+ *     dX = rstd (g - mean(g) - n mean(g o n)) + dR
+ *     dweight = column sums of dY o n,  dbias = column sums of dY
+ * dR (T x N, or NULL): a gradient that reaches X another way, as a residual stream
+ * has it.  dX may be dR, dY or X itself with the same stride.  dweight and dbias (N
+ * elements of the call's dtype): either may be NULL; summed in fp32 and a fixed
+ * order; with either the call needs a workspace of pf_layernorm_workspace_bytes.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ */
+pf_status pf_layernorm_bwd(pf_dtype dtype, int64_t T, int64_t N, const void *dY, int64_t lddy,
+                           const void *X, int64_t ldx, const void *weight, const float *mean,
+                           const float *rstd, const void *dR, int64_t lddr, void *dX, int64_t lddx,
+                           void *dweight, void *dbias, void *workspace, size_t ws_bytes, void *stream);
+
+/* Workspace bytes of pf_layernorm_bwd (0 on invalid arguments). */
+size_t pf_layernorm_workspace_bytes(pf_dtype dtype, int64_t T, int64_t N);
+
+/*
+ * Norm over all gradients of a model, and the gradients scaled to at most a given
+ * norm.
+ *
+ * A list names the tensors: n elements at src, and where their scaled values go
+ * (dst: src itself, or another buffer, which may be of another type, as an
+ * optimizer's fp32 copy).  Elements need their own alignment only; tensors may be
+ * empty.  What is written must not overlap any other tensor of the list.  The list
+ * is made once for the buffers a program keeps; pf_grads_upload copies it to the
+ * current device (one-time, synchronous on `stream`), which it then serves alone.
+ * The buffers stay the caller's.  Errors: INVALID_ARG, NOMEM, HIP.
+ */
+typedef struct {
+  const void *src;
+  void *dst;
+  int64_t n;
+  int32_t src_dtype, dst_dtype; /* pf_dtype */
+} pf_grad_tensor;
+typedef struct pf_grads pf_grads; /* opaque; immutable after create */
+pf_status pf_grads_create(int32_t n, const pf_grad_tensor *tensors, pf_grads **out);
+pf_status pf_grads_upload(pf_grads *grads, void *stream);
+void pf_grads_destroy(pf_grads *grads);
+
+/*
+ * pf_grads_clip:   norm = sqrt(sum of all squares); dst = src * min(1, max_norm /
+ *                  norm) (norm: one fp32 on the device, or NULL).
+ * pf_grads_norm:   the sum of squares (one fp64 on the device) and the norm alone;
+ *                  either may be NULL, not both.
+ * pf_grads_scale:  the scaling alone, by a sum of squares on the device: with the
+ *                  sums of several processes added up in between, the two clip
+ *                  gradients that are spread over them.
+ * Squares are summed in 64 bits and a fixed order (repeat calls agree bitwise).  A
+ * norm that is infinite or NaN scales nothing: the caller sees it in norm and drops
+ * the step.  Scaled values are products in fp32, rounded once; tensors in place
+ * that need no scaling are not touched.  max_norm finite and >= 0.  Workspace of
+ * clip and norm: pf_grads_workspace_bytes.
+ * Errors: INVALID_ARG, STATE, WORKSPACE, HIP.
+ */
+size_t pf_grads_workspace_bytes(const pf_grads *grads);
+pf_status pf_grads_clip(const pf_grads *grads, float max_norm, float *norm, void *workspace,
+                        size_t ws_bytes, void *stream);
+pf_status pf_grads_norm(const pf_grads *grads, double *sumsq, float *norm, void *workspace,
+                        size_t ws_bytes, void *stream);
+pf_status pf_grads_scale(const pf_grads *grads, float max_norm, const double *sumsq, void *stream);
+
+/*
  * Dense comparator GEMM built from the same MFMA tiles as the sparse
  * kernels (the speedup baseline: an equally shaped dense layer):
  *   PF_OP_NT: C[M][N] = A[M][K] . B[N][K]^T   (forward,  X W^T)
@@ -659,8 +800,10 @@ typedef enum {
   PF_KERNEL_LOWRANK_T = 3,      /* rank-r product T_lr = X V^T */
   PF_KERNEL_LOWRANK_S = 4,      /* rank-r product S = dY U */
   PF_KERNEL_REDUCE = 5,         /* sums of split partial results; the b = 32
-                                   backward-data pair-block gather; pf_relpos_bias */
-  PF_KERNEL_GELU_BWD = 6,       /* standalone GELU backward, pf_linear_act_bwd */
+                                   backward-data pair-block gather; pf_relpos_bias;
+                                   pf_layernorm_*, pf_grads_* */
+  PF_KERNEL_GELU_BWD = 6,       /* standalone GELU backward, pf_linear_act_bwd,
+                                   pf_linear_gated_bwd */
   PF_KERNEL_ATTN_FWD = 7,
   PF_KERNEL_ATTN_BWD_DQ = 8,    /* dQ (and the row terms delta) */
   PF_KERNEL_ATTN_BWD_DKV = 9,   /* dK, dV (and the sums of dtable) */

@@ -131,7 +131,9 @@ bool use_small_nt(int dtype, int blk, int G, int64_t M, int ntiles) {
 hipError_t nt_launch(pf_kernel_class kc, int dtype, int blk, int G, bool b_kn, int bm, int kmax,
                      const pf::NTArgs &a_in, hipStream_t s) {
   Timed t(kc, s);
-  if (!a_in.dense && use_small_nt(dtype, blk, G, a_in.M, a_in.ntiles))
+  // (A workgroup of the small-product kernel takes both blocks of a gated pair.)
+  const bool gated = !a_in.dense && a_in.epi == pf::kEpiGated;
+  if (!a_in.dense && use_small_nt(dtype, blk, gated ? G / 2 : G, a_in.M, a_in.ntiles))
     return pf::launch_small(dtype, blk, G, b_kn, kmax, a_in, s);
   pf::NTArgs a = a_in;
   a.band = nt_band(a.dense != 0, b_kn, a.ntiles);
@@ -508,6 +510,14 @@ NTList fwd_list(const pf_layout *L, int dt, int64_t T) {
   return NTList{false, L->G_fwd, (int)L->fwd_tiles.size(), L->kmax_fwd, L->d_fwd_tiles,
                 L->d_kcols_fwd, L->d_blks_fwd};
 }
+// Of the gated forward: pairs of 128-row blocks are 256 columns whatever the token
+// count.
+NTList gated_list(const pf_layout *L, int dt, int64_t T) {
+  if (L->b == 128)
+    return NTList{true, L->G_fwd_w, (int)L->fwd_tiles_w.size(), L->kmax_fwd, L->d_fwd_tiles_w,
+                  L->d_kcols_fwd_w, L->d_blks_fwd_w};
+  return fwd_list(L, dt, T);
+}
 NTList bwd_list(const pf_layout *L, int dt, int64_t T) {
   const bool wide = ntd_width(dt, L->b, L->G_bwd_w) && L->G_bwd_w * L->b == 256 && T >= PF_WIDE_MIN_T;
   if (wide)
@@ -632,6 +642,55 @@ pf_status pf_layout_create(int64_t n_out, int64_t n_in, int32_t b, int32_t max_s
   }
   *out = L;
   return PF_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// A new layout from build(layout), which returns "" or an error.
+template <typename Build>
+pf_status new_layout(pf_layout **out, Build build) {
+  if (!out) return fail(PF_ERR_INVALID_ARG, "out is NULL");
+  *out = nullptr;
+  pf_layout *L = new (std::nothrow) pf_layout();
+  if (!L) return fail(PF_ERR_NOMEM, "host allocation failed");
+  std::string e;
+  try {
+    e = build(*L);
+  } catch (const std::bad_alloc &) {
+    delete L;
+    return fail(PF_ERR_NOMEM, "host allocation failed");
+  } catch (...) {
+    delete L;
+    return fail(PF_ERR_INVALID_ARG, "layout build failed");
+  }
+  if (!e.empty()) {
+    delete L;
+    return fail(PF_ERR_INVALID_ARG, e);
+  }
+  *out = L;
+  return PF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+pf_status pf_layout_create_gated(int64_t n_out, int64_t n_in, int32_t b, int32_t max_stride,
+                                 pf_layout **out) {
+  return new_layout(out, [&](pf_layout &L) {
+    std::string e = pf::build_layout(L, n_out, n_in, b, max_stride);
+    return e.empty() ? pf::build_gated_layout(L) : e;
+  });
+}
+
+pf_status pf_layout_create_gated_from_mask(int32_t nb_out, int32_t nb_in, int32_t b,
+                                           const uint8_t *block_mask, pf_layout **out) {
+  return new_layout(out, [&](pf_layout &L) {
+    std::string e = pf::build_layout_from_mask(L, nb_out, nb_in, b, block_mask);
+    return e.empty() ? pf::build_gated_layout(L) : e;
+  });
 }
 
 pf_status pf_layout_create_from_mask(int32_t nb_out, int32_t nb_in, int32_t b,
@@ -1042,7 +1101,7 @@ void set_mix(pf::NTArgs &a, const Mix &m) {
 
 // What follows the products in the forward's epilogue: kEpiNone, kEpiGelu, or
 // kEpiAct with a bias (N), an activation and a residual (T x N; both may be
-// null).
+// null), or kEpiGated with a bias and an activation (Y is half as wide).
 struct FwdEpi {
   int epi;
   const void *bias;
@@ -1065,6 +1124,11 @@ pf_status check_fwd_epi(const FwdEpi &e, const void *Y_pre) {
       return fail(PF_ERR_INVALID_ARG, "Y_pre given without an activation");
     return Y_pre ? need_ptr(Y_pre, "Y_pre") : PF_OK;
   }
+  if (e.epi == pf::kEpiGated) {
+    if (e.act < pf::kActNone || e.act > pf::kActRelu) return fail(PF_ERR_INVALID_ARG, "bad activation");
+    if (e.bias && (st = need_ptr(e.bias, "bias")) != PF_OK) return st;
+    return Y_pre ? need_ptr(Y_pre, "Z") : PF_OK;
+  }
   if (e.epi < 0) return fail(PF_ERR_INVALID_ARG, "bad epilogue");
   if (e.epi == PF_EPI_GELU && (st = need_ptr(Y_pre, "Y_pre")) != PF_OK) return st;
   if (e.epi == PF_EPI_NONE && Y_pre) return fail(PF_ERR_INVALID_ARG, "Y_pre given without GELU epilogue");
@@ -1079,8 +1143,11 @@ pf_status linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, c
   if (st != PF_OK) return st;
   if ((st = check_dtype_r(dtype, T, r, L->b)) != PF_OK) return st;
   if ((st = check_extent(L, dtype, r)) != PF_OK) return st;
+  const bool gated = epi.epi == pf::kEpiGated;
+  if (gated && !L->gated)
+    return fail(PF_ERR_INVALID_ARG, "not a gated layout (pf_layout_create_gated)");
   if ((st = need_ptr(X, "X")) != PF_OK || (st = need_ptr(Wblk, "Wblk")) != PF_OK ||
-      (st = need_ptr(Y, "Y")) != PF_OK)
+      (st = need_ptr(Y, gated ? "H" : "Y")) != PF_OK)
     return st;
   if (r > 0 && ((st = need_ptr(U, "U")) != PF_OK || (st = need_ptr(V, "V")) != PF_OK ||
                 (st = need_ptr(T_lr, "T_lr")) != PF_OK))
@@ -1117,15 +1184,22 @@ pf_status linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, c
     // Nothing to add or apply: the plain epilogue.
     if (!a.bias && !a.aux && a.act == pf::kActNone) a.epi = pf::kEpiNone;
   }
+  if (gated) {
+    a.bias = epi.bias;
+    a.act = epi.act;
+    a.ldc = L->n_out / 2;
+    a.ldc2 = L->n_out;
+  }
   a.M = T;
-  const NTList tl = fwd_list(L, dt, T);
+  const NTList tl = gated ? gated_list(L, dt, T) : fwd_list(L, dt, T);
   a.tiles = tl.tiles;
   a.ntiles = tl.ntiles;
   a.kcols = tl.kcols;
   a.blks = tl.blks;
   a.nsplit = 1;
   set_mix(a, mix);
-  return hip_status(nt_launch(PF_KERNEL_SPMM_FWD, dt, b, tl.G, false, 128, tl.kmax + a.nlr, a, s),
+  const int bm = gated && b == 128 ? 64 : 128;
+  return hip_status(nt_launch(PF_KERNEL_SPMM_FWD, dt, b, tl.G, false, bm, tl.kmax + a.nlr, a, s),
                     "forward kernel");
 }
 
@@ -1158,6 +1232,24 @@ pf_status pf_linear_fwd_mixed(const pf_layout *L, pf_dtype dtype, int64_t T, int
   if (st != PF_OK) return st;
   return linear_fwd(L, dtype, T, r, Mix{true, gamma, 1.f - gamma}, X, Wblk, U, V, Y, T_lr,
                     plain_epi(epi), Y_pre, workspace, ws_bytes, stream);
+}
+
+pf_status pf_linear_gated_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, const void *X,
+                              const void *Wblk, const void *U, const void *V, const void *bias,
+                              pf_activation act, void *H, void *Z, void *T_lr, void *workspace,
+                              size_t ws_bytes, void *stream) {
+  return linear_fwd(L, dtype, T, r, kNoMix, X, Wblk, U, V, H, T_lr,
+                    FwdEpi{pf::kEpiGated, bias, (int)act, nullptr}, Z, workspace, ws_bytes, stream);
+}
+
+pf_status pf_linear_gated_fwd_mixed(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, float gamma,
+                                    const void *X, const void *Wblk, const void *U, const void *V,
+                                    const void *bias, pf_activation act, void *H, void *Z, void *T_lr,
+                                    void *workspace, size_t ws_bytes, void *stream) {
+  pf_status st = check_gamma(gamma);
+  if (st != PF_OK) return st;
+  return linear_fwd(L, dtype, T, r, Mix{true, gamma, 1.f - gamma}, X, Wblk, U, V, H, T_lr,
+                    FwdEpi{pf::kEpiGated, bias, (int)act, nullptr}, Z, workspace, ws_bytes, stream);
 }
 
 pf_status pf_linear_fwd_act_mixed(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r,

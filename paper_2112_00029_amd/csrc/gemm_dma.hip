@@ -60,7 +60,11 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
   constexpr int KW = BK < BLK ? BK : BLK;  // K width of one sub-block
   constexpr int NH = BK / KW;              // sub-blocks per step
   // Waves: WGN = BN / 64 along N (64 output columns each), the rest along M.
-  constexpr int WTN = 64, WGN = BN / WTN, WGM = NW / WGN, WTM = BM / WGM;
+  // A gated wave's columns are two runs of WTN / 2: of gate blocks and, at the same
+  // places, of the other factor's, so that a lane holds both factors of its outputs.
+  // Tiles of eight waves take 128 columns each: output rows of 128 bytes.
+  constexpr bool GATED = EPI == 4;
+  constexpr int WTN = GATED && NW == 8 ? 128 : 64, WGN = BN / WTN, WGM = NW / WGN, WTM = BM / WGM;
   constexpr int TM = WTM / 32, TN = WTN / 32;
   // A region: NH sub-blocks of [BM][KW]; B region: G x NH pieces of [BLK][KW]
   // (NT) or [KW][BLK] (B read as [k][n]).
@@ -321,8 +325,16 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
         xf[tm] = frag_rows<RBA>(st.a + h * (BM * RBA), wm * WTM + tm * 32, kq, lane);
       });
       sfor<TN>([&](auto tn) __attribute__((always_inline)) {
-        const int n0 = wn * WTN + tn * 32;
-        const int g = n0 / BLK, nl = n0 % BLK;
+        int g, nl;
+        if constexpr (GATED) {
+          const int h = wn * (WTN / 2) + tn % (TN / 2) * 32;
+          g = 2 * (h / BLK) + tn / (TN / 2);
+          nl = h % BLK;
+        } else {
+          const int n0 = wn * WTN + tn * 32;
+          g = n0 / BLK;
+          nl = n0 % BLK;
+        }
         const uint8_t *piece = st.b + (g * NH + h) * PIECE;
         if constexpr (BKN) wf[tn] = frag_kn<RBB>(piece, nl, kq, lane);
         else wf[tn] = frag_rows<RBB>(piece, nl, kq, lane);
@@ -383,7 +395,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
   // lane then writes 8 consecutive columns of one row.  The staging area is the stage
   // buffer no wave reads in the last step; it needs no barrier because each
   // wave only touches its own slice and a wave's LDS accesses are ordered.
-  constexpr int SROW = WTN * 4, SCH = SROW / 16;  // staged row bytes, chunks
+  // (Gated: bf16 values.)
+  constexpr int SROW = WTN * (GATED ? 2 : 4), SCH = SROW / 16;  // staged row bytes, chunks
   constexpr int SP = 32;                          // rows per pass
   constexpr int LPR = WTN / 8, RPI = 64 / LPR;    // lanes per row, rows per store step
   // Staging slices per stage (in its A array, then its B array); the stages
@@ -400,6 +413,86 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
   int ob[G];
   sfor<G>([&](auto g) __attribute__((always_inline)) { ob[g] = out_blk(g); });
   bf16_t *C = (bf16_t *)a.C;
+  if constexpr (GATED) {
+    // Z = sums + biases stays in the accumulators; its rounded rows, then those of
+    // act(gate) x other, pass through the staging area as below: units of 4
+    // columns, XOR-swizzled by row, read back as 16-byte chunks.
+    constexpr int HT = TN / 2;
+    auto gate_h = [&](int t) __attribute__((always_inline)) { return wn * (WTN / 2) + t * 32; };
+    auto blk_at = [&](int g) __attribute__((always_inline)) -> int {
+      int o = ob[0];
+      sfor<G>([&](auto gg) __attribute__((always_inline)) { if (g == gg) o = ob[gg]; });
+      return o;
+    };
+    // Biases of this lane's columns.
+    u32x2 bz[TN][4];
+    sfor<TN>([&](auto tn) __attribute__((always_inline)) {
+      const int h = gate_h(tn % HT), g = 2 * (h / BLK) + tn / HT;
+      const bf16_t *p = (const bf16_t *)a.bias + (int64_t)blk_at(g) * BLK + h % BLK + (lane >> 5) * 4;
+      sfor<4>([&](auto q) __attribute__((always_inline)) {
+        bz[tn][q] = a.bias ? *(const u32x2 *)(p + q * 8) : u32x2{0u, 0u};
+      });
+    });
+    // Rows of COLS staged columns to memory: out(column of the wave's run) gives
+    // the matrix column, or -1.
+    auto flush = [&](auto cols, bf16_t *out, int64_t ld, int tm, auto at) __attribute__((always_inline)) {
+      constexpr int COLS = decltype(cols)::value, L = COLS / 8, R = 64 / L, U = COLS / 4;
+      const int j = lane % L;
+      const int64_t c = at(j * 8);
+      sfor<32 / R>([&](auto it) __attribute__((always_inline)) {
+        const int rr = it * R + lane / L, sw = rr & (U < 16 ? U - 1 : 15);
+        u32x4 v = *(const u32x4 *)(stg + rr * (COLS * 2) + ((((2 * j) ^ sw) >> 1) << 4));
+        if (sw & 1) v = u32x4{v[2], v[3], v[0], v[1]};
+        const int64_t gm = m0 + wm * WTM + tm * 32 + rr;
+        if (gm < a.M && c >= 0) __builtin_nontemporal_store(v, (u32x4 *)(out + gm * ld + c));
+      });
+    };
+    auto put = [&](auto cols, int u, const float (&v)[4]) __attribute__((always_inline)) {
+      constexpr int COLS = decltype(cols)::value, U = COLS / 4;
+      const int r = lane & 31;
+      *(u32x2 *)(stg + r * (COLS * 2) + ((u ^ (r & (U < 16 ? U - 1 : 15))) << 3)) =
+          u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    };
+    sfor<TM>([&](auto tm) __attribute__((always_inline)) {
+      sfor<TN>([&](auto tn) __attribute__((always_inline)) {
+        sfor<4>([&](auto q) __attribute__((always_inline)) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = acc[tn][tm][q * 4 + e];
+            if (a.mix) v[e] *= a.mix_out;
+            v[e] += __uint_as_float(e & 1 ? bz[tn][q][e / 2] & 0xffff0000u : bz[tn][q][e / 2] << 16);
+            acc[tn][tm][q * 4 + e] = v[e];
+          }
+          if (a.C2) put(std::integral_constant<int, WTN>{}, tn * 8 + q * 2 + (lane >> 5), v);
+        });
+      });
+      if (a.C2)
+        flush(std::integral_constant<int, WTN>{}, (bf16_t *)a.C2, a.ldc2, tm,
+              [&](int c) __attribute__((always_inline)) -> int64_t {
+                const int h = gate_h(c / 32 % HT), g = 2 * (h / BLK) + c / 32 / HT;
+                return g < g_valid ? (int64_t)blk_at(g) * BLK + h % BLK + c % 32 : -1;
+              });
+      sfor<HT>([&](auto t) __attribute__((always_inline)) {
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = acc[t][tm][e];
+        act_apply<bf16_t>(a.act, v);
+        sfor<4>([&](auto q) __attribute__((always_inline)) {
+          float y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = v[q * 4 + e] * acc[HT + t][tm][q * 4 + e];
+          put(std::integral_constant<int, WTN / 2>{}, t * 8 + q * 2 + (lane >> 5), y);
+        });
+      });
+      flush(std::integral_constant<int, WTN / 2>{}, C, a.ldc, tm,
+            [&](int c) __attribute__((always_inline)) -> int64_t {
+              const int h = gate_h(c / 32), g = 2 * (h / BLK);
+              return g < g_valid ? (int64_t)(blk_at(g) >> 1) * BLK + h % BLK + c % 32 : -1;
+            });
+    });
+    return;
+  }
   const int jl = lane % LPR, rl = lane / LPR;
   const int cn = wn * WTN + jl * 8;  // first of this lane's 8 columns in the tile
   const int gcol = cn / BLK;
@@ -565,7 +658,13 @@ hipError_t ntd_go(const NTArgs &a, hipStream_t s) {
   const int64_t mtiles = (a.M + BM - 1) / BM;
   const int64_t grid = mtiles * a.ntiles * std::max(1, a.nsplit);
   if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (!DENSE && a.epi == kEpiAct) {
+  if (!DENSE && a.epi == kEpiGated) {
+    if constexpr (!DENSE && !BKN && G % 2 == 0)
+      launch_kernel(ntd_kernel<BLK, G, BKN, BM, BK, NS, NW, DENSE, 4, OCC>,
+                    dim3((unsigned)grid), dim3(64 * NW), s, a);
+    else
+      return hipErrorInvalidValue;
+  } else if (!DENSE && a.epi == kEpiAct) {
     if constexpr (!DENSE && !BKN)
       launch_kernel(ntd_kernel<BLK, G, BKN, BM, BK, NS, NW, DENSE, 3, OCC>,
                     dim3((unsigned)grid), dim3(64 * NW), s, a);

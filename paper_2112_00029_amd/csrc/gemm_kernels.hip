@@ -266,9 +266,10 @@ __device__ __forceinline__ u32x4 bload(rsrc_t r, uint32_t off) {
 // ---------------------------------------------------------------------------
 // EPI: 0 plain store, 1 forward GELU (also store the pre-activation),
 // 2 backward GELU (scale by gelu' of the pre-activation a.aux), 3 bias,
-// activation and residual (kEpiAct).
+// activation and residual (kEpiAct), 4 bias, activation and product of pairs of
+// output blocks (kEpiGated).
 template <typename T, int BLK, int G, bool BKN, int BM, bool DENSE, int EPI>
-__global__ __launch_bounds__(256, 2) void nt_kernel(NTArgs a_arg) {
+__global__ __launch_bounds__(256, EPI == 4 && BM == 64 ? 1 : 2) void nt_kernel(NTArgs a_arg) {
   const NTArgs a = a_arg;  // local copy: lambdas below capture it by reference
   constexpr bool BF = std::is_same<T, bf16_t>::value;
   constexpr int ES = (int)sizeof(T);
@@ -541,6 +542,44 @@ __global__ __launch_bounds__(256, 2) void nt_kernel(NTArgs a_arg) {
   int ob[G];
   static_for<G>([&](auto g) __attribute__((always_inline)) { ob[g] = out_blk(g); });
   T *C = (T *)a.C;
+  if constexpr (EPI == 4) {
+    // 8 columns of a gate block (block 2 p of the tile) and the same of the other
+    // factor's (2 p + 1) make 8 columns of the output.
+    constexpr int HCH = BN / 16;
+    static_for<(BM * HCH) / 256>([&](auto it) __attribute__((always_inline)) {
+      const int q = tid + it * 256;
+      const int row = q / HCH, c8 = (q % HCH) * 8;
+      const int p = c8 / BLK, off = c8 % BLK;
+      int obg = ob[0];
+      static_for<G / 2>([&](auto pp) __attribute__((always_inline)) { if (p == pp) obg = ob[2 * pp]; });
+      const int64_t gm = m0 + row;
+      if (gm >= a.M || 2 * p >= g_valid) return;
+      const int64_t zc = (int64_t)obg * BLK + off;
+      float v[8], u[8];
+      const float *cg = Cs + row * CS + 2 * p * BLK + off;
+      load8(cg, v);
+      load8(cg + BLK, u);
+      float bg[8] = {}, bu[8] = {};
+      if (a.bias) {
+        load8((const T *)a.bias + zc, bg);
+        load8((const T *)a.bias + zc + BLK, bu);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = (a.mix ? v[e] * a.mix_out : v[e]) + bg[e];
+        u[e] = (a.mix ? u[e] * a.mix_out : u[e]) + bu[e];
+      }
+      if (a.C2) {
+        store8((T *)a.C2 + gm * a.ldc2 + zc, v);
+        store8((T *)a.C2 + gm * a.ldc2 + zc + BLK, u);
+      }
+      act_apply<T>(a.act, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= u[e];
+      store8(C + gm * a.ldc + (int64_t)(obg >> 1) * BLK + off, v);
+    });
+    return;
+  }
   constexpr int RCH = BN / 8;  // 8-column chunks per row
   static_for<(BM * RCH) / 256>([&](auto it) __attribute__((always_inline)) {
     const int q = tid + it * 256;
@@ -1034,7 +1073,13 @@ static hipError_t nt_go(const NTArgs &a, hipStream_t s) {
   // Epilogue variants: the forward takes the GELU-forward one or the one of
   // bias, activation and residual, the backward-data (B read as [k][n]) the
   // GELU-backward one.
-  if (!DENSE && a.epi == kEpiAct) {
+  if (!DENSE && a.epi == kEpiGated) {
+    // (bf16 gated tiles are all of the direct-to-LDS family.)
+    if constexpr (!DENSE && !BKN && G % 2 == 0 && std::is_same<T, float>::value)
+      launch_kernel(nt_kernel<T, BLK, G, BKN, BM, DENSE, 4>, dim3((unsigned)grid), dim3(256), s, a);
+    else
+      return hipErrorInvalidValue;
+  } else if (!DENSE && a.epi == kEpiAct) {
     if constexpr (!DENSE && !BKN)
       launch_kernel(nt_kernel<T, BLK, G, BKN, BM, DENSE, 3>, dim3((unsigned)grid), dim3(256), s, a);
     else
@@ -1054,7 +1099,8 @@ static hipError_t nt_go(const NTArgs &a, hipStream_t s) {
 
 // Instantiated tiles: sparse tiles with BM = 128 and G * b <= 128; dense
 // tiles (comparator, skinny rank-r products) with G * b = 128 and BM = 128
-// or 64.
+// or 64.  Pairs of 128-row blocks (gated, fp32): 64 x 256, whose epilogue tile
+// still fits what the operands leave.
 template <typename T, int BLK, bool BKN>
 static hipError_t nt_dispatch_g(int G, int bm, bool dense, const NTArgs &a, hipStream_t s) {
   constexpr int GMAX = 128 / BLK;
@@ -1070,6 +1116,13 @@ static hipError_t nt_dispatch_g(int G, int bm, bool dense, const NTArgs &a, hipS
     if (G != GMAX) return hipErrorInvalidValue;
     return bm == 64 ? nt_go<T, BLK, GMAX, BKN, 64, true>(a, s) : nt_go<T, BLK, GMAX, BKN, 128, true>(a, s);
   }
+  if constexpr (BLK == 128 && !BKN && std::is_same<T, float>::value)
+    if (G == 2 && bm == 64 && a.epi == kEpiGated) {
+      const int64_t grid = (a.M + 63) / 64 * a.ntiles;
+      if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
+      launch_kernel(nt_kernel<T, 128, 2, false, 64, false, 4>, dim3((unsigned)grid), dim3(256), s, a);
+      return hipGetLastError();
+    }
   if (bm != 128) return hipErrorInvalidValue;
   if (G == 1) return nt_go<T, BLK, 1, BKN, 128, false>(a, s);
   if constexpr (GMAX >= 2)

@@ -335,6 +335,22 @@ std::string build_layout_from_mask(pf_layout &L, int32_t nb_out, int32_t nb_in, 
   return finish_layout(L);
 }
 
+std::string build_gated_layout(pf_layout &L) {
+  if (L.nb_out > (1 << 29)) return "too many blocks";
+  std::vector<int32_t> ptr(1, 0), idx;
+  idx.reserve(2 * L.col_idx.size());
+  for (int32_t i = 0; i < 2 * L.nb_out; ++i) {
+    idx.insert(idx.end(), L.col_idx.begin() + L.row_ptr[i / 2], L.col_idx.begin() + L.row_ptr[i / 2 + 1]);
+    ptr.push_back((int32_t)idx.size());
+  }
+  L.row_ptr = std::move(ptr);
+  L.col_idx = std::move(idx);
+  L.n_out *= 2;
+  L.nb_out *= 2;
+  L.gated = true;
+  return finish_layout(L);
+}
+
 // Pair lists of b = 32 layouts with even block counts (see pf_layout): the
 // pair block-CSR, each pair block's sources, one backward-data tile per pair
 // column (pair rows ascending) and the weight-gradient items.

@@ -15,6 +15,9 @@ struct pf_layout {
   // factors (strides 2 .. 2^bfly_nfac); 0 for every other layout.
   int64_t bfly_n = 0;
   int32_t bfly_nfac = 0;
+  // Gated layouts: block rows 2 i and 2 i + 1 keep the same columns (those of
+  // block row i of the mask it was made from).
+  bool gated = false;
   int64_t nnzb = 0;
   std::vector<int32_t> row_ptr, col_idx, col_ptr, row_idx, tperm;
 
@@ -87,6 +90,9 @@ std::string build_cover_layout(pf_layout &L, int64_t n_out, int64_t n_in, int32_
 // (L = log2 max_stride, nb = n / b) whose f-th diagonal block keeps (p, p)
 // and (p, p XOR 2^f).  Its block-CSR order is the packing of the factors.
 std::string build_butterfly_layout(pf_layout &L, int64_t n, int32_t b, int32_t max_stride);
+// Layout of two projections on one mask (the block rows of L, each twice):
+// block row 2 i is the gate's block row i, 2 i + 1 the other factor's.
+std::string build_gated_layout(pf_layout &L);
 std::string finish_layout(pf_layout &L);
 // Re-verify the work lists against the block-CSR.  Returns "" or an error.
 std::string check_layout(const pf_layout &L);

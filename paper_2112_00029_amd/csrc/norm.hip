@@ -1,0 +1,317 @@
+// Layer normalisation of token rows, forward and backward.
+//
+//   n = (x - mean) rstd,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+//   y = n o w + b
+//   dx = rstd (g - mean(g) - n mean(g o n)) + dR,  g = dy o w
+//   dw = column sums of dy o n,  db = column sums of dy
+//
+// Every element is read once and written once (the backward reads two or three
+// tensors): memory is the bound.  A row lives in the registers of TPR threads, up
+// to 16 elements each, so that mean, variance and output need no second read; the
+// sums cross the wave by DPP and the waves of a row through LDS, one barrier a
+// sum.  Rows of at most 1024 elements take one wave and no barrier.  A workgroup
+// walks over rows (its weights stay in registers, and in the backward its fp32
+// sums of dw and db); the next row's loads are issued before the present row is
+// worked on.  The backward's workgroups leave their sums as one row of fp32
+// partials each, added in order by a second launch: no atomics, so the same call
+// gives the same bits.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "pf_io.h"
+#include "pf_launch.h"
+
+namespace pf {
+namespace {
+
+constexpr int kEPT = 16;  // elements of a row per thread, at most
+
+// A row's raw chunks of this thread: chunk c covers columns (c TPR + i) V ...
+template <typename T, int V, int C, int TPR>
+__device__ __forceinline__ void load_row(const T *p, int N, int i, Raw<T, V> (&r)[C]) {
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * TPR + i) * V;
+    r[c] = col < N ? ld_raw<T, V>(p + col) : zero_raw<T, V>();
+  }
+}
+
+template <typename T, int V, int C, int TPR>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(NormArgs a) {
+  constexpr int BT = TPR < 256 ? 256 : TPR, RPB = BT / TPR;  // threads, rows at a time
+  __shared__ float box[2][2 * (BT / 64)];
+  const int i = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+  const int N = (int)a.N;
+  const T *X = (const T *)a.X;
+  T *Y = (T *)a.Y;
+  const float inv = 1.0f / (float)N;
+  Raw<T, V> w[C], b[C];
+  if (a.weight) load_row<T, V, C, TPR>((const T *)a.weight, N, i, w);
+  if (a.bias) load_row<T, V, C, TPR>((const T *)a.bias, N, i, b);
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  Raw<T, V> x[C], nx[C];
+  int64_t t = (int64_t)blockIdx.x * RPB + slot;
+  if (t < a.T) load_row<T, V, C, TPR>(X + t * a.ldx, N, i, x);
+  for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < a.T; t0 += step, t += step) {
+    const bool live = t < a.T;
+    if (t + step < a.T) load_row<T, V, C, TPR>(X + (t + step) * a.ldx, N, i, nx);
+    // Mean; then sums of x - mean and its square: the first corrects the mean's
+    // own rounding, which rows far from zero would show.
+    float d[C][V], s1[1] = {0.f}, s2[2] = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      unpack<T, V>(x[c], d[c]);
+#pragma unroll
+      for (int e = 0; e < V; ++e) s1[0] += d[c][e];
+    }
+    group_sum<TPR, 1>(s1, box[0]);
+    const float m0 = s1[0] * inv;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const bool in = (c * TPR + i) * V < N;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        d[c][e] = in ? d[c][e] - m0 : 0.f;
+        s2[0] += d[c][e];
+        s2[1] = __builtin_fmaf(d[c][e], d[c][e], s2[1]);
+      }
+    }
+    group_sum<TPR, 2>(s2, box[1]);
+    const float m1 = s2[0] * inv;
+    const float var = fmaxf(__builtin_fmaf(-m1, m1, s2[1] * inv), 0.f);
+    // (fmaxf drops a NaN: the sum of squares still carries it.)
+    const float rstd = 1.0f / sqrtf((s2[1] != s2[1] ? s2[1] : var) + a.eps);
+    if (live) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int col = (c * TPR + i) * V;
+        float y[V], f[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = (d[c][e] - m1) * rstd;
+        if (a.weight) {
+          unpack<T, V>(w[c], f);
+#pragma unroll
+          for (int e = 0; e < V; ++e) y[e] *= f[e];
+        }
+        if (a.bias) {
+          unpack<T, V>(b[c], f);
+#pragma unroll
+          for (int e = 0; e < V; ++e) y[e] += f[e];
+        }
+        if (col < N) st_raw<T, V>(Y + t * a.ldy + col, pack<T, V>(y));
+      }
+      if (i == 0) {
+        if (a.mean) a.mean[t] = m0 + m1;
+        if (a.rstd) a.rstd[t] = rstd;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) x[c] = nx[c];
+  }
+}
+
+template <typename T, int V, int C, int TPR>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormArgs a) {
+  constexpr int BT = TPR < 256 ? 256 : TPR, RPB = BT / TPR;
+  __shared__ float box[2][2 * (BT / 64)];
+  __shared__ float red[RPB > 1 ? (RPB - 1) * TPR * V * C : 1];
+  const int i = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+  const int N = (int)a.N;
+  const T *X = (const T *)a.X, *dY = (const T *)a.dY, *dR = (const T *)a.dR;
+  T *dX = (T *)a.dX;
+  const float inv = 1.0f / (float)N;
+  Raw<T, V> w[C];
+  if (a.weight) load_row<T, V, C, TPR>((const T *)a.weight, N, i, w);
+  float dw[C][V] = {}, db[C][V] = {};
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  // (1024 threads leave 128 registers each: no room for a second row.)
+  constexpr bool AHEAD = TPR < 1024;
+  Raw<T, V> x[C], g[C], nx[C], ng[C];
+  float mean = 0.f, rstd = 0.f, nmean = 0.f, nrstd = 0.f;
+  int64_t t = (int64_t)blockIdx.x * RPB + slot;
+  auto fetch = [&](int64_t r, Raw<T, V> (&xx)[C], Raw<T, V> (&gg)[C], float &m, float &s)
+                   __attribute__((always_inline)) {
+    load_row<T, V, C, TPR>(X + r * a.ldx, N, i, xx);
+    load_row<T, V, C, TPR>(dY + r * a.lddy, N, i, gg);
+    m = a.mean_in[r];
+    s = a.rstd_in[r];
+  };
+  if (AHEAD && t < a.T) fetch(t, x, g, mean, rstd);
+  int buf = 0;
+  for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < a.T; t0 += step, t += step) {
+    const bool live = t < a.T;
+    if (!AHEAD && live) fetch(t, x, g, mean, rstd);
+    if (AHEAD && t + step < a.T) fetch(t + step, nx, ng, nmean, nrstd);
+    Raw<T, V> r[C];
+    if (dR && live) load_row<T, V, C, TPR>(dR + t * a.lddr, N, i, r);
+    float s[2] = {0.f, 0.f};
+    // n of a chunk (zero past the row) and dy; formed again after the sums, which
+    // costs less than the registers that would keep them.
+    auto norm_of = [&](int c, float (&n)[V], float (&q)[V]) __attribute__((always_inline)) {
+      const bool in = (c * TPR + i) * V < N;
+      unpack<T, V>(x[c], n);
+      unpack<T, V>(g[c], q);
+#pragma unroll
+      for (int e = 0; e < V; ++e) n[e] = in ? (n[e] - mean) * rstd : 0.f;
+    };
+    if (live) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float n[V], q[V], f[V];
+        norm_of(c, n, q);
+        if (a.weight) unpack<T, V>(w[c], f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          dw[c][e] = __builtin_fmaf(q[e], n[e], dw[c][e]);
+          db[c][e] += q[e];
+          if (a.weight) q[e] *= f[e];
+          s[0] += q[e];
+          s[1] = __builtin_fmaf(q[e], n[e], s[1]);
+        }
+      }
+    }
+    // Boxes in turn: a group writes one while others still read the last.
+    group_sum<TPR, 2>(s, box[buf]);
+    buf ^= 1;
+    if (live) {
+      const float c1 = s[0] * inv, c2 = s[1] * inv;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int col = (c * TPR + i) * V;
+        float n[V], y[V], f[V];
+        norm_of(c, n, y);
+        if (a.weight) unpack<T, V>(w[c], f);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          y[e] = rstd * ((a.weight ? y[e] * f[e] : y[e]) - __builtin_fmaf(n[e], c2, c1));
+        if (dR) {
+          unpack<T, V>(r[c], f);
+#pragma unroll
+          for (int e = 0; e < V; ++e) y[e] += f[e];
+        }
+        if (col < N) st_raw<T, V>(dX + t * a.lddx + col, pack<T, V>(y));
+      }
+    }
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        x[c] = nx[c];
+        g[c] = ng[c];
+      }
+      mean = nmean;
+      rstd = nrstd;
+    }
+  }
+  if (!a.partials) return;
+  // The workgroup's sums: its row slots in order, dw then db.
+  auto leave = [&](float (&v)[C][V], float *out, bool second) __attribute__((always_inline)) {
+    if constexpr (RPB > 1) {
+      if (second) __syncthreads();
+      if (slot) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int e = 0; e < V; ++e) red[(((slot - 1) * C + c) * V + e) * TPR + i] = v[c][e];
+      }
+      __syncthreads();
+      if (slot) return;
+#pragma unroll
+      for (int k = 0; k < RPB - 1; ++k)
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[c][e] += red[((k * C + c) * V + e) * TPR + i];
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TPR + i) * V;
+      if (col < N) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[col + e] = v[c][e];
+      }
+    }
+  };
+  float *P = a.partials + (int64_t)blockIdx.x * 2 * N;
+  leave(dw, P, false);
+  leave(db, P + N, true);
+}
+
+// Column sums of the partials [parts][2 N] into dw and db: 16 columns a workgroup,
+// 16 threads a column every 16th part each, added in order.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_sum_kernel(NormArgs a) {
+  __shared__ float red[256];
+  const int64_t col = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15), n2 = 2 * a.N;
+  const int q = threadIdx.x >> 4;
+  float s = 0.f;
+  if (col < n2) {
+#pragma unroll 4
+    for (int p = q; p < a.parts; p += 16) s += a.partials[(int64_t)p * n2 + col];
+  }
+  red[threadIdx.x] = s;
+  __syncthreads();
+  if (q || col >= n2) return;
+  for (int p = 1; p < 16; ++p) s += red[p * 16 + threadIdx.x];
+  T *out = (T *)(col < a.N ? a.dweight : a.dbias);
+  if (out) down(out[col < a.N ? col : col - a.N], s);
+}
+
+// f(V, C, TPR) of a plan.
+template <typename T, typename F>
+bool norm_pick(const NormArgs &a, F f) {
+  constexpr int VW = 16 / sizeof(T);
+  auto tpr = [&](auto v, auto c) -> bool {
+    switch (a.tpr) {
+      case 64: f(v, c, std::integral_constant<int, 64>{}); return true;
+      case 128: f(v, c, std::integral_constant<int, 128>{}); return true;
+      case 256: f(v, c, std::integral_constant<int, 256>{}); return true;
+      case 512: f(v, c, std::integral_constant<int, 512>{}); return true;
+      case 1024: f(v, c, std::integral_constant<int, 1024>{}); return true;
+    }
+    return false;
+  };
+  if ((int64_t)a.tpr * a.chunks * a.vec < a.N) return false;
+  if (a.vec == 1) return a.chunks == kEPT && tpr(std::integral_constant<int, 1>{}, std::integral_constant<int, kEPT>{});
+  if (a.vec != VW) return false;
+  if (a.chunks == 1) return tpr(std::integral_constant<int, VW>{}, std::integral_constant<int, 1>{});
+  if (a.chunks == 2) return tpr(std::integral_constant<int, VW>{}, std::integral_constant<int, 2>{});
+  if constexpr (VW == 4)
+    if (a.chunks == 4) return tpr(std::integral_constant<int, VW>{}, std::integral_constant<int, 4>{});
+  return false;
+}
+
+template <typename T>
+hipError_t norm_fwd(const NormArgs &a, hipStream_t s) {
+  const bool ok = norm_pick<T>(a, [&](auto v, auto c, auto t) {
+    constexpr int V = decltype(v)::value, C = decltype(c)::value, TPR = decltype(t)::value;
+    launch_kernel(norm_fwd_kernel<T, V, C, TPR>, dim3((unsigned)a.parts), dim3(std::max(256, TPR)), s, a);
+  });
+  return ok ? hipGetLastError() : hipErrorInvalidValue;
+}
+template <typename T>
+hipError_t norm_bwd(const NormArgs &a, hipStream_t s) {
+  const bool ok = norm_pick<T>(a, [&](auto v, auto c, auto t) {
+    constexpr int V = decltype(v)::value, C = decltype(c)::value, TPR = decltype(t)::value;
+    launch_kernel(norm_bwd_kernel<T, V, C, TPR>, dim3((unsigned)a.parts), dim3(std::max(256, TPR)), s, a);
+  });
+  return ok ? hipGetLastError() : hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_norm_fwd(int dtype, const NormArgs &a, hipStream_t s) {
+  return dtype == 0 ? norm_fwd<bf16_t>(a, s) : norm_fwd<float>(a, s);
+}
+hipError_t launch_norm_bwd(int dtype, const NormArgs &a, hipStream_t s) {
+  return dtype == 0 ? norm_bwd<bf16_t>(a, s) : norm_bwd<float>(a, s);
+}
+hipError_t launch_norm_sum(int dtype, const NormArgs &a, hipStream_t s) {
+  const unsigned grid = (unsigned)((2 * a.N + 15) / 16);
+  if (dtype == 0) launch_kernel(norm_sum_kernel<bf16_t>, dim3(grid), dim3(256), s, a);
+  else launch_kernel(norm_sum_kernel<float>, dim3(grid), dim3(256), s, a);
+  return hipGetLastError();
+}
+
+}  // namespace pf

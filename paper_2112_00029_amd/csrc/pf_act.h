@@ -146,6 +146,69 @@ __device__ __forceinline__ void act_apply(int act, float (&v)[N]) {
   }
 }
 
+// f[i] = act(x[i]), d[i] = act'(x[i]); the two share their exponentials.
+template <typename T>
+__device__ __forceinline__ void act_sigmoid_both(float x, float y, float dy, float &f, float &d) {
+  float s, c;
+  act_sigmoid<T>(y, s, c);
+  f = x * s;
+  d = __builtin_fmaf(x * s * c, dy, s);
+}
+template <typename T, int N>
+__device__ __forceinline__ void act_both(int act, const float (&x)[N], float (&f)[N], float (&d)[N]) {
+  switch (act) {
+    case kActGelu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        if constexpr (sizeof(T) == 2) {
+          const float v = x[e], a = fabsf(__builtin_amdgcn_fmed3f(v, -1e4f, 1e4f));
+          const float tail = normal_tail_bf16(a);
+          f[e] = __builtin_fmaf(-a, tail, v < 0.f ? 0.f : v);
+          d[e] = __builtin_fmaf(v * 0.39894228040143268f, __builtin_amdgcn_exp2f(v * v * -0.72134752f),
+                                v < 0.f ? tail : 1.0f - tail);
+        } else {
+          f[e] = act_gelu<T>(x[e]);
+          d[e] = act_gelu_grad<T>(x[e]);
+        }
+      }
+      break;
+    case kActGeluTanh:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        if constexpr (sizeof(T) == 2) {
+          // (The clamp as in act_gelu_tanh_grad; s has its limits there.)
+          const float v = x[e], z = __builtin_amdgcn_fmed3f(v, -16.f, 16.f), z2 = z * z;
+          float s, c;
+          act_sigmoid<T>(kTanh2k * __builtin_fmaf(kTanhC * z, z2, z), s, c);
+          f[e] = v * s;
+          d[e] = __builtin_fmaf(z * s * c, kTanh2k * __builtin_fmaf(3 * kTanhC, z2, 1.0f), s);
+        } else {
+          f[e] = act_gelu_tanh<T>(x[e]);
+          d[e] = act_gelu_tanh_grad<T>(x[e]);
+        }
+      }
+      break;
+    case kActSilu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) act_sigmoid_both<T>(x[e], x[e], 1.0f, f[e], d[e]);
+      break;
+    case kActRelu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        f[e] = x[e] < 0.f ? 0.f : x[e];
+        d[e] = x[e] > 0.f ? 1.f : 0.f;
+      }
+      break;
+    default:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        f[e] = x[e];
+        d[e] = 1.f;
+      }
+      break;
+  }
+}
+
 // v[i] *= act'(x[i]).
 template <typename T, int N>
 __device__ __forceinline__ void act_grad_apply(int act, float (&v)[N], const float (&x)[N]) {

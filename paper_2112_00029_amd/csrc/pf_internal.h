@@ -47,7 +47,10 @@ struct TNItem {
 // Epilogues of the NT kernels (NTArgs::epi).  kEpiGelu: GELU of the forward
 // (C2 = the pre-activation, C = gelu) or, for backward-data, GELU' of aux.
 // kEpiAct (forward only): z = sum + bias, C2 (if not null) = z, C = aux + act(z).
-constexpr int kEpiNone = 0, kEpiGelu = 1, kEpiAct = 2;
+// kEpiGated (forward on a gated layout's tiles, whose block rows 2 p and 2 p + 1 are
+// the gate and the other factor of one output block): z = sum + bias, C2 (if not
+// null, row stride ldc2) = z, C = act(z gate) z other, half as wide.
+constexpr int kEpiNone = 0, kEpiGelu = 1, kEpiAct = 2, kEpiGated = 3;
 // Activations (pf_activation).
 constexpr int kActNone = 0, kActGelu = 1, kActGeluTanh = 2, kActSilu = 3, kActRelu = 4;
 
@@ -68,10 +71,11 @@ struct NTArgs {
   void *C;              // T x ldc output
   int64_t ldc;
   void *C2;             // GELU forward: pre-activation output
+  int64_t ldc2;         // kEpiGated: its row stride
   const void *aux;      // GELU backward: pre-activation input; kEpiAct: residual or null
   int epi;              // kEpi*
-  const void *bias;     // kEpiAct: N elements or null
-  int act;              // kEpiAct: kAct*
+  const void *bias;     // kEpiAct, kEpiGated: one element per row of B, or null
+  int act;              // kEpiAct, kEpiGated: kAct*
   int64_t M;            // tokens
   const NTTile *tiles;  // null in dense mode
   int ntiles;           // output column tiles (dense mode: ceil(nblk / G))
@@ -319,6 +323,58 @@ struct ActBwdArgs {
 };
 hipError_t launch_act_bwd(int dtype, const ActBwdArgs &a, hipStream_t s);
 hipError_t launch_act_dbias(int dtype, const ActBwdArgs &a, hipStream_t s);
+
+// Way back through the gated product (gated.hip): cw chunks of 16 bytes of H's
+// columns per workgroup (a power of two, at most 64), `groups` workgroups across
+// them, nparts parts of rows_per_part rows.  b: columns of a block.  With nparts >
+// 1 and a dbias the sums go to partials [nparts][2 N], which launch_act_dbias adds.
+struct GatedBwdArgs {
+  const void *dH, *Z;
+  void *dZ, *dbias;
+  float *partials;
+  int64_t T, N, rows_per_part;
+  int b, act, cw, groups, nparts;
+  int stream;  // store dZ past the caches
+};
+hipError_t launch_gated_bwd(int dtype, const GatedBwdArgs &a, hipStream_t s);
+
+// Layer normalisation (norm.hip): tpr threads per row, `chunks` chunks of `vec`
+// elements each; `parts` workgroups.  The backward's leave partials [parts][2 N]
+// (dw, db), which launch_norm_sum adds.
+struct NormArgs {
+  const void *X, *weight, *bias, *dY, *dR;
+  void *Y, *dX, *dweight, *dbias;
+  float *mean, *rstd;
+  const float *mean_in, *rstd_in;
+  float *partials;
+  int64_t T, N, ldx, ldy, lddy, lddr, lddx;
+  float eps;
+  int tpr, vec, chunks, parts;
+};
+constexpr int64_t kNormMaxN = 16384;
+hipError_t launch_norm_fwd(int dtype, const NormArgs &a, hipStream_t s);
+hipError_t launch_norm_bwd(int dtype, const NormArgs &a, hipStream_t s);
+hipError_t launch_norm_sum(int dtype, const NormArgs &a, hipStream_t s);
+
+// Norm and scaling of many gradients (grads.hip).
+constexpr int kGradChunk = 8192;  // elements of a chunk, at most
+constexpr int kGradSrcF32 = 1, kGradDstF32 = 2;
+struct GradChunk {
+  uint64_t src, dst;  // addresses
+  int32_t n, types;   // types: kGrad*F32, bf16 without
+};
+struct GradArgs {
+  const GradChunk *chunks;
+  int nchunk;
+  double *partials;  // one sum of squares per workgroup of launch_grad_sumsq
+  int nparts;
+  double *sumsq;     // total and norm, or null
+  float *norm;
+  float max_norm;
+};
+hipError_t launch_grad_sumsq(const GradArgs &a, hipStream_t s);
+hipError_t launch_grad_total(const GradArgs &a, hipStream_t s);
+hipError_t launch_grad_scale(const GradArgs &a, int grid, hipStream_t s);
 
 // Attention with a relative position bias (relpos.hip).  A tensor is rows of 64
 // contiguous bf16 elements, strides in elements.

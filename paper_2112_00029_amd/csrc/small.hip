@@ -14,6 +14,10 @@
 // stages in flight before the first wait); the waves' 32 x 32 sums are added
 // through LDS in wave order (deterministic), and the epilogue (GELU, GELU',
 // mixing weight) is applied once.
+//
+// On a gated layout a workgroup owns a slice of both blocks of a pair: its first
+// half of the waves split the gate's K list, the second half the other factor's,
+// and the epilogue multiplies the two sums.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -44,7 +48,8 @@ __device__ __forceinline__ f32x4 get4(const float *p) { return *(const f32x4 *)p
 
 // T: bf16 or float storage.  NH: sub-blocks per step (2 for bf16 blocks of 32,
 // half a 128-byte step each).  BKN: B read as [k][n].  EPI: 0 none, 1 GELU
-// forward, 2 GELU backward, 3 bias, activation and residual (kEpiAct).
+// forward, 2 GELU backward, 3 bias, activation and residual (kEpiAct), 4 bias,
+// activation and product of a pair (kEpiGated).
 template <typename T, int NH, bool BKN, bool DENSE, int EPI, int NW>
 __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   constexpr int ES = sizeof(T), KW = 128 / NH / ES;  // K width of a sub-block
@@ -53,10 +58,12 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   constexpr int SUB = 4096 / NH;                     // bytes of an A or B sub-block
   constexpr int WPS = SUB / 1024;                    // 1 KiB copies per sub-block
   constexpr int DPS = 2 * NH * WPS;                  // copies per wave and step (8)
+  constexpr int KWV = EPI == 4 ? NW / 2 : NW;        // waves that split one K list
   const NTArgs &n = a.nt;
 
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = w / KWV, wk = w % KWV;  // (KWV < NW: factor of the pair)
   const int bid = xcd_remap(blockIdx.x, gridDim.x);
   const int mtiles = (int)((n.M + 31) / 32);
   const int mt = bid % mtiles, cs = bid / mtiles;  // token tiles of a slice adjacent
@@ -71,8 +78,9 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
     c0 = cs % sl * 32;
   } else {
     const int o = cs / sl;
-    const NTTile *tile = n.tiles + o / a.G;
-    g = o % a.G;
+    const int G = EPI == 4 ? a.G / 2 : a.G;
+    const NTTile *tile = n.tiles + o / G;
+    g = EPI == 4 ? 2 * (o % G) + half : o % G;
     c0 = cs % sl * 32;
     if (g >= ld_meta(&tile->g)) return;
     nsteps = ld_meta(&tile->nsteps);
@@ -95,7 +103,8 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   // columns of one token row.  Its pre-activations are loaded up front.
   const int il = threadIdx.x & 63, ig = threadIdx.x >> 6;
   const int64_t et = m0 + (il & 31);
-  const int64_t eoff = et * n.ldc + col0 + ig * 8 + (il >> 5) * 4;
+  const int ec = ig * 8 + (il >> 5) * 4;
+  const int64_t eoff = et * n.ldc + col0 + ec;
   const bool elive = threadIdx.x < 256 && et < n.M;
   // (EPI 3: its residual and bias.)
   f32x4 aux = {0.f, 0.f, 0.f, 0.f}, bz = {0.f, 0.f, 0.f, 0.f};
@@ -103,8 +112,17 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
     if (elive) aux = get4((const T *)n.aux + eoff);
   if constexpr (EPI == 3) {
     if (elive && n.aux) aux = get4((const T *)n.aux + eoff);
-    if (elive && n.bias) bz = get4((const T *)n.bias + col0 + ig * 8 + (il >> 5) * 4);
+    if (elive && n.bias) bz = get4((const T *)n.bias + col0 + ec);
   }
+  // (EPI 4: the two biases.)  Output block ob of the gate is 2 i, the pair's i.
+  f32x4 bu = {0.f, 0.f, 0.f, 0.f};
+  const int64_t zcol = ((int64_t)(ob & ~1) << lb) + c0 + ec;  // the gate's column of Z
+  const int64_t hcol = ((int64_t)(ob >> 1) << lb) + c0 + ec;
+  if constexpr (EPI == 4)
+    if (elive && n.bias) {
+      bz = get4((const T *)n.bias + zcol);
+      bu = get4((const T *)n.bias + zcol + blk);
+    }
 
   // Lane part of the copies.  Rows of 8 chunks are swizzled by row pair (two
   // variants: even / odd windows), rows of 4 by groups of 4 rows; a [k][n]
@@ -122,7 +140,7 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   const uint32_t a_row = (uint32_t)(lane / CPRA), b_row = (uint32_t)(lane / CPRB);
 
   auto issue = [&](int i, uint8_t *da, uint8_t *db) __attribute__((always_inline)) {
-    const int s = w + i * NW;
+    const int s = wk + i * KWV;
     sfor<NH>([&](auto h) __attribute__((always_inline)) {
       const int k0 = __builtin_amdgcn_readfirstlane((s * NH + h) * KW);
       const int c = k0 >> lb, kk = k0 & (blk - 1);
@@ -191,7 +209,7 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   // and columns (e / 4) * 8 + (l / 32) * 4 + e % 4.
   auto compute = [&](int i, auto j, const uint8_t *da, const uint8_t *db) __attribute__((always_inline)) {
     f32x16 &sum = acc[decltype(j)::value % NACC];
-    const int s = w + i * NW;
+    const int s = wk + i * KWV;
     sfor<NH>([&](auto h) __attribute__((always_inline)) {
       if (scale && (s * NH + h) * KW >= kswitch) rescale();
       if constexpr (ES == 2) {
@@ -225,7 +243,7 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
 
   // Each wave on its own: two steps in flight, a stage refilled as soon as
   // its reads have returned.  Steps past the end copy nothing and add zeros.
-  const int steps = (total + NW - 1) / NW;
+  const int steps = (total + KWV - 1) / KWV;
   sfor<2>([&](auto j) __attribute__((always_inline)) { issue(j, stage_a(j), stage_b(j)); });
   for (int i = 0; i < steps; i += 2) {
     sfor<2>([&](auto j) __attribute__((always_inline)) {
@@ -249,9 +267,30 @@ __global__ __launch_bounds__(64 * NW) void small_kernel(SmallArgs a) {
   if (!elive) return;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int ww = 0; ww < NW; ++ww)
+  for (int ww = 0; ww < KWV; ++ww)
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] += red[ww * 1024 + (ig * 4 + q) * 64 + il];
+  if constexpr (EPI == 4) {
+    float u[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ww = KWV; ww < NW; ++ww)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) u[q] += red[ww * 1024 + (ig * 4 + q) * 64 + il];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v[q] = (n.mix ? v[q] * n.mix_out : v[q]) + bz[q];
+      u[q] = (n.mix ? u[q] * n.mix_out : u[q]) + bu[q];
+    }
+    if (n.C2) {
+      put4((T *)n.C2 + et * n.ldc2 + zcol, v);
+      put4((T *)n.C2 + et * n.ldc2 + zcol + blk, u);
+    }
+    act_apply<T>(n.act, v);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] *= u[q];
+    put4((T *)n.C + et * n.ldc + hcol, v);
+    return;
+  }
   if (n.mix) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] *= n.mix_out;
@@ -287,6 +326,10 @@ hipError_t small_go(const SmallArgs &a, int64_t grid, bool deep, hipStream_t s) 
 
 template <typename T, int NH, bool BKN>
 hipError_t small_epi(const SmallArgs &a, int64_t grid, bool deep, hipStream_t s) {
+  if (a.nt.epi == kEpiGated) {
+    if constexpr (BKN) return hipErrorInvalidValue;
+    else return small_go<T, NH, BKN, false, 4>(a, grid, deep, s);
+  }
   if (a.nt.epi == kEpiAct) {
     if constexpr (BKN) return hipErrorInvalidValue;
     else return small_go<T, NH, BKN, false, 3>(a, grid, deep, s);
@@ -302,11 +345,15 @@ hipError_t launch_small(int dtype, int blk, int G, bool b_kn, int kmax, const NT
   SmallArgs a{nt, G, 0};
   while ((1 << a.log2_blk) < blk) ++a.log2_blk;
   if (blk < 32 || (1 << a.log2_blk) != blk) return hipErrorInvalidValue;
-  const int64_t slices = nt.dense ? (int64_t)nt.dense_nblk * (blk / 32) : (int64_t)nt.ntiles * G * (blk / 32);
+  const bool gated = !nt.dense && nt.epi == kEpiGated;
+  if (gated && G % 2) return hipErrorInvalidValue;
+  const int64_t slices = nt.dense ? (int64_t)nt.dense_nblk * (blk / 32)
+                                  : (int64_t)nt.ntiles * (gated ? G / 2 : G) * (blk / 32);
   const int64_t grid = ((nt.M + 31) / 32) * slices;
   if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
   // Eight waves once four would have eight or more steps each.
-  const bool deep = (int64_t)kmax * blk * (dtype == 0 ? 2 : 4) >= 32 * 128;
+  // (A pair's lists are split by half of them.)
+  const bool deep = (int64_t)kmax * blk * (dtype == 0 ? 2 : 4) * (gated ? 2 : 1) >= 32 * 128;
   if (nt.dense) {
     if (dtype == 0) return hipErrorInvalidValue;
     return b_kn ? small_go<float, 1, true, true, 0>(a, grid, deep, s)

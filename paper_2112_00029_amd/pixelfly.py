@@ -113,6 +113,25 @@ _SIGS = {
     "pf_linear_act_bwd": (_i32, [_i32, _i64, _i64, _i32, _p, _p, _p, _p, _p, _sz, _p]),
     "pf_linear_act_workspace_bytes": (_sz, [_i32, _i64, _i64]),
     "pf_gelu_bwd": (_i32, [_i32, _i64, _p, _p, _p, _p]),
+    "pf_layout_create_gated": (_i32, [_i64, _i64, _i32, _i32, ctypes.POINTER(_p)]),
+    "pf_layout_create_gated_from_mask": (_i32, [_i32, _i32, _i32, _p, ctypes.POINTER(_p)]),
+    "pf_linear_gated_fwd": (_i32, [_p, _i32, _i64, _i32, _p, _p, _p, _p, _p, _i32, _p, _p, _p, _p, _sz,
+                                   _p]),
+    "pf_linear_gated_fwd_mixed": (_i32, [_p, _i32, _i64, _i32, _f32, _p, _p, _p, _p, _p, _i32, _p, _p,
+                                         _p, _p, _sz, _p]),
+    "pf_linear_gated_bwd": (_i32, [_i32, _i64, _i64, _i32, _i32, _p, _p, _p, _p, _p, _sz, _p]),
+    "pf_linear_gated_workspace_bytes": (_sz, [_i32, _i64, _i64]),
+    "pf_layernorm_fwd": (_i32, [_i32, _i64, _i64, _f32, _p, _i64, _p, _p, _p, _i64, _p, _p, _p]),
+    "pf_layernorm_bwd": (_i32, [_i32, _i64, _i64, _p, _i64, _p, _i64, _p, _p, _p, _p, _i64, _p, _i64,
+                                _p, _p, _p, _sz, _p]),
+    "pf_layernorm_workspace_bytes": (_sz, [_i32, _i64, _i64]),
+    "pf_grads_create": (_i32, [_i32, _p, ctypes.POINTER(_p)]),
+    "pf_grads_upload": (_i32, [_p, _p]),
+    "pf_grads_destroy": (None, [_p]),
+    "pf_grads_workspace_bytes": (_sz, [_p]),
+    "pf_grads_clip": (_i32, [_p, _f32, _p, _p, _sz, _p]),
+    "pf_grads_norm": (_i32, [_p, _p, _p, _p, _sz, _p]),
+    "pf_grads_scale": (_i32, [_p, _f32, _p, _p]),
     "pf_attn_fwd": (_i32, [_p, _i32, _i32, _i32, _i32, _f32, _p, _p, _p, _p, _p, _p]),
     "pf_attn_bwd": (_i32, [_p, _i32, _i32, _i32, _i32, _f32, _p, _p, _p, _p, _p, _p, _p, _p,
                            _p, _p, _sz, _p]),
@@ -266,6 +285,23 @@ def pf_layout_create_factor(n: int, b: int, k: int) -> Layout:
     return Layout(h.value)
 
 
+def pf_layout_create_gated(n_out: int, n_in: int, b: int, max_stride: int) -> Layout:
+    """Two n_out x n_in projections as one matrix of 2 n_out rows in blocks of b
+    that alternate gate, other factor."""
+    h = _p()
+    _check(_lib.pf_layout_create_gated(n_out, n_in, b, max_stride, ctypes.byref(h)))
+    return Layout(h.value)
+
+
+def pf_layout_create_gated_from_mask(nb_out: int, nb_in: int, b: int, block_mask) -> Layout:
+    m = np.ascontiguousarray(np.asarray(block_mask) != 0, dtype=np.uint8)
+    if m.shape != (nb_out, nb_in):
+        raise ValueError(f"mask shape {m.shape} != ({nb_out}, {nb_in})")
+    h = _p()
+    _check(_lib.pf_layout_create_gated_from_mask(nb_out, nb_in, b, m.ctypes.data_as(_p), ctypes.byref(h)))
+    return Layout(h.value)
+
+
 def pf_layout_create_butterfly(n: int, b: int, max_stride: int) -> Layout:
     h = _p()
     _check(_lib.pf_layout_create_butterfly(n, b, max_stride, ctypes.byref(h)))
@@ -407,6 +443,118 @@ def pf_linear_act_bwd(dtype, T, N, act, dY, Y_pre, dY_pre, dbias, workspace=None
 
 def pf_linear_act_workspace_bytes(dtype, T, N) -> int:
     return int(_lib.pf_linear_act_workspace_bytes(_dt(dtype), T, N))
+
+
+def pf_linear_gated_fwd(layout, dtype, T, r, X, Wblk, U, V, bias, act, H, Z, T_lr, workspace=None,
+                        ws_bytes=0, stream=None) -> None:
+    """act: PF_ACT_*; bias and Z may be None."""
+    _check(_lib.pf_linear_gated_fwd(layout.handle, _dt(dtype), T, r, _ptr(X), _ptr(Wblk), _ptr(U), _ptr(V),
+                                    _ptr(bias), act, _ptr(H), _ptr(Z), _ptr(T_lr), _ptr(workspace), ws_bytes,
+                                    _stream(stream)))
+
+
+def pf_linear_gated_fwd_mixed(layout, dtype, T, r, gamma, X, Wblk, U, V, bias, act, H, Z, T_lr,
+                              workspace=None, ws_bytes=0, stream=None) -> None:
+    _check(_lib.pf_linear_gated_fwd_mixed(layout.handle, _dt(dtype), T, r, float(gamma), _ptr(X), _ptr(Wblk),
+                                          _ptr(U), _ptr(V), _ptr(bias), act, _ptr(H), _ptr(Z), _ptr(T_lr),
+                                          _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_linear_gated_bwd(dtype, T, N, b, act, dH, Z, dZ, dbias, workspace=None, ws_bytes=0,
+                        stream=None) -> None:
+    _check(_lib.pf_linear_gated_bwd(_dt(dtype), T, N, b, act, _ptr(dH), _ptr(Z), _ptr(dZ), _ptr(dbias),
+                                    _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_linear_gated_workspace_bytes(dtype, T, N) -> int:
+    return int(_lib.pf_linear_gated_workspace_bytes(_dt(dtype), T, N))
+
+
+def pf_layernorm_fwd(dtype, T, N, eps, X, ldx, weight, bias, Y, ldy, mean=None, rstd=None,
+                     stream=None) -> None:
+    """Row strides ldx, ldy in elements; weight, bias, mean and rstd may be None."""
+    _check(_lib.pf_layernorm_fwd(_dt(dtype), T, N, eps, _ptr(X), ldx, _ptr(weight), _ptr(bias), _ptr(Y), ldy,
+                                 _ptr(mean), _ptr(rstd), _stream(stream)))
+
+
+def pf_layernorm_bwd(dtype, T, N, dY, lddy, X, ldx, weight, mean, rstd, dR, lddr, dX, lddx, dweight, dbias,
+                     workspace=None, ws_bytes=0, stream=None) -> None:
+    """dR: a gradient to add to dX, or None."""
+    _check(_lib.pf_layernorm_bwd(_dt(dtype), T, N, _ptr(dY), lddy, _ptr(X), ldx, _ptr(weight), _ptr(mean),
+                                 _ptr(rstd), _ptr(dR), lddr, _ptr(dX), lddx, _ptr(dweight), _ptr(dbias),
+                                 _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_layernorm_workspace_bytes(dtype, T, N) -> int:
+    return int(_lib.pf_layernorm_workspace_bytes(_dt(dtype), T, N))
+
+
+class Grads:
+    """Owner of a pf_grads* (destroyed with the object) and holder of the tensors
+    it names."""
+
+    def __init__(self, handle: int, tensors):
+        self.handle = handle
+        self.tensors = tensors
+
+    def __del__(self):
+        h, self.handle = getattr(self, "handle", None), None
+        if h and _lib is not None:
+            _lib.pf_grads_destroy(h)
+
+
+# pf_grad_tensor.
+_pack_grad = struct.Struct("PPqii").pack
+
+
+def pf_grads_create(tensors) -> Grads:
+    """tensors: gradients (scaled in place), or pairs (gradient, where its scaled
+    values go); contiguous float32 or bfloat16 tensors of one device."""
+    rows, keep = [], []
+    for i, t in enumerate(tensors):
+        src, dst = t if isinstance(t, (tuple, list)) else (t, t)
+        for x in (src, dst):
+            if x.dtype not in (torch.float32, torch.bfloat16) or not x.is_contiguous():
+                raise ValueError(f"gradient {i}: expected a contiguous float32 or bfloat16 tensor, got {x.dtype}"
+                                 f"{'' if x.is_contiguous() else ' with strides'}")
+            if keep and x.device != keep[0][0].device or x.device != src.device:
+                raise ValueError(f"gradient {i}: on {x.device}, the first on {(keep[0][0] if keep else src).device}")
+        if src.numel() != dst.numel():
+            raise ValueError(f"gradient {i}: {src.numel()} elements into {dst.numel()}")
+        keep.append((src, dst))
+        rows.append(_pack_grad(src.data_ptr(), dst.data_ptr(), src.numel(), _dt(src.dtype), _dt(dst.dtype)))
+    h = _p()
+    _check(_lib.pf_grads_create(len(rows), b"".join(rows) or None, ctypes.byref(h)))
+    return Grads(h.value, keep)
+
+
+def pf_grads_upload(grads, stream=None) -> None:
+    _check(_lib.pf_grads_upload(grads.handle, _stream(stream)))
+
+
+def pf_grads_destroy(grads) -> None:
+    h, grads.handle = grads.handle, None
+    if h:
+        _lib.pf_grads_destroy(h)
+
+
+def pf_grads_workspace_bytes(grads) -> int:
+    return int(_lib.pf_grads_workspace_bytes(grads.handle))
+
+
+def pf_grads_clip(grads, max_norm, norm=None, workspace=None, ws_bytes=0, stream=None) -> None:
+    """norm: one float32 on the device, or None."""
+    _check(_lib.pf_grads_clip(grads.handle, max_norm, _ptr(norm), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pf_grads_norm(grads, sumsq, norm, workspace=None, ws_bytes=0, stream=None) -> None:
+    """sumsq: one float64 on the device; it or norm may be None."""
+    _check(_lib.pf_grads_norm(grads.handle, _ptr(sumsq), _ptr(norm), _ptr(workspace), ws_bytes,
+                              _stream(stream)))
+
+
+def pf_grads_scale(grads, max_norm, sumsq, stream=None) -> None:
+    _check(_lib.pf_grads_scale(grads.handle, max_norm, _ptr(sumsq), _stream(stream)))
 
 
 def pf_gelu_bwd(dtype, n, dH, H_pre, dH_pre, stream=None) -> None:

@@ -1,0 +1,304 @@
+"""GPU parity of the gated layer (both projections, activation and product in one
+kernel) and of its way back, against the formulas in float64.
+
+Tolerances, element by element, derived from the arithmetic (the constants of
+tests/test_act_parity.py):
+  * Z as there: a rounding u = finfo(t).eps / 2, the rounded T_lr, fp32 sums;
+  * H = f(g) v with f the activation: g off by tg, v by tv, f evaluated within
+    own(g): |f(g)| tv + |v| (1.13 tg + own) + (1.13 tg + own) tv, one product in fp32,
+    one rounding;
+  * dZg = d v f'(g): f' within 3e-6 (GELU in bf16 1e-5), two fp32 products, one
+    rounding; dZu = d f(g) the same with own;
+  * dbias: T fp32 additions of the products, a rounding."""
+import numpy as np
+import pytest
+
+from tests._gpu_util import torch_cuda
+from tests.test_act_parity import ACTS, LIP, _act, _mask, _slope
+
+pytestmark = pytest.mark.gpu
+E24 = 2.0 ** -24
+
+
+def _own(dtype, act, z, ref):
+    return 1e-6 * (1 + z.abs()) + (3.1e-5 * ref.abs() if dtype == "bf16" and act == "gelu" else 0.0)
+
+
+class Gated:
+    """Inputs of a gated layer on the GPU and its exact pre-activations in fp64
+    (T x N/b x 2 x b)."""
+
+    def __init__(self, dtype, T, K, N, b, ms, r, seed=0, gamma=None, mask=None):
+        t = self.t = torch_cuda()
+        from paper_2112_00029_amd import pixelfly as pf
+        self.pf, self.dtype, self.T, self.K, self.N, self.b, self.r = pf, dtype, T, K, N, b, r
+        self.dt = t.bfloat16 if dtype == "bf16" else t.float32
+        self.u = t.finfo(self.dt).eps / 2
+        g = t.Generator(device="cuda").manual_seed(seed)
+        rnd = lambda shape, std: t.randn(shape, generator=g, device="cuda").mul_(std).to(self.dt)
+        m = _mask(N // b, K // b, ms) if mask is None else mask
+        i, j = np.nonzero(np.repeat(m, 2, axis=0))
+        fan = len(i) / (2 * N // b) * b
+        self.x, self.w = rnd((T, K), 1.0), rnd((len(i), b, b), fan ** -0.5)
+        self.U = rnd((2 * N, r), 0.5 * r ** -0.5) if r else None
+        self.V = rnd((r, K), K ** -0.5) if r else None
+        self.bias = rnd((2 * N,), 0.5)
+        self.L = (pf.pf_layout_create_gated(N, K, b, ms) if mask is None
+                  else pf.pf_layout_create_gated_from_mask(N // b, K // b, b, mask))
+        pf.pf_layout_upload(self.L)
+        W = t.zeros((2 * N // b, K // b, b, b), dtype=t.float64, device="cuda")
+        W[t.from_numpy(i).cuda(), t.from_numpy(j).cuda()] = self.w.double()
+        self.W = W = W.permute(0, 2, 1, 3).reshape(2 * N, K)
+        al, be = (1.0, 1.0) if gamma is None else (gamma, 1 - gamma)
+        x = self.x.double()
+        self.z = al * x @ W.t()
+        mag = al * x.abs() @ W.abs().t()
+        self.tol = t.zeros_like(self.z)
+        if r:
+            tl = x @ self.V.double().t()
+            self.z = self.z + be * tl @ self.U.double().t()
+            lr = be * tl.abs() @ self.U.double().abs().t()
+            mag = mag + lr
+            self.tol = self.tol + 1.01 * self.u * lr
+            tmag = x.abs() @ self.V.double().abs().t()
+            self.tol = self.tol + be * K * E24 * tmag @ self.U.double().abs().t()
+        self.tol = self.tol + (K + r + 4) * E24 * (mag + self.bias.double().abs())
+        self.ws_bytes = pf.pf_workspace_bytes(self.L, T, r, dtype)
+        self.ws = t.empty((max(self.ws_bytes, 256),), dtype=t.uint8, device="cuda")
+
+    def empty(self, cols):
+        return self.t.full((self.T, cols), float("nan"), dtype=self.dt, device="cuda")
+
+    def run(self, act, bias=True, pre=True, gamma=None, stream=None):
+        h, z = self.empty(self.N), self.empty(2 * self.N) if pre else None
+        tl = self.empty(self.r) if self.r else None
+        args = (self.x, self.w, self.U, self.V, self.bias if bias else None,
+                getattr(self.pf, "PF_ACT_" + act.upper()), h, z, tl, self.ws, self.ws_bytes, stream)
+        if gamma is None:
+            self.pf.pf_linear_gated_fwd(self.L, self.dtype, self.T, self.r, *args)
+        else:
+            self.pf.pf_linear_gated_fwd_mixed(self.L, self.dtype, self.T, self.r, gamma, *args)
+        return h, z, tl
+
+    def check(self, h, z, act, bias=True):
+        ref = self.z + self.bias.double() if bias else self.z
+        if z is not None:
+            bad = (z.double() - ref).abs() - (self.u * ref.abs() + self.tol * (1 + self.u))
+            assert not (bad > 0).any() and not z.isnan().any(), ("z", float(bad.max()))
+        pair = lambda x: x.view(self.T, self.N // self.b, 2, self.b).unbind(2)
+        g, v = pair(ref)
+        tg, tv = pair(self.tol)
+        f = _act(self.t, g, act)
+        df = LIP * tg + _own(self.dtype, act, g, f)
+        want = f * v
+        bound = self.u * want.abs() + (1 + self.u) * (f.abs() * tv + v.abs() * df + df * tv + 2 * E24 * want.abs())
+        bad = (h.double().view(want.shape) - want).abs() - bound
+        assert not (bad > 0).any() and not h.isnan().any(), ("h", act, float(bad.max()))
+
+
+# One for every kernel and tile the forward can run on: few tiles (bf16 and fp32,
+# all blocks, ragged rows, one token), 64- to 256-column tiles, tall and short-K
+# ones, 256 x 256 in bands, tiles that are not full.
+SHAPES = [
+    ("bf16", 1, 256, 512, 64, 4, 64), ("bf16", 33, 320, 416, 32, 8, 32), ("bf16", 8, 512, 256, 128, 2, 0),
+    ("bf16", 1, 4096, 512, 128, 32, 256), ("fp32", 1, 256, 512, 128, 2, 0),
+    ("fp32", 5, 256, 512, 64, 4, 64), ("fp32", 200, 224, 288, 32, 4, 32), ("fp32", 2048, 512, 1024, 32, 8, 32),
+    ("fp32", 2001, 512, 1024, 128, 4, 128), ("fp32", 1001, 512, 1024, 64, 4, 64), ("fp32", 1500, 512, 800, 32, 4, 0),
+    ("bf16", 1000, 768, 768, 32, 16, 96), ("bf16", 1000, 512, 2048, 128, 2, 0),
+    ("bf16", 1000, 1024, 4096, 64, 16, 128), ("bf16", 2100, 1024, 4096, 64, 16, 0),
+    ("bf16", 4100, 4096, 1024, 64, 16, 128), ("bf16", 2509, 2048, 4096, 32, 32, 64),
+    ("bf16", 2049, 1024, 4096, 128, 8, 256), ("bf16", 8200, 512, 512, 128, 2, 128),
+    ("bf16", 3000, 512, 832, 64, 4, 64), ("bf16", 2100, 512, 1184, 32, 4, 32), ("bf16", 700, 96, 1056, 32, 1, 0),
+    ("bf16", 4500, 1024, 1088, 32, 16, 32),
+]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(map(str, s)))
+def test_forward(shape):
+    lay = Gated(*shape)
+    for act in ACTS:
+        h, z, _ = lay.run(act)
+        lay.check(h, z, act)
+    h, z, _ = lay.run("silu", bias=False, pre=False)
+    lay.check(h, None, "silu", bias=False)
+
+
+@pytest.mark.parametrize("shape", [("bf16", 40, 256, 512, 64, 4, 64), ("bf16", 2100, 512, 1024, 64, 4, 64),
+                                   ("bf16", 2200, 512, 1024, 128, 4, 128), ("fp32", 70, 256, 512, 32, 4, 32),
+                                   ("fp32", 2000, 256, 1024, 128, 2, 128), ("bf16", 600, 512, 1024, 32, 4, 0)],
+                         ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("gamma", [0.0, 0.3, 1.0])
+def test_mixed(shape, gamma):
+    lay = Gated(*shape, gamma=gamma)
+    h, z, _ = lay.run("gelu_tanh", gamma=gamma)
+    lay.check(h, z, "gelu_tanh")
+
+
+def test_other_masks():
+    rng = np.random.default_rng(5)
+    for T, nbo, nbi, b in ((50, 7, 5, 32), (2300, 9, 6, 64), (2100, 5, 3, 128), (900, 13, 8, 32)):
+        m = rng.random((nbo, nbi)) < 0.4
+        m[np.arange(nbo), rng.integers(0, nbi, nbo)] = True
+        lay = Gated("bf16", T, nbi * b, nbo * b, b, 0, b, mask=m)
+        h, z, _ = lay.run("gelu")
+        lay.check(h, z, "gelu")
+
+
+@pytest.mark.parametrize("shape", [("bf16", 300, 256, 512, 32, 4, 32), ("bf16", 2500, 512, 1024, 128, 4, 128),
+                                   ("fp32", 300, 256, 512, 128, 2, 128)], ids=lambda s: "-".join(map(str, s)))
+def test_same_as_the_layer_it_is(shape):
+    """Z is what the plain forward gives on the same 2 N x K layout, whose other
+    calls serve the gated layer too."""
+    lay = Gated(*shape)
+    _, z, tl = lay.run("silu", bias=False)
+    y, t2 = lay.empty(2 * lay.N), lay.empty(lay.r)
+    lay.pf.pf_linear_fwd(lay.L, lay.dtype, lay.T, lay.r, lay.x, lay.w, lay.U, lay.V, y, t2, workspace=lay.ws,
+                         ws_bytes=lay.ws_bytes)
+    assert lay.t.equal(tl, t2)
+    assert not ((y.double() - z.double()).abs() > 2 * (lay.u * lay.z.abs() + 1.01 * lay.tol)).any()
+
+
+def test_rows_and_repeats():
+    """Rows past T and everything else around the outputs stay as they were;
+    repeat calls and another stream give the same bits."""
+    t = torch_cuda()
+    for shape in (("bf16", 45, 256, 512, 32, 4, 32), ("bf16", 2121, 512, 1024, 128, 4, 0),
+                  ("fp32", 1100, 256, 512, 64, 4, 0)):
+        lay = Gated(*shape)
+        T, N = lay.T, lay.N
+        big_h = t.full((T + 3, N), 7.0, dtype=lay.dt, device="cuda")
+        big_z = t.full((T + 3, 2 * N), 7.0, dtype=lay.dt, device="cuda")
+        h, z, tl = lay.run("silu")
+        lay.pf.pf_linear_gated_fwd(lay.L, lay.dtype, T, lay.r, lay.x, lay.w, lay.U, lay.V, lay.bias,
+                                   lay.pf.PF_ACT_SILU, big_h, big_z, tl, lay.ws, lay.ws_bytes)
+        assert t.equal(big_h[:T], h) and t.equal(big_z[:T], z)
+        assert bool((big_h[T:] == 7).all()) and bool((big_z[T:] == 7).all())
+        st = t.cuda.Stream()
+        st.wait_stream(t.cuda.current_stream())
+        h2, z2, _ = lay.run("silu", stream=st)
+        st.synchronize()
+        assert t.equal(h2, h) and t.equal(z2, z)
+
+
+def test_captured():
+    t = torch_cuda()
+    lay = Gated("bf16", 300, 256, 512, 64, 4, 64)
+    h, z, _ = lay.run("gelu")
+    out = {}
+    st = t.cuda.Stream()
+    g = t.cuda.CUDAGraph()
+    with t.cuda.graph(g, stream=st):
+        out["h"], out["z"], out["t"] = lay.run("gelu", stream=st)
+    for _ in range(3):
+        out["h"].fill_(3.0)
+        out["z"].fill_(3.0)
+        g.replay()
+        t.cuda.synchronize()
+        assert t.equal(out["h"], h) and t.equal(out["z"], z)
+
+
+# ---- way back ---------------------------------------------------------------
+
+def _bwd(t, dtype, T, N, b, act, dh, z, dbias=True, inplace=False):
+    from paper_2112_00029_amd import pixelfly as pf
+    wsb = pf.pf_linear_gated_workspace_bytes(dtype, T, N)
+    ws = t.full((max(wsb, 16),), 255, dtype=t.uint8, device="cuda")
+    dz = z.clone() if inplace else t.full_like(z, float("nan"))
+    db = t.full((2 * N,), float("nan"), dtype=z.dtype, device="cuda") if dbias else None
+    pf.pf_linear_gated_bwd(dtype, T, N, b, getattr(pf, "PF_ACT_" + act.upper()), dh, dz if inplace else z, dz, db,
+                           ws, wsb)
+    return dz, db
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,N,b", [(1, 32, 32), (3, 64, 64), (7, 128, 128), (33, 416, 32), (250, 832, 64),
+                                   (1000, 1152, 128), (4099, 256, 32), (2100, 4096, 64)])
+def test_backward(dtype, T, N, b):
+    t = torch_cuda()
+    dt = t.bfloat16 if dtype == "bf16" else t.float32
+    u = t.finfo(dt).eps / 2
+    g = t.Generator(device="cuda").manual_seed(T + N)
+    dh = t.randn((T, N), generator=g, device="cuda").to(dt)
+    z = (t.randn((T, 2 * N), generator=g, device="cuda") * 1.5).to(dt)
+    z.view(T, N // b, 2, b)[0, 0, :, :6] = t.tensor([0.0, -0.75, 9.0, -9.0, 30.0, -30.0], device="cuda").to(dt)
+    pair = lambda x: x.double().view(T, N // b, 2, b).unbind(2)
+    gate, other = pair(z)
+    d = dh.double().view(T, N // b, b)
+    for act in ACTS:
+        f, s = _act(t, gate, act), _slope(t, gate, act) if act != "none" else t.ones_like(gate)
+        slope_tol = 1e-5 if act == "gelu" and dtype == "bf16" else 3e-6
+        want = t.stack([d * other * s, d * f], 2).view(T, 2 * N)
+        tol = t.stack([(d * other).abs() * (slope_tol + 3 * E24 * s.abs()),
+                       d.abs() * (_own(dtype, act, gate, f) + 3 * E24 * f.abs())], 2).view(T, 2 * N)
+        dz, db = _bwd(t, dtype, T, N, b, act, dh, z)
+        bad = (dz.double() - want).abs() - (u * want.abs() + (1 + u) * tol)
+        assert not (bad > 0).any() and not dz.isnan().any(), (act, float(bad.max()))
+        col = want.sum(0)
+        tc = tol.sum(0) + T * E24 * (want.abs() + tol).sum(0)
+        bad = (db.double() - col).abs() - (u * col.abs() + (1 + u) * tc)
+        assert not (bad > 0).any() and not db.isnan().any(), ("dbias", act, float(bad.max()))
+        again, none = _bwd(t, dtype, T, N, b, act, dh, z, dbias=False, inplace=True)
+        assert none is None and t.equal(again, dz)
+        again, db2 = _bwd(t, dtype, T, N, b, act, dh, z)
+        assert t.equal(db, db2)
+
+
+def test_backward_large_and_masked_values():
+    """Gates far out, where a formula squares or exponentiates: no NaN, and the
+    limits of the activations."""
+    t = torch_cuda()
+    z = t.zeros((1, 64), device="cuda")
+    z[0, :8] = t.tensor([1e4, -1e4, 1e18, -1e18, 3e38, -3e38, 3000.0, -3000.0])
+    z[0, 32:] = 2.0
+    dh = t.ones((1, 32), device="cuda")
+    for dtype, dt in (("bf16", t.bfloat16), ("fp32", t.float32)):
+        for act in ("gelu", "gelu_tanh", "silu", "relu"):
+            zz = z.to(dt)
+            dz, _ = _bwd(t, dtype, 1, 32, 32, act, dh.to(dt), zz)
+            pos = zz[0, :8] > 0
+            assert not dz.isnan().any(), (dtype, act)
+            assert t.equal(dz[0, :8].float(), pos.float() * 2), (dtype, act, dz[0, :8])
+            big = dz[0, 32:40].float()
+            assert t.equal(big, t.where(pos, zz[0, :8].float(), t.zeros_like(big))), (dtype, act, big)
+
+
+def test_gradients_against_differences():
+    """The whole gated layer in fp32: dX, dW, dU, dV and dbias of L = <G, H>, against
+    central differences in fp64 along random directions."""
+    t = torch_cuda()
+    lay = Gated("fp32", 60, 128, 192, 32, 4, 32, seed=3)
+    pf, T, K, N, r = lay.pf, lay.T, lay.K, lay.N, lay.r
+    gen = t.Generator(device="cuda").manual_seed(8)
+    G = t.randn((T, N), generator=gen, device="cuda")
+    h, z, tl = lay.run("gelu")
+    dz, db = _bwd(t, "fp32", T, N, 32, "gelu", G, z)
+    S, dX = lay.empty(r), lay.empty(K)
+    dW, dU, dV = t.empty_like(lay.w), t.empty_like(lay.U), t.empty_like(lay.V)
+    pf.pf_linear_bwd_data(lay.L, "fp32", T, r, dz, lay.w, lay.U, lay.V, S, dX, workspace=lay.ws, ws_bytes=lay.ws_bytes)
+    pf.pf_linear_bwd_weight(lay.L, "fp32", T, r, dz, lay.x, tl, S, dW, dU, dV, lay.ws, lay.ws_bytes)
+    i, j = np.nonzero(np.repeat(_mask(N // 32, K // 32, 4), 2, axis=0))
+    ii, jj = t.from_numpy(i).cuda(), t.from_numpy(j).cuda()
+
+    def loss(x, w, U, V, bias):
+        W = t.zeros((2 * N // 32, K // 32, 32, 32), dtype=t.float64, device="cuda")
+        W[ii, jj] = w
+        zz = x @ W.permute(0, 2, 1, 3).reshape(2 * N, K).t() + (x @ V.t()) @ U.t() + bias
+        a, v = zz.view(T, N // 32, 2, 32).unbind(2)
+        return float((G.double().view(a.shape) * _act(t, a, "gelu") * v).sum())
+
+    at = [p.double() for p in (lay.x, lay.w, lay.U, lay.V, lay.bias)]
+    for k, grad in enumerate((dX, dW, dU, dV, db)):
+        way = t.randn(at[k].shape, generator=gen, device="cuda", dtype=t.float64)
+        way /= way.norm()
+        e = 1e-4
+        ends = []
+        for sgn in (1, -1):
+            p = list(at)
+            p[k] = p[k] + sgn * e * way
+            ends.append(loss(*p))
+        num = (ends[0] - ends[1]) / (2 * e)
+        got = float((grad.double() * way).sum())
+        # The differences' own error is of third order (below 1e-6 of the gradient's
+        # norm here); the kernels' fp32 sums of 60 .. 384 terms below 400 2^-24 of
+        # the terms' norm, taken ten times the gradient's.
+        assert abs(num - got) <= (1e-6 + 4000 * E24) * float(grad.double().norm()), (k, num, got)
