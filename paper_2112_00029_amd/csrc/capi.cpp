@@ -128,16 +128,47 @@ bool use_small_nt(int dtype, int blk, int G, int64_t M, int ntiles) {
   return use_small(dtype, blk, M, (int64_t)ntiles * G * (blk / 32));
 }
 
+// The gated forward's.  A workgroup of the small-product kernel takes a slice of both
+// blocks of a pair: T / 32 x N / 32 of them.  Small / tiles, us, by their number: b =
+// 32 13.1 / 14.4 (398: 10 x 12736), 15.3 / 13.3 (528: 113 x 4224), 15.8 / 12.8 (513: 599
+// x 864); b = 64 11.8 / 13.9 (366: 18 x 11712), 20.1 / 18.5 (520: 41 x 8320), 12.8 / 10.7
+// (576: 2304 x 256); b = 128 12.6 / 29.2 (240: 640 x 384), 24.6 / 35.2 (912: 100 x 7296),
+// 35.7 / 33.1 (1836: 269 x 6528); fp32 66 / 98 (644: 1456 x 448, K lists of 960), 55.5 /
+// 65.3 (952: 1070 x 896, 640), 35.8 / 33.4 (1300: 775 x 1664, 224).
+bool use_small_gated(int dtype, int blk, int G, int64_t M, int ntiles) {
+  const int64_t wg = (M + 31) / 32 * ntiles * (G / 2) * (blk / 32);
+  return wg <= (dtype != 0 ? 1280 : blk == 32 ? 384 : blk == 64 ? 512 : 1024);
+}
+// Tiles of 128 stacked columns: short K-steps for blocks of 32 with K lists up to 416,
+// 64-deep ones otherwise (2509 x 4096 b = 32, K 224, 30.5 / 33.5 us; 3712 x 9440, 192,
+// 65 / 81; 512 x 7776, 416, 26.0 / 30.3; 16384 x 16384, 480, 890 / 888 on 512 x 128 tiles,
+// which are no faster anywhere; b = 64: 2048 x 8704, 512, 62.5 / 56.8, 8192 x 11264, 384,
+// 267 / 247).  Pairs of 128-row blocks: 256 x 256 tiles, a workgroup per CU; or
+// 128 x 256, two per CU and about a tenth more time for the same work, where that
+// saves a round (4909 x 1664: 260 tiles or 507, 45.2 / 36.5 us).
+NTChoice gated_choose(int dtype, int blk, int G, int bm, int kmax, int64_t M, int ntiles) {
+  if (!ntd_width(dtype, blk, G)) return NTChoice{false, 0, bm, G * blk};
+  const int w = G * blk, k = kmax * blk;
+  if (w == 256) {
+    const int64_t full = ((M + 255) / 256 * ntiles + 255) / 256, half = ((M + 127) / 128 * ntiles + 511) / 512;
+    return blk == 128 && 11 * half < 10 * full ? NTChoice{true, pf::NTD_HALF, 128, w}
+                                               : NTChoice{true, pf::NTD_DEFAULT, 256, w};
+  }
+  if (w == 128) return NTChoice{true, blk == 32 && k <= 416 ? pf::NTD_SHORT_K : pf::NTD_DEFAULT, 128, w};
+  return nt_choose(dtype, blk, G, bm, kmax, M, ntiles, 1, false);
+}
+
 hipError_t nt_launch(pf_kernel_class kc, int dtype, int blk, int G, bool b_kn, int bm, int kmax,
                      const pf::NTArgs &a_in, hipStream_t s) {
   Timed t(kc, s);
-  // (A workgroup of the small-product kernel takes both blocks of a gated pair.)
   const bool gated = !a_in.dense && a_in.epi == pf::kEpiGated;
-  if (!a_in.dense && use_small_nt(dtype, blk, gated ? G / 2 : G, a_in.M, a_in.ntiles))
+  if (gated ? use_small_gated(dtype, blk, G, a_in.M, a_in.ntiles)
+            : !a_in.dense && use_small_nt(dtype, blk, G, a_in.M, a_in.ntiles))
     return pf::launch_small(dtype, blk, G, b_kn, kmax, a_in, s);
   pf::NTArgs a = a_in;
   a.band = nt_band(a.dense != 0, b_kn, a.ntiles);
-  const NTChoice c = nt_choose(dtype, blk, G, bm, kmax, a.M, a.ntiles, a.nsplit, a.dense != 0);
+  const NTChoice c = gated ? gated_choose(dtype, blk, G, bm, kmax, a.M, a.ntiles)
+                           : nt_choose(dtype, blk, G, bm, kmax, a.M, a.ntiles, a.nsplit, a.dense != 0);
   if (c.dma) return pf::launch_ntd(blk, G, b_kn, c.variant, a, s);
   return pf::launch_nt(dtype, blk, G, b_kn, bm, a, s);
 }
@@ -511,12 +542,19 @@ NTList fwd_list(const pf_layout *L, int dt, int64_t T) {
                 L->d_kcols_fwd, L->d_blks_fwd};
 }
 // Of the gated forward: pairs of 128-row blocks are 256 columns whatever the token
-// count.
-NTList gated_list(const pf_layout *L, int dt, int64_t T) {
-  if (L->b == 128)
+// count; others take the wide list for long K lists and four rounds of workgroups
+// (16384 x 16384, b = 64, K 704: 987 us, on 128 columns 1097; b = 32, 480: 860 / 890;
+// 4096 x 8192, b = 64, 448: 108 / 116; 8192 x 11264, 384: 255 / 247; 2048 x 8704, 512,
+// 544 workgroups: 65.8 / 56.8).
+NTList gated_list(const pf_layout *L, int dt, int64_t T, int32_t r) {
+  const bool wide = ntd_width(dt, L->b, L->G_fwd_w) && L->G_fwd_w * L->b == 256 &&
+                    (T + 255) / 256 * (int64_t)L->fwd_tiles_w.size() >= 1024 &&
+                    L->kmax_fwd * (int64_t)L->b + r >= 448;
+  if (L->b == 128 || wide)
     return NTList{true, L->G_fwd_w, (int)L->fwd_tiles_w.size(), L->kmax_fwd, L->d_fwd_tiles_w,
                   L->d_kcols_fwd_w, L->d_blks_fwd_w};
-  return fwd_list(L, dt, T);
+  return NTList{false, L->G_fwd, (int)L->fwd_tiles.size(), L->kmax_fwd, L->d_fwd_tiles,
+                L->d_kcols_fwd, L->d_blks_fwd};
 }
 NTList bwd_list(const pf_layout *L, int dt, int64_t T) {
   const bool wide = ntd_width(dt, L->b, L->G_bwd_w) && L->G_bwd_w * L->b == 256 && T >= PF_WIDE_MIN_T;
@@ -1191,7 +1229,7 @@ pf_status linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, c
     a.ldc2 = L->n_out;
   }
   a.M = T;
-  const NTList tl = gated ? gated_list(L, dt, T) : fwd_list(L, dt, T);
+  const NTList tl = gated ? gated_list(L, dt, T, r) : fwd_list(L, dt, T);
   a.tiles = tl.tiles;
   a.ntiles = tl.ntiles;
   a.kcols = tl.kcols;

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
   // places, of the other factor's, so that a lane holds both factors of its outputs.
   // Tiles of eight waves take 128 columns each: output rows of 128 bytes.
   constexpr bool GATED = EPI == 4;
-  constexpr int WTN = GATED && NW == 8 ? 128 : 64, WGN = BN / WTN, WGM = NW / WGN, WTM = BM / WGM;
+  constexpr int WTN = GATED && (NW == 8 || BN == 256) ? 128 : 64, WGN = BN / WTN, WGM = NW / WGN, WTM = BM / WGM;
   constexpr int TM = WTM / 32, TN = WTN / 32;
   // A region: NH sub-blocks of [BM][KW]; B region: G x NH pieces of [BLK][KW]
   // (NT) or [KW][BLK] (B read as [k][n]).
@@ -296,14 +296,36 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
     });
   };
 
-  f32x16 acc[TN][TM];
-  sfor<TN>([&](auto i) __attribute__((always_inline)) {
-    sfor<TM>([&](auto j) __attribute__((always_inline)) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  // Gated: column of Z where each run of 32 columns of the wave begins (-1: past
+  // the tile), the same in all lanes, and the biases of the lane's columns, which the
+  // sums start from (with a mixing weight, added at the end).
+  constexpr int HT = GATED ? TN / 2 : 1;
+  int64_t zc[GATED ? TN : 1];
+  u32x2 gb[GATED ? TN : 1][4];
+  auto load_bias = [&](bool on) __attribute__((always_inline)) {
+    if constexpr (GATED) {
+      sfor<TN>([&](auto tn) __attribute__((always_inline)) {
+        const bf16_t *p = (const bf16_t *)a.bias + zc[tn] + (lane >> 5) * 4;
+        sfor<4>([&](auto q) __attribute__((always_inline)) { gb[tn][q] = u32x2{0u, 0u}; });
+        if (on && zc[tn] >= 0)
+          sfor<4>([&](auto q) __attribute__((always_inline)) { gb[tn][q] = *(const u32x2 *)(p + q * 8); });
+      });
+    }
+  };
+  auto bias_at = [&](auto tn, int e) __attribute__((always_inline)) -> float {
+    const uint32_t x = gb[tn][e / 4][(e & 3) / 2];
+    return __uint_as_float(e & 1 ? x & 0xffff0000u : x << 16);
+  };
+  if constexpr (GATED) {
+    sfor<TN>([&](auto tn) __attribute__((always_inline)) {
+      const int h = wn * (WTN / 2) + tn % HT * 32;
+      const int g = 2 * (h / BLK) + tn / HT;
+      zc[tn] = g < g_valid ? (int64_t)ld_meta(&tile->out_blk[g]) * BLK + h % BLK : -1;
     });
-  });
+    load_bias(a.bias && !a.mix);
+  }
 
+  f32x16 acc[TN][TM];
   // Mixing weight: scale the kept-block sums once, at the first low-rank
   // K-block (virtual K index nsteps * BLK).
   const int kswitch = nsteps * BLK;
@@ -351,6 +373,15 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
   // copies of step t + NS - 1 go into the stage freed by step t - 1.
   sfor<NS - 1>([&](auto j) __attribute__((always_inline)) {
     if (j < total) issue(j, stage(j));
+  });
+  sfor<TN>([&](auto i) __attribute__((always_inline)) {
+    sfor<TM>([&](auto j) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if constexpr (GATED) acc[i][j][e] = bias_at(i, e);
+        else acc[i][j][e] = 0.f;
+      }
+    });
   });
   auto run = [&](auto mix) __attribute__((always_inline)) {
     auto compute = [&](Stage st, int t) __attribute__((always_inline)) {
@@ -416,79 +447,80 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
   if constexpr (GATED) {
     // Z = sums + biases stays in the accumulators; its rounded rows, then those of
     // act(gate) x other, pass through the staging area as below: units of 4
-    // columns, XOR-swizzled by row, read back as 16-byte chunks.
-    constexpr int HT = TN / 2;
-    auto gate_h = [&](int t) __attribute__((always_inline)) { return wn * (WTN / 2) + t * 32; };
-    auto blk_at = [&](int g) __attribute__((always_inline)) -> int {
-      int o = ob[0];
-      sfor<G>([&](auto gg) __attribute__((always_inline)) { if (g == gg) o = ob[gg]; });
-      return o;
-    };
-    // Biases of this lane's columns.
-    u32x2 bz[TN][4];
-    sfor<TN>([&](auto tn) __attribute__((always_inline)) {
-      const int h = gate_h(tn % HT), g = 2 * (h / BLK) + tn / HT;
-      const bf16_t *p = (const bf16_t *)a.bias + (int64_t)blk_at(g) * BLK + h % BLK + (lane >> 5) * 4;
-      sfor<4>([&](auto q) __attribute__((always_inline)) {
-        bz[tn][q] = a.bias ? *(const u32x2 *)(p + q * 8) : u32x2{0u, 0u};
-      });
-    });
+    // columns, XOR-swizzled by row, read back as 16-byte chunks.  Z, which the way
+    // back reads much later, is stored past the caches; H, which the next layer
+    // reads, is not (16384 x 16384, b = 128, 1308 us with H past them, 1289 so; 2048 x
+    // 4096 36.0, 34.6).  The output columns are kept one by one: an array of the
+    // tile's blocks, indexed here, went to private memory, and the launch took 20 us
+    // for what takes 8 (1000 x 4096).
     // Rows of COLS staged columns to memory: out(column of the wave's run) gives
     // the matrix column, or -1.
-    auto flush = [&](auto cols, bf16_t *out, int64_t ld, int tm, auto at) __attribute__((always_inline)) {
+    auto flush = [&](auto cols, auto past, bf16_t *out, int64_t ld, int tm, auto at) __attribute__((always_inline)) {
       constexpr int COLS = decltype(cols)::value, L = COLS / 8, R = 64 / L, U = COLS / 4;
       const int j = lane % L;
       const int64_t c = at(j * 8);
+      u32x4 v[32 / R];
       sfor<32 / R>([&](auto it) __attribute__((always_inline)) {
         const int rr = it * R + lane / L, sw = rr & (U < 16 ? U - 1 : 15);
-        u32x4 v = *(const u32x4 *)(stg + rr * (COLS * 2) + ((((2 * j) ^ sw) >> 1) << 4));
-        if (sw & 1) v = u32x4{v[2], v[3], v[0], v[1]};
-        const int64_t gm = m0 + wm * WTM + tm * 32 + rr;
-        if (gm < a.M && c >= 0) __builtin_nontemporal_store(v, (u32x4 *)(out + gm * ld + c));
+        v[it] = *(const u32x4 *)(stg + rr * (COLS * 2) + ((((2 * j) ^ sw) >> 1) << 4));
+        if (sw & 1) v[it] = u32x4{v[it][2], v[it][3], v[it][0], v[it][1]};
+      });
+      sfor<32 / R>([&](auto it) __attribute__((always_inline)) {
+        const int64_t gm = m0 + wm * WTM + tm * 32 + it * R + lane / L;
+        if (gm >= a.M || c < 0) return;
+        if constexpr (decltype(past)::value) __builtin_nontemporal_store(v[it], (u32x4 *)(out + gm * ld + c));
+        else *(u32x4 *)(out + gm * ld + c) = v[it];
       });
     };
-    auto put = [&](auto cols, int u, const float (&v)[4]) __attribute__((always_inline)) {
+    auto put = [&](auto cols, int u, float v0, float v1, float v2, float v3) __attribute__((always_inline)) {
       constexpr int COLS = decltype(cols)::value, U = COLS / 4;
       const int r = lane & 31;
       *(u32x2 *)(stg + r * (COLS * 2) + ((u ^ (r & (U < 16 ? U - 1 : 15))) << 3)) =
-          u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+          u32x2{pack_bf16x2(v0, v1), pack_bf16x2(v2, v3)};
     };
-    sfor<TM>([&](auto tm) __attribute__((always_inline)) {
+    if (a.mix) {
+      load_bias(a.bias != nullptr);
       sfor<TN>([&](auto tn) __attribute__((always_inline)) {
-        sfor<4>([&](auto q) __attribute__((always_inline)) {
-          float v[4];
+        sfor<TM>([&](auto tm) __attribute__((always_inline)) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[e] = acc[tn][tm][q * 4 + e];
-            if (a.mix) v[e] *= a.mix_out;
-            v[e] += __uint_as_float(e & 1 ? bz[tn][q][e / 2] & 0xffff0000u : bz[tn][q][e / 2] << 16);
-            acc[tn][tm][q * 4 + e] = v[e];
-          }
-          if (a.C2) put(std::integral_constant<int, WTN>{}, tn * 8 + q * 2 + (lane >> 5), v);
+          for (int e = 0; e < 16; ++e) acc[tn][tm][e] = __builtin_fmaf(acc[tn][tm][e], a.mix_out, bias_at(tn, e));
         });
       });
-      if (a.C2)
-        flush(std::integral_constant<int, WTN>{}, (bf16_t *)a.C2, a.ldc2, tm,
+    }
+    sfor<TM>([&](auto tm) __attribute__((always_inline)) {
+      if (a.C2) {
+        sfor<TN>([&](auto tn) __attribute__((always_inline)) {
+          sfor<4>([&](auto q) __attribute__((always_inline)) {
+            const f32x16 &x = acc[tn][tm];
+            put(std::integral_constant<int, WTN>{}, tn * 8 + q * 2 + (lane >> 5), x[q * 4], x[q * 4 + 1],
+                x[q * 4 + 2], x[q * 4 + 3]);
+          });
+        });
+        flush(std::integral_constant<int, WTN>{}, std::true_type{}, (bf16_t *)a.C2, a.ldc2, tm,
               [&](int c) __attribute__((always_inline)) -> int64_t {
-                const int h = gate_h(c / 32 % HT), g = 2 * (h / BLK) + c / 32 / HT;
-                return g < g_valid ? (int64_t)blk_at(g) * BLK + h % BLK + c % 32 : -1;
+                int64_t z = zc[0];
+                sfor<TN>([&](auto tn) __attribute__((always_inline)) { if (c / 32 == tn) z = zc[tn]; });
+                return z < 0 ? -1 : z + c % 32;
               });
+      }
       sfor<HT>([&](auto t) __attribute__((always_inline)) {
         float v[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = acc[t][tm][e];
         act_apply<bf16_t>(a.act, v);
-        sfor<4>([&](auto q) __attribute__((always_inline)) {
-          float y[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = v[q * 4 + e] * acc[HT + t][tm][q * 4 + e];
-          put(std::integral_constant<int, WTN / 2>{}, t * 8 + q * 2 + (lane >> 5), y);
+        for (int e = 0; e < 16; ++e) v[e] *= acc[HT + t][tm][e];
+        sfor<4>([&](auto q) __attribute__((always_inline)) {
+          put(std::integral_constant<int, WTN / 2>{}, t * 8 + q * 2 + (lane >> 5), v[q * 4], v[q * 4 + 1],
+              v[q * 4 + 2], v[q * 4 + 3]);
         });
       });
-      flush(std::integral_constant<int, WTN / 2>{}, C, a.ldc, tm,
+      flush(std::integral_constant<int, WTN / 2>{}, std::false_type{}, C, a.ldc, tm,
             [&](int c) __attribute__((always_inline)) -> int64_t {
-              const int h = gate_h(c / 32), g = 2 * (h / BLK);
-              return g < g_valid ? (int64_t)(blk_at(g) >> 1) * BLK + h % BLK + c % 32 : -1;
+              // The gate's block is 2 i, H's is i.
+              int64_t z = zc[0];
+              sfor<HT>([&](auto t) __attribute__((always_inline)) { if (c / 32 == t) z = zc[t]; });
+              return z < 0 ? -1 : z / (2 * BLK) * BLK + z % BLK + c % 32;
             });
     });
     return;
@@ -658,13 +690,7 @@ hipError_t ntd_go(const NTArgs &a, hipStream_t s) {
   const int64_t mtiles = (a.M + BM - 1) / BM;
   const int64_t grid = mtiles * a.ntiles * std::max(1, a.nsplit);
   if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (!DENSE && a.epi == kEpiGated) {
-    if constexpr (!DENSE && !BKN && G % 2 == 0)
-      launch_kernel(ntd_kernel<BLK, G, BKN, BM, BK, NS, NW, DENSE, 4, OCC>,
-                    dim3((unsigned)grid), dim3(64 * NW), s, a);
-    else
-      return hipErrorInvalidValue;
-  } else if (!DENSE && a.epi == kEpiAct) {
+  if (!DENSE && a.epi == kEpiAct) {
     if constexpr (!DENSE && !BKN)
       launch_kernel(ntd_kernel<BLK, G, BKN, BM, BK, NS, NW, DENSE, 3, OCC>,
                     dim3((unsigned)grid), dim3(64 * NW), s, a);
@@ -698,6 +724,31 @@ hipError_t ntd_go(const NTArgs &a, hipStream_t s) {
 // the operand bytes per flop of the 128 x 128 ones and keep two waves per
 // SIMD; the short-K variant keeps more workgroups per CU in flight when each
 // has only a few steps.
+// The gated forward's tiles: those below but for the tall ones, and 128 x 256 with
+// K-steps of 32 in three stages, two workgroups per CU.
+template <int BLK, int G, int BM, int BK, int NS, int NW, int OCC>
+hipError_t ntd_gated(const NTArgs &a, hipStream_t s) {
+  const int64_t grid = (a.M + BM - 1) / BM * a.ntiles;
+  if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
+  launch_kernel(ntd_kernel<BLK, G, false, BM, BK, NS, NW, false, 4, OCC>, dim3((unsigned)grid), dim3(64 * NW), s, a);
+  return hipGetLastError();
+}
+template <int BLK, int G>
+hipError_t ntd_gated_cfg(int variant, const NTArgs &a, hipStream_t s) {
+  constexpr int BN = G * BLK;
+  if constexpr (BN == 128) {
+    if (variant == NTD_SHORT_K) return ntd_gated<BLK, G, 128, 32, 3, 4, 3>(a, s);
+    return ntd_gated<BLK, G, 128, 64, 2, 4, 2>(a, s);
+  } else if constexpr (BN == 256) {
+    if constexpr (BLK == 128)
+      if (variant == NTD_HALF) return ntd_gated<BLK, G, 128, 32, 3, 4, 2>(a, s);
+    return ntd_gated<BLK, G, 256, 64, 2, 8, 1>(a, s);
+  } else {
+    if (variant == NTD_SHORT_K) return ntd_gated<BLK, G, 128, 64, 3, 4, 2>(a, s);
+    return ntd_gated<BLK, G, 256, 64, 2, 4, 2>(a, s);
+  }
+}
+
 template <int BLK, int G, bool BKN, bool DENSE>
 hipError_t ntd_cfg(int variant, const NTArgs &a, hipStream_t s) {
   constexpr int BN = G * BLK;
@@ -726,6 +777,10 @@ hipError_t launch_ntd_bb(int G, int variant, const NTArgs &a, hipStream_t s) {
   const bool dense = a.dense != 0;
   auto go = [&](auto g) {
     constexpr int GG = decltype(g)::value;
+    if (!dense && a.epi == kEpiGated) {
+      if constexpr (!BKN && GG % 2 == 0) return ntd_gated_cfg<BLK, GG>(variant, a, s);
+      else return hipErrorInvalidValue;
+    }
     return dense ? ntd_cfg<BLK, GG, BKN, true>(variant, a, s)
                  : ntd_cfg<BLK, GG, BKN, false>(variant, a, s);
   };

@@ -200,8 +200,9 @@ hipError_t launch_pair_scatter(const void *Wp, const int32_t *src, int npair, vo
 // The output tile is G * blk = 64, 128 or 256 columns wide (the token tile
 // follows: 256, 128, 256).  For 128-column tiles `variant` picks 512-token
 // tiles (NTD_TALL) or short K-steps with more workgroups per CU
-// (NTD_SHORT_K).
-enum { NTD_DEFAULT = 0, NTD_TALL = 1, NTD_SHORT_K = 2 };
+// (NTD_SHORT_K); for the gated forward's 256-column ones 128-token tiles
+// (NTD_HALF).
+enum { NTD_DEFAULT = 0, NTD_TALL = 1, NTD_SHORT_K = 2, NTD_HALF = 3 };
 // Per-(block size, B orientation) parts (one object file each).
 template <int BLK, bool BKN>
 hipError_t launch_ntd_bb(int G, int variant, const NTArgs &a, hipStream_t s);

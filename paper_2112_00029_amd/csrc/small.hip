@@ -351,9 +351,12 @@ hipError_t launch_small(int dtype, int blk, int G, bool b_kn, int kmax, const NT
                                   : (int64_t)nt.ntiles * (gated ? G / 2 : G) * (blk / 32);
   const int64_t grid = ((nt.M + 31) / 32) * slices;
   if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  // Eight waves once four would have eight or more steps each.
-  // (A pair's lists are split by half of them.)
-  const bool deep = (int64_t)kmax * blk * (dtype == 0 ? 2 : 4) * (gated ? 2 : 1) >= 32 * 128;
+  // Eight waves once four would have eight or more steps each.  (A pair's lists are
+  // split by half of them; past one workgroup per CU, which is what eight waves leave
+  // room for, four stay ahead: 1 x 16384 b = 128, K 1024, 24.2 -> 21.3 us, 64 x 8192
+  // 18.3 -> 15.1.)
+  const bool deep = (int64_t)kmax * blk * (dtype == 0 ? 2 : 4) * (gated ? 2 : 1) >= 32 * 128 &&
+                    !(gated && grid > 256);
   if (nt.dense) {
     if (dtype == 0) return hipErrorInvalidValue;
     return b_kn ? small_go<float, 1, true, true, 0>(a, grid, deep, s)
