@@ -23,14 +23,16 @@ struct GatedPlan {
 GatedPlan gated_plan(pf_dtype dt, int64_t T, int64_t N) {
   const int64_t chunks = N / (dt == PF_BF16 ? 8 : 4);
   GatedPlan p{};
-  // Widest workgroup row that leaves at most an eighth of its chunks idle.
-  p.cw = 64;
+  // Widest workgroup row, of 512 bytes at most, that leaves at most an eighth of its
+  // chunks idle (16384 x 16384: rows of 4096 bytes 559 us, 1024 593, 512 466, 256 523;
+  // 2100 x 4096 35.1, 22.2, 20.9, 20.6).
+  p.cw = 32;
   while (p.cw > 4 && (chunks + p.cw - 1) / p.cw * p.cw * 7 > chunks * 8) p.cw /= 2;
   p.groups = (int)((chunks + p.cw - 1) / p.cw);
   const int tall = 256 / p.cw;
-  // Eight workgroups per CU, each with at least four rows per thread.
+  // Eight workgroups per CU, each with at least two rows per thread.
   const int64_t want = std::max<int64_t>(1, 2048 / p.groups);
-  const int64_t most = std::max<int64_t>(1, T / (4 * tall));
+  const int64_t most = std::max<int64_t>(1, T / (2 * tall));
   p.rows = (T + std::min(want, most) - 1) / std::min(want, most);
   p.rows = (p.rows + tall - 1) / tall * tall;
   p.nparts = (int)((T + p.rows - 1) / p.rows);
@@ -111,8 +113,13 @@ NormPlan norm_plan(pf_dtype dt, int64_t T, int64_t N, bool wide, bool backward) 
   while (p.vec > 1 && p.chunks > 1 && (int64_t)p.tpr * p.vec * (p.chunks / 2) >= N) p.chunks /= 2;
   const int64_t rpb = p.tpr < 256 ? 256 / p.tpr : 1;
   const int64_t rows = (T + rpb - 1) / rpb;
-  const int64_t fill = 256 * (backward ? 2 : 8) * 256 / std::max(256, p.tpr);
-  p.parts = (int)std::min(rows, fill);
+  // Forward: rows in plenty per CU, so that short ones still fill memory (16384 x
+  // 4096: 8 workgroups per CU 52.5 us, 32 48.9).  Backward: two per CU, whose sums of dw
+  // and db are then few (16384 x 4096, 1 / 2 / 3 / 4 per CU: 111, 109, 114, 125 us; 16384
+  // x 1024 37, 32, 34, 37).  All of them take the same number of rows, or one less.
+  const int64_t fill = 256 * (backward ? 2 : 32) * 256 / std::max(256, p.tpr);
+  const int64_t it = (rows + fill - 1) / fill;
+  p.parts = (int)((rows + it - 1) / it);
   return p;
 }
 
@@ -165,7 +172,8 @@ size_t pf_layernorm_workspace_bytes(pf_dtype dtype, int64_t T, int64_t N) {
   // (Rows that only single-element accesses can read take the same plan or fewer
   // workgroups.)
   const NormPlan p = norm_plan(dtype, T, N, false, true), q = norm_plan(dtype, T, N, true, true);
-  return (size_t)std::max(p.parts, q.parts) * 2 * N * sizeof(float);
+  const int parts = std::max(p.parts, q.parts);
+  return parts > 1 ? (size_t)parts * 2 * N * sizeof(float) : 0;
 }
 
 pf_status pf_layernorm_bwd(pf_dtype dtype, int64_t T, int64_t N, const void *dY, int64_t lddy, const void *X,
@@ -184,13 +192,13 @@ pf_status pf_layernorm_bwd(pf_dtype dtype, int64_t T, int64_t N, const void *dY,
   const bool wide = N % vw == 0 && (T == 1 || (lddy % vw == 0 && ldx % vw == 0 && lddx % vw == 0 &&
                                                (!dR || lddr % vw == 0)));
   const NormPlan p = norm_plan(dtype, T, N, wide, true);
-  const bool sums = dweight || dbias;
-  if ((st = need_ws(sums ? (size_t)p.parts * 2 * N * sizeof(float) : 0, workspace, ws_bytes)) != PF_OK) return st;
+  const bool sums = dweight || dbias, many = p.parts > 1;
+  if ((st = need_ws(sums && many ? (size_t)p.parts * 2 * N * sizeof(float) : 0, workspace, ws_bytes)) != PF_OK) return st;
   pf::NormArgs a{};
   a.X = X; a.weight = weight; a.dY = dY; a.dR = dR; a.dX = dX;
   a.dweight = dweight; a.dbias = dbias;
   a.mean_in = mean; a.rstd_in = rstd;
-  a.partials = sums ? (float *)workspace : nullptr;
+  a.partials = sums && many ? (float *)workspace : nullptr;
   a.T = T; a.N = N; a.ldx = ldx; a.lddy = lddy; a.lddr = lddr; a.lddx = lddx;
   a.tpr = p.tpr; a.vec = p.vec; a.chunks = p.chunks; a.parts = p.parts;
   hipStream_t s = (hipStream_t)stream;
@@ -199,7 +207,7 @@ pf_status pf_layernorm_bwd(pf_dtype dtype, int64_t T, int64_t N, const void *dY,
     if ((st = hip_status(pf::launch_norm_bwd((int)dtype, a, s), "layer normalisation backward kernel")) != PF_OK)
       return st;
   }
-  if (!sums) return PF_OK;
+  if (!sums || !many) return PF_OK;
   Timed t(PF_KERNEL_REDUCE, s);
   return hip_status(pf::launch_norm_sum((int)dtype, a, s), "layer normalisation weight gradients");
 }
@@ -211,18 +219,23 @@ pf_status pf_layernorm_bwd(pf_dtype dtype, int64_t T, int64_t N, const void *dY,
 // ---------------------------------------------------------------------------
 struct pf_grads {
   std::vector<pf::GradChunk> chunks;
+  int64_t written = 0;  // bytes of the scaled gradients
   int device = -1;
   void *dev_mem = nullptr;
 };
 
 namespace {
 
-// Workgroups of the passes: up to eight per CU.
-constexpr int kGradGrid = 2048;
+// Workgroups of the passes: up to three per CU.
+constexpr int kGradGrid = 768;
+// Scaled gradients from here on are stored past the caches; fewer stay in them for
+// the optimizer.
+constexpr int64_t kGradStream = (int64_t)64 << 20;
+constexpr int64_t kGradMaxChunks = (int64_t)1 << 24;
 int grad_grid(const pf_grads *g) { return (int)std::min<size_t>(kGradGrid, std::max<size_t>(1, g->chunks.size())); }
 
 // Chunks of the tensors; "" or an error.
-std::string grad_chunks(int32_t n, const pf_grad_tensor *t, std::vector<pf::GradChunk> &out) {
+std::string grad_chunks(int32_t n, const pf_grad_tensor *t, std::vector<pf::GradChunk> &out, int64_t &written) {
   struct Span {
     uint64_t lo, hi;
     int tensor;
@@ -232,8 +245,12 @@ std::string grad_chunks(int32_t n, const pf_grad_tensor *t, std::vector<pf::Grad
   for (int32_t i = 0; i < n; ++i) {
     const std::string name = "tensor " + std::to_string(i);
     if (!type_ok(t[i].src_dtype) || !type_ok(t[i].dst_dtype)) return name + ": bad dtype";
-    if (t[i].n < 0 || t[i].n > ((int64_t)1 << 40)) return name + ": n must be in 0 .. 2^40";
+    if (t[i].n < 0) return name + ": n is negative";
     if (t[i].n == 0) continue;
+    // (2^37 elements in whole chunks; no card holds more.)
+    if (t[i].n > kGradMaxChunks * pf::kGradChunk ||
+        (int64_t)out.size() + (t[i].n + pf::kGradChunk - 1) / pf::kGradChunk > kGradMaxChunks)
+      return name + ": too many elements";
     const int ss = t[i].src_dtype == PF_BF16 ? 2 : 4, ds = t[i].dst_dtype == PF_BF16 ? 2 : 4;
     const uint64_t src = (uint64_t)(uintptr_t)t[i].src, dst = (uint64_t)(uintptr_t)t[i].dst;
     if (!src || !dst) return name + ": src or dst is NULL";
@@ -241,8 +258,8 @@ std::string grad_chunks(int32_t n, const pf_grad_tensor *t, std::vector<pf::Grad
     if (src == dst && ss != ds) return name + ": in place, but the types differ";
     if (src != dst) spans.push_back({src, src + (uint64_t)t[i].n * ss, i, false});
     spans.push_back({dst, dst + (uint64_t)t[i].n * ds, i, true});
+    written += t[i].n * ds;
     const int types = (ss == 4 ? pf::kGradSrcF32 : 0) | (ds == 4 ? pf::kGradDstF32 : 0);
-    if (out.size() + t[i].n / pf::kGradChunk >= (size_t)0x7fffffff - 2 * kGradGrid) return "too many elements";
     for (int64_t e = 0; e < t[i].n; e += pf::kGradChunk)
       out.push_back({src + e * ss, dst + e * ds, (int32_t)std::min<int64_t>(pf::kGradChunk, t[i].n - e), types});
   }
@@ -272,6 +289,7 @@ pf::GradArgs grad_args(const pf_grads *g) {
   a.chunks = (const pf::GradChunk *)g->dev_mem;
   a.nchunk = (int)g->chunks.size();
   a.nparts = grad_grid(g);
+  a.stream = g->written >= kGradStream;
   return a;
 }
 
@@ -297,7 +315,7 @@ pf_status pf_grads_create(int32_t n, const pf_grad_tensor *tensors, pf_grads **o
   if (!g) return fail(PF_ERR_NOMEM, "host allocation failed");
   std::string e;
   try {
-    e = grad_chunks(n, tensors, g->chunks);
+    e = grad_chunks(n, tensors, g->chunks, g->written);
   } catch (const std::exception &) {
     delete g;
     return fail(PF_ERR_NOMEM, "host allocation failed");

@@ -14,7 +14,9 @@
 // sums of dw and db); the next row's loads are issued before the present row is
 // worked on.  The backward's workgroups leave their sums as one row of fp32
 // partials each, added in order by a second launch: no atomics, so the same call
-// gives the same bits.
+// gives the same bits.  16384 x 4096 in bf16: forward 48.9 us, 5.5 TB/s, backward with an
+// added gradient 109 us, 4.9 TB/s (a large copy: 4.9); 2509 x 768 backward 8 us and 4
+// for the partials, launches more than memory.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -204,9 +206,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormArg
       rstd = nrstd;
     }
   }
-  if (!a.partials) return;
-  // The workgroup's sums: its row slots in order, dw then db.
-  auto leave = [&](float (&v)[C][V], float *out, bool second) __attribute__((always_inline)) {
+  // The workgroup's sums: its row slots in order, dw then db; to the partials, or the
+  // one workgroup of few rows to the results themselves.
+  auto leave = [&](float (&v)[C][V], float *part, T *out, bool second) __attribute__((always_inline)) {
     if constexpr (RPB > 1) {
       if (second) __syncthreads();
       if (slot) {
@@ -227,33 +229,41 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormArg
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = (c * TPR + i) * V;
-      if (col < N) {
+      if (col >= N) continue;
+      if (part) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) out[col + e] = v[c][e];
+        for (int e = 0; e < V; ++e) part[col + e] = v[c][e];
+      } else if (out) {
+        st_raw<T, V>(out + col, pack<T, V>(v[c]));
       }
     }
   };
-  float *P = a.partials + (int64_t)blockIdx.x * 2 * N;
-  leave(dw, P, false);
-  leave(db, P + N, true);
+  if (!a.partials && (gridDim.x > 1 || (!a.dweight && !a.dbias))) return;
+  float *P = a.partials ? a.partials + (int64_t)blockIdx.x * 2 * N : nullptr;
+  leave(dw, P, (T *)a.dweight, false);
+  leave(db, P ? P + N : P, (T *)a.dbias, true);
 }
 
 // Column sums of the partials [parts][2 N] into dw and db: 16 columns a workgroup,
-// 16 threads a column every 16th part each, added in order.
+// 64 threads a column every 64th part each, added in order.
 template <typename T>
-__global__ __launch_bounds__(256) void norm_sum_kernel(NormArgs a) {
-  __shared__ float red[256];
+__global__ __launch_bounds__(1024) void norm_sum_kernel(NormArgs a) {
+  __shared__ float red[16 * 16];
   const int64_t col = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15), n2 = 2 * a.N;
-  const int q = threadIdx.x >> 4;
+  const int q = threadIdx.x >> 4, w = threadIdx.x >> 6;
   float s = 0.f;
   if (col < n2) {
 #pragma unroll 4
-    for (int p = q; p < a.parts; p += 16) s += a.partials[(int64_t)p * n2 + col];
+    for (int p = q; p < a.parts; p += 64) s += a.partials[(int64_t)p * n2 + col];
   }
-  red[threadIdx.x] = s;
+  s += __shfl_xor(s, 16);
+  s += __shfl_xor(s, 32);
+  if ((threadIdx.x & 63) < 16) red[w * 16 + (threadIdx.x & 15)] = s;
   __syncthreads();
   if (q || col >= n2) return;
-  for (int p = 1; p < 16; ++p) s += red[p * 16 + threadIdx.x];
+  s = 0.f;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) s += red[k * 16 + threadIdx.x];
   T *out = (T *)(col < a.N ? a.dweight : a.dbias);
   if (out) down(out[col < a.N ? col : col - a.N], s);
 }
@@ -309,8 +319,8 @@ hipError_t launch_norm_bwd(int dtype, const NormArgs &a, hipStream_t s) {
 }
 hipError_t launch_norm_sum(int dtype, const NormArgs &a, hipStream_t s) {
   const unsigned grid = (unsigned)((2 * a.N + 15) / 16);
-  if (dtype == 0) launch_kernel(norm_sum_kernel<bf16_t>, dim3(grid), dim3(256), s, a);
-  else launch_kernel(norm_sum_kernel<float>, dim3(grid), dim3(256), s, a);
+  if (dtype == 0) launch_kernel(norm_sum_kernel<bf16_t>, dim3(grid), dim3(1024), s, a);
+  else launch_kernel(norm_sum_kernel<float>, dim3(grid), dim3(1024), s, a);
   return hipGetLastError();
 }
 

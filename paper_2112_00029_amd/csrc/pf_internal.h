@@ -372,6 +372,7 @@ struct GradArgs {
   double *sumsq;     // total and norm, or null
   float *norm;
   float max_norm;
+  int stream;        // store the scaled gradients past the caches
 };
 hipError_t launch_grad_sumsq(const GradArgs &a, hipStream_t s);
 hipError_t launch_grad_total(const GradArgs &a, hipStream_t s);
