@@ -331,8 +331,10 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
   const int kswitch = nsteps * BLK;
   // The switch check is a branch per K slice; launches without the mixing
   // weight run an instantiation without it (see the loop below).
-  auto compute_m = [&](Stage st, int t, auto mix) __attribute__((always_inline)) {
-    sfor<BK / 16>([&](auto ks) __attribute__((always_inline)) {
+  auto compute_m = [&](Stage st, int t, auto mix, auto half) __attribute__((always_inline)) {
+    constexpr int HALF = decltype(half)::value, KS = BK / 16;  // 0: all slices, 1, 2: a half
+    sfor<HALF ? KS / 2 : KS>([&](auto ks0) __attribute__((always_inline)) {
+      constexpr int ks = ks0 + (HALF == 2 ? KS / 2 : 0);
       constexpr int h = (ks * 16) / KW, kq = ks % (KW / 16);
       if (decltype(mix)::value && (s_begin + t) * BK + ks * 16 == kswitch) {
         sfor<TN>([&](auto tn) __attribute__((always_inline)) {
@@ -384,8 +386,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
     });
   });
   auto run = [&](auto mix) __attribute__((always_inline)) {
-    auto compute = [&](Stage st, int t) __attribute__((always_inline)) {
-      compute_m(st, t, mix);
+    auto compute = [&](Stage st, int t, auto half) __attribute__((always_inline)) {
+      compute_m(st, t, mix, half);
     };
     for (int t0 = 0; t0 < total; t0 += NS) {
       bool done = false;
@@ -409,8 +411,23 @@ __global__ __launch_bounds__(64 * NW, OCC) void ntd_kernel(NTArgs a_arg) {
           else wait_vm<0>();
         }
         barrier();
-        if (t + NS - 1 < total) issue(t + NS - 1, stage(std::integral_constant<int, (j + NS - 1) % NS>{}));
-        compute(stage(j), t);
+        const Stage next = stage(std::integral_constant<int, (j + NS - 1) % NS>{});
+        // Gated tiles of eight waves: of the two waves of a SIMD one issues the copies
+        // before its products and one in their middle, so that while one copies the
+        // other multiplies (16384 x 16384, b = 128: 1293 -> 1248 us, b = 32 824 -> 786).
+        // The products then run at the rate of a large matrix product (50 us for each
+        // 64 of K there, 1370 TFLOP/s; the chip's power sets it): fragments read a slice
+        // ahead, four waves of 128 x 128, a deeper pipeline of shorter steps or
+        // workgroups that walk over tiles gained nothing.
+        if constexpr (GATED && NW == 8) {
+          if (w < 4 && t + NS - 1 < total) issue(t + NS - 1, next);
+          compute(stage(j), t, std::integral_constant<int, 1>{});
+          if (w >= 4 && t + NS - 1 < total) issue(t + NS - 1, next);
+          compute(stage(j), t, std::integral_constant<int, 2>{});
+        } else {
+          if (t + NS - 1 < total) issue(t + NS - 1, next);
+          compute(stage(j), t, std::integral_constant<int, 0>{});
+        }
       });
     }
   };
