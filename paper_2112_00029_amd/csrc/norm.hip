@@ -43,12 +43,13 @@ __device__ __forceinline__ void load_row(const T *p, int N, int i, Raw<T, V> (&r
 template <typename T, int V, int C, int TPR>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(NormArgs a) {
   constexpr int BT = TPR < 256 ? 256 : TPR, RPB = BT / TPR;  // threads, rows at a time
-  __shared__ float box[2][2 * (BT / 64)];
+  __shared__ double dbox[BT / 64];
+  __shared__ float box[BT / 64];
   const int i = threadIdx.x % TPR, slot = threadIdx.x / TPR;
   const int N = (int)a.N;
   const T *X = (const T *)a.X;
   T *Y = (T *)a.Y;
-  const float inv = 1.0f / (float)N;
+  const double inv = 1.0 / (double)N;
   Raw<T, V> w[C], b[C];
   if (a.weight) load_row<T, V, C, TPR>((const T *)a.weight, N, i, w);
   if (a.bias) load_row<T, V, C, TPR>((const T *)a.bias, N, i, b);
@@ -59,39 +60,38 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(NormArg
   for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < a.T; t0 += step, t += step) {
     const bool live = t < a.T;
     if (t + step < a.T) load_row<T, V, C, TPR>(X + (t + step) * a.ldx, N, i, nx);
-    // Mean; then sums of x - mean and its square: the first corrects the mean's
-    // own rounding, which rows far from zero would show.
-    float d[C][V], s1[1] = {0.f}, s2[2] = {0.f, 0.f};
+    // The mean from a sum in 64 bits, as m0 + m1: rows far from zero keep the digits of
+    // their differences, and a mean near zero its own (16384 x 4096: its error 8e-8 of
+    // the means' size with fp32 sums, 3e-8, a rounding, so).
+    double sum[1] = {0.0};
+    float d[C][V], sq[1] = {0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       unpack<T, V>(x[c], d[c]);
 #pragma unroll
-      for (int e = 0; e < V; ++e) s1[0] += d[c][e];
+      for (int e = 0; e < V; ++e) sum[0] += (double)d[c][e];
     }
-    group_sum<TPR, 1>(s1, box[0]);
-    const float m0 = s1[0] * inv;
+    group_sum<TPR, 1>(sum, dbox);
+    const double mean = sum[0] * inv;
+    const float m0 = (float)mean, m1 = (float)(mean - (double)m0);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const bool in = (c * TPR + i) * V < N;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        d[c][e] = in ? d[c][e] - m0 : 0.f;
-        s2[0] += d[c][e];
-        s2[1] = __builtin_fmaf(d[c][e], d[c][e], s2[1]);
+        d[c][e] = in ? (d[c][e] - m0) - m1 : 0.f;
+        sq[0] = __builtin_fmaf(d[c][e], d[c][e], sq[0]);
       }
     }
-    group_sum<TPR, 2>(s2, box[1]);
-    const float m1 = s2[0] * inv;
-    const float var = fmaxf(__builtin_fmaf(-m1, m1, s2[1] * inv), 0.f);
-    // (fmaxf drops a NaN: the sum of squares still carries it.)
-    const float rstd = 1.0f / sqrtf((s2[1] != s2[1] ? s2[1] : var) + a.eps);
+    group_sum<TPR, 1>(sq, box);
+    const float rstd = 1.0f / sqrtf(sq[0] * (float)inv + a.eps);
     if (live) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const int col = (c * TPR + i) * V;
         float y[V], f[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) y[e] = (d[c][e] - m1) * rstd;
+        for (int e = 0; e < V; ++e) y[e] = d[c][e] * rstd;
         if (a.weight) {
           unpack<T, V>(w[c], f);
 #pragma unroll
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(NormArg
         if (col < N) st_raw<T, V>(Y + t * a.ldy + col, pack<T, V>(y));
       }
       if (i == 0) {
-        if (a.mean) a.mean[t] = m0 + m1;
+        if (a.mean) a.mean[t] = m0;
         if (a.rstd) a.rstd[t] = rstd;
       }
     }

@@ -98,11 +98,32 @@ __device__ __forceinline__ float wave_sum(float x) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
+// The same of doubles, whose halves move together.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xf, false);
+  return x + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double x) {
+  x = dpp_add<0x111, 0xf>(x);
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);
+  x = dpp_add<0x143, 0xc>(x);
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
 // Sums of NV values over groups of TPR threads (a multiple of 64), the same in
-// every thread of a group.  `box`: NV * (threads / 64) floats of LDS; a box is
+// every thread of a group.  `box`: NV * (threads / 64) of them in LDS; a box is
 // free again after the next barrier that follows.
-template <int TPR, int NV>
-__device__ __forceinline__ void group_sum(float (&v)[NV], float *box) {
+template <int TPR, int NV, typename S>
+__device__ __forceinline__ void group_sum(S (&v)[NV], S *box) {
 #pragma unroll
   for (int i = 0; i < NV; ++i) v[i] = wave_sum(v[i]);
   if constexpr (TPR > 64) {
@@ -113,9 +134,9 @@ __device__ __forceinline__ void group_sum(float (&v)[NV], float *box) {
       for (int i = 0; i < NV; ++i) box[w * NV + i] = v[i];
     }
     __syncthreads();
-    const float *g = box + w / W * W * NV;
+    const S *g = box + w / W * W * NV;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = 0.f;
+    for (int i = 0; i < NV; ++i) v[i] = 0;
 #pragma unroll
     for (int k = 0; k < W; ++k)
 #pragma unroll
