@@ -135,8 +135,8 @@ bool use_small_nt(int dtype, int blk, int G, int64_t M, int ntiles) {
 // (576: 2304 x 256); b = 128 12.6 / 29.2 (240: 640 x 384), 24.6 / 35.2 (912: 100 x 7296),
 // 35.7 / 33.1 (1836: 269 x 6528); fp32 66 / 98 (644: 1456 x 448, K lists of 960), 55.5 /
 // 65.3 (952: 1070 x 896, 640), 35.8 / 33.4 (1300: 775 x 1664, 224).
-bool use_small_gated(int dtype, int blk, int G, int64_t M, int ntiles) {
-  const int64_t wg = (M + 31) / 32 * ntiles * (G / 2) * (blk / 32);
+bool use_small_gated(int dtype, int blk, int64_t M, int npairs) {
+  const int64_t wg = (M + 31) / 32 * npairs * (blk / 32);
   return wg <= (dtype != 0 ? 1280 : blk == 32 ? 384 : blk == 64 ? 512 : 1024);
 }
 // Tiles of 128 stacked columns: short K-steps for blocks of 32 with K lists up to 416,
@@ -162,7 +162,7 @@ hipError_t nt_launch(pf_kernel_class kc, int dtype, int blk, int G, bool b_kn, i
                      const pf::NTArgs &a_in, hipStream_t s) {
   Timed t(kc, s);
   const bool gated = !a_in.dense && a_in.epi == pf::kEpiGated;
-  if (gated ? use_small_gated(dtype, blk, G, a_in.M, a_in.ntiles)
+  if (gated ? use_small_gated(dtype, blk, a_in.M, a_in.npairs)
             : !a_in.dense && use_small_nt(dtype, blk, G, a_in.M, a_in.ntiles))
     return pf::launch_small(dtype, blk, G, b_kn, kmax, a_in, s);
   pf::NTArgs a = a_in;
@@ -1227,6 +1227,9 @@ pf_status linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, c
     a.act = epi.act;
     a.ldc = L->n_out / 2;
     a.ldc2 = L->n_out;
+    a.row_ptr = L->d_row_ptr;
+    a.col_idx = L->d_col_idx;
+    a.npairs = L->nb_out / 2;
   }
   a.M = T;
   const NTList tl = gated ? gated_list(L, dt, T, r) : fwd_list(L, dt, T);

@@ -81,6 +81,10 @@ struct NTArgs {
   int ntiles;           // output column tiles (dense mode: ceil(nblk / G))
   const int32_t *kcols;
   const int32_t *blks;
+  // kEpiGated, the small-product kernel: the layout's block-CSR, by whose block rows
+  // it goes instead of the tiles.
+  const int32_t *row_ptr, *col_idx;
+  int npairs;           // pairs of block rows
   // Split of the K-steps across workgroups (dense mode only): each split
   // writes fp32 partial outputs P[split][M][ldp]; reduce_rows sums them.
   int nsplit;
