@@ -687,8 +687,9 @@ size_t pf_attn_relpos_workspace_bytes(const pf_layout *layout, const pf_relpos *
  * weight, bias: N elements of the call's dtype or NULL (one; zero).  mean, rstd: T
  * fp32 each, for the backward; either may be NULL.  Statistics are fp32, of the
  * whole row in registers: var is the mean of squared differences (a row of equal
- * elements has var 0 exactly; squares beyond fp32's range give rstd = 0).  Y may be
- * X itself with the same stride.  A NaN or infinity stays in its row.  Pointers
+ * elements has var 0 but for roundings of the mean in 64 bits; squares beyond fp32's
+ * range give rstd = 0).  mean comes from a sum in 64 bits.  Y may be X itself with the
+ * same stride; nothing else may overlap.  A NaN or infinity stays in its row.  Pointers
  * 16-byte aligned; N and strides that are multiples of 16 bytes are fastest.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP.
  */
@@ -702,7 +703,8 @@ pf_status pf_layernorm_fwd(pf_dtype dtype, int64_t T, int64_t N, float eps, cons
  *     dX = rstd (g - mean(g) - n mean(g o n)) + dR
  *     dweight = column sums of dY o n,  dbias = column sums of dY
  * dR (T x N, or NULL): a gradient that reaches X another way, as a residual stream
- * has it.  dX may be dR, dY or X itself with the same stride.  dweight and dbias (N
+ * has it.  dX may be dR, dY or X itself with the same stride; nothing else may
+ * overlap.  dweight and dbias (N
  * elements of the call's dtype): either may be NULL; summed in fp32 and a fixed
  * order; with either the call needs a workspace of pf_layernorm_workspace_bytes.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
@@ -750,7 +752,8 @@ void pf_grads_destroy(pf_grads *grads);
  * norm that is infinite or NaN scales nothing: the caller sees it in norm and drops
  * the step.  Scaled values are products in fp32, rounded once; tensors in place
  * that need no scaling are not touched.  max_norm finite and >= 0.  Workspace of
- * clip and norm: pf_grads_workspace_bytes.
+ * clip and norm: pf_grads_workspace_bytes.  Calls on one list that may overlap need
+ * workspaces of their own, and must not write the same tensors.
  * Errors: INVALID_ARG, STATE, WORKSPACE, HIP.
  */
 size_t pf_grads_workspace_bytes(const pf_grads *grads);

@@ -48,7 +48,8 @@ __global__ __launch_bounds__(256) void gated_bwd_kernel(GatedBwdArgs a) {
       rd = nd;
       rg = ng;
       ru = nu;
-      fetch(min(t + rows, t1 - 1), nd, ng, nu);  // (past the end: a row again)
+      // (Past the end: this row again, whose dZ, which may be Z, is stored below.)
+      fetch(t + rows < t1 ? t + rows : t, nd, ng, nu);
       float d[V], g[V], u[V], f[V], s[V];
       unpack<T, V>(rd, d);
       unpack<T, V>(rg, g);

@@ -529,6 +529,9 @@ def pf_grads_create(tensors) -> Grads:
 
 
 def pf_grads_upload(grads, stream=None) -> None:
+    dev = grads.tensors[0][0].device if grads.tensors else None
+    if dev is not None and (dev.type != "cuda" or dev.index != _current_device()):
+        raise ValueError(f"gradients are on {dev}, not on the GPU in use")
     _check(_lib.pf_grads_upload(grads.handle, _stream(stream)))
 
 

@@ -181,6 +181,7 @@ def _check_bwd(t, dy, x, w, mean, rstd, dr, dx, dw, db):
 @pytest.mark.parametrize("N", WIDTHS)
 def test_backward(dtype, N):
     t = torch_cuda()
+    from paper_2112_00029_amd import pixelfly as pf
     for T, pad in ((1, 0), (6, 0), (700, 0), (37, 8), (11, 3)):
         g, _, x, w, b = _inputs(t, dtype, T, N, pad, N + T)
         _, _, mean, rstd = _forward(t, dtype, x, w, b, 0)
@@ -203,6 +204,13 @@ def test_backward(dtype, N):
             assert t.equal(dx2, dx) and t.equal(dw2, dw) and t.equal(db2, db), k
         _, dx2, _, _ = _backward(t, dtype, dy, x, w, mean, rstd, dr, pad, sums=False)
         assert t.equal(dx2, dx)
+        # One of the column sums alone.
+        wsb = pf.pf_layernorm_workspace_bytes(dtype, T, N)
+        ws, ld = t.empty((wsb,), dtype=t.uint8, device="cuda"), x.stride(0) if T > 1 else N
+        for k in range(2):
+            o = [t.zeros_like(dw), None] if k == 0 else [None, t.zeros_like(db)]
+            pf.pf_layernorm_bwd(dtype, T, N, dy, ld, x, ld, w, mean, rstd, dr, ld, dx2, ld, *o, ws, wsb)
+            assert t.equal(dx2, dx) and t.equal(o[k], (dw, db)[k])
     _, dx, dw, db = _backward(t, dtype, dy, x, None, mean, rstd, None, pad)
     _check_bwd(t, dy, x, None, mean, rstd, None, dx, dw, db)
 

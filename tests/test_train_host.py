@@ -248,3 +248,6 @@ def test_gradient_tensors():
             pf.pf_grads_create(bad)
     with pytest.raises(pf.PixelflyError):
         pf.pf_grads_create([a, a])
+    # Kernels would read host memory.
+    with pytest.raises(ValueError, match="not on the GPU"):
+        pf.pf_grads_upload(pf.pf_grads_create([a]))
