@@ -690,7 +690,7 @@ size_t pf_attn_relpos_workspace_bytes(const pf_layout *layout, const pf_relpos *
  * elements has var 0 but for roundings of the mean in 64 bits; squares beyond fp32's
  * range give rstd = 0).  mean comes from a sum in 64 bits.  Y may be X itself with the
  * same stride; nothing else may overlap.  A NaN or infinity stays in its row.  Pointers
- * 16-byte aligned; N and strides that are multiples of 16 bytes are fastest.
+ * 16-byte aligned; N a multiple of 16 bytes is fastest.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP.
  */
 pf_status pf_layernorm_fwd(pf_dtype dtype, int64_t T, int64_t N, float eps, const void *X, int64_t ldx,

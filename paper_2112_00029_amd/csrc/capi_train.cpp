@@ -97,20 +97,23 @@ pf_status pf_linear_gated_bwd(pf_dtype dtype, int64_t T, int64_t N, int32_t b, p
 // ---------------------------------------------------------------------------
 namespace {
 
-// Threads per row and chunks per thread for rows of N elements, and the workgroups
-// that share T rows.
+// Threads per row and chunks of 16 bytes per thread for rows of N elements, and the
+// workgroups that share T rows.
 struct NormPlan {
-  int tpr, vec, chunks, parts;
+  int tpr, chunks, parts;
 };
-NormPlan norm_plan(pf_dtype dt, int64_t T, int64_t N, bool wide, bool backward) {
+NormPlan norm_plan(pf_dtype dt, int64_t T, int64_t N, bool backward) {
   const int vw = dt == PF_BF16 ? 8 : 4;
   NormPlan p{};
-  p.vec = wide ? vw : 1;
-  p.chunks = 16 / p.vec;
+  // 16 elements a thread; 32 for the longest rows of the backward, which keeps two sums
+  // of each: 1024 threads have too few registers and 512 workgroups of them too many
+  // partials (5000 x 16384 in bf16: 1024 threads, 128 / 256 / 512 workgroups, 224 / 163 /
+  // 186 us, 512 threads, 256 workgroups, 148; fp32 1000 x 12000 127 / 109 / 128, 60).
   p.tpr = 64;
-  while ((int64_t)p.tpr * 16 < N) p.tpr *= 2;
+  while ((int64_t)p.tpr * 16 < N && !(backward && p.tpr == 512)) p.tpr *= 2;
+  p.chunks = ((int64_t)p.tpr * 16 < N ? 32 : 16) / vw;
   // Fewer chunks where they cover the row.
-  while (p.vec > 1 && p.chunks > 1 && (int64_t)p.tpr * p.vec * (p.chunks / 2) >= N) p.chunks /= 2;
+  while (p.chunks > 1 && (int64_t)p.tpr * vw * (p.chunks / 2) >= N) p.chunks /= 2;
   const int64_t rpb = p.tpr < 256 ? 256 / p.tpr : 1;
   const int64_t rows = (T + rpb - 1) / rpb;
   // Forward: rows in plenty per CU, so that short ones still fill memory (16384 x
@@ -154,14 +157,13 @@ pf_status pf_layernorm_fwd(pf_dtype dtype, int64_t T, int64_t N, float eps, cons
       (st = check_vector(weight, "weight")) != PF_OK || (st = check_vector(bias, "bias")) != PF_OK ||
       (st = check_vector(mean, "mean")) != PF_OK || (st = check_vector(rstd, "rstd")) != PF_OK)
     return st;
-  const int vw = dtype == PF_BF16 ? 8 : 4;
-  const NormPlan p = norm_plan(dtype, T, N, N % vw == 0 && (T == 1 || (ldx % vw == 0 && ldy % vw == 0)), false);
+  const NormPlan p = norm_plan(dtype, T, N, false);
   pf::NormArgs a{};
   a.X = X; a.weight = weight; a.bias = bias; a.Y = Y;
   a.mean = mean; a.rstd = rstd;
   a.T = T; a.N = N; a.ldx = ldx; a.ldy = ldy;
   a.eps = eps;
-  a.tpr = p.tpr; a.vec = p.vec; a.chunks = p.chunks; a.parts = p.parts;
+  a.tpr = p.tpr; a.chunks = p.chunks; a.parts = p.parts;
   hipStream_t s = (hipStream_t)stream;
   Timed t(PF_KERNEL_REDUCE, s);
   return hip_status(pf::launch_norm_fwd((int)dtype, a, s), "layer normalisation kernel");
@@ -169,10 +171,7 @@ pf_status pf_layernorm_fwd(pf_dtype dtype, int64_t T, int64_t N, float eps, cons
 
 size_t pf_layernorm_workspace_bytes(pf_dtype dtype, int64_t T, int64_t N) {
   if (!type_ok(dtype) || T < 1 || T > ((int64_t)1 << 30) || N < 1 || N > pf::kNormMaxN) return 0;
-  // (Rows that only single-element accesses can read take the same plan or fewer
-  // workgroups.)
-  const NormPlan p = norm_plan(dtype, T, N, false, true), q = norm_plan(dtype, T, N, true, true);
-  const int parts = std::max(p.parts, q.parts);
+  const int parts = norm_plan(dtype, T, N, true).parts;
   return parts > 1 ? (size_t)parts * 2 * N * sizeof(float) : 0;
 }
 
@@ -188,10 +187,7 @@ pf_status pf_layernorm_bwd(pf_dtype dtype, int64_t T, int64_t N, const void *dY,
       (st = check_rows(dX, "dX", N, lddx)) != PF_OK || (st = check_vector(dweight, "dweight")) != PF_OK ||
       (st = check_vector(dbias, "dbias")) != PF_OK)
     return st;
-  const int vw = dtype == PF_BF16 ? 8 : 4;
-  const bool wide = N % vw == 0 && (T == 1 || (lddy % vw == 0 && ldx % vw == 0 && lddx % vw == 0 &&
-                                               (!dR || lddr % vw == 0)));
-  const NormPlan p = norm_plan(dtype, T, N, wide, true);
+  const NormPlan p = norm_plan(dtype, T, N, true);
   const bool sums = dweight || dbias, many = p.parts > 1;
   if ((st = need_ws(sums && many ? (size_t)p.parts * 2 * N * sizeof(float) : 0, workspace, ws_bytes)) != PF_OK) return st;
   pf::NormArgs a{};
@@ -200,7 +196,7 @@ pf_status pf_layernorm_bwd(pf_dtype dtype, int64_t T, int64_t N, const void *dY,
   a.mean_in = mean; a.rstd_in = rstd;
   a.partials = sums && many ? (float *)workspace : nullptr;
   a.T = T; a.N = N; a.ldx = ldx; a.lddy = lddy; a.lddr = lddr; a.lddx = lddx;
-  a.tpr = p.tpr; a.vec = p.vec; a.chunks = p.chunks; a.parts = p.parts;
+  a.tpr = p.tpr; a.chunks = p.chunks; a.parts = p.parts;
   hipStream_t s = (hipStream_t)stream;
   {
     Timed t(PF_KERNEL_REDUCE, s);

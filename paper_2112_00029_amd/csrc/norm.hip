@@ -6,8 +6,8 @@
 //   dw = column sums of dy o n,  db = column sums of dy
 //
 // Every element is read once and written once (the backward reads two or three
-// tensors): memory is the bound.  A row lives in the registers of TPR threads, up
-// to 16 elements each, so that mean, variance and output need no second read; the
+// tensors): memory is the bound.  A row lives in the registers of TPR threads, 16
+// elements each (32 for the backward's longest rows) or fewer, so that mean, variance and output need no second read; the
 // sums cross the wave by DPP and the waves of a row through LDS, one barrier a
 // sum.  Rows of at most 1024 elements take one wave and no barrier.  A workgroup
 // walks over rows (its weights stay in registers, and in the backward its fp32
@@ -28,20 +28,55 @@
 namespace pf {
 namespace {
 
-constexpr int kEPT = 16;  // elements of a row per thread, at most
-
+// A row's chunk from column col on lies at `from`.  Where V does not divide N (TAIL),
+// the last chunk is the row's last V elements, of which those before `first` belong to
+// the chunk before: they are loaded as zeros and not stored.  (Odd widths and strides by
+// single elements instead: backward of 184 rows of 9056, 9065 apart, 39 us for what
+// takes 18.)
+template <int V, bool TAIL>
+__device__ __forceinline__ int from(int col, int N) {
+  return TAIL ? min(col, N - V) : col;
+}
+template <int V, bool TAIL>
+__device__ __forceinline__ int first(int col, int N) {  // V: past the row
+  if constexpr (TAIL) return min(max(col - (N - V), 0), V);
+  else return col < N ? 0 : V;
+}
 // A row's raw chunks of this thread: chunk c covers columns (c TPR + i) V ...
-template <typename T, int V, int C, int TPR>
+template <typename T, int V, int C, int TPR, bool TAIL>
 __device__ __forceinline__ void load_row(const T *p, int N, int i, Raw<T, V> (&r)[C]) {
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int col = (c * TPR + i) * V;
-    r[c] = col < N ? ld_raw<T, V>(p + col) : zero_raw<T, V>();
+    r[c] = col < N ? ld_raw<T, V>(p + from<V, TAIL>(col, N)) : zero_raw<T, V>();
+    if constexpr (TAIL) {
+      const int k = first<V, TAIL>(col, N);
+      if (k > 0) {
+        float v[V];
+        unpack<T, V>(r[c], v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = e < k ? 0.f : v[e];
+        r[c] = pack<T, V>(v);
+      }
+    }
+  }
+}
+// A chunk to its place.
+template <typename T, int V, bool TAIL>
+__device__ __forceinline__ void store_chunk(T *p, int N, int col, const float (&v)[V]) {
+  const int k = first<V, TAIL>(col, N);
+  if (k == 0) {
+    st_raw<T, V>(p + col, pack<T, V>(v));
+  } else if (TAIL && k < V) {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e >= k) down(p[N - V + e], v[e]);
   }
 }
 
-template <typename T, int V, int C, int TPR>
+template <typename T, int V, int C, int TPR, bool TAIL>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(NormArgs a) {
+  constexpr auto load = load_row<T, V, C, TPR, TAIL>;
   constexpr int BT = TPR < 256 ? 256 : TPR, RPB = BT / TPR;  // threads, rows at a time
   __shared__ double dbox[BT / 64];
   __shared__ float box[BT / 64];
@@ -51,15 +86,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(NormArg
   T *Y = (T *)a.Y;
   const double inv = 1.0 / (double)N;
   Raw<T, V> w[C], b[C];
-  if (a.weight) load_row<T, V, C, TPR>((const T *)a.weight, N, i, w);
-  if (a.bias) load_row<T, V, C, TPR>((const T *)a.bias, N, i, b);
+  if (a.weight) load((const T *)a.weight, N, i, w);
+  if (a.bias) load((const T *)a.bias, N, i, b);
   const int64_t step = (int64_t)gridDim.x * RPB;
   Raw<T, V> x[C], nx[C];
   int64_t t = (int64_t)blockIdx.x * RPB + slot;
-  if (t < a.T) load_row<T, V, C, TPR>(X + t * a.ldx, N, i, x);
+  if (t < a.T) load(X + t * a.ldx, N, i, x);
   for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < a.T; t0 += step, t += step) {
     const bool live = t < a.T;
-    if (t + step < a.T) load_row<T, V, C, TPR>(X + (t + step) * a.ldx, N, i, nx);
+    if (t + step < a.T) load(X + (t + step) * a.ldx, N, i, nx);
     // The mean from a sum in 64 bits, as m0 + m1: rows far from zero keep the digits of
     // their differences, and a mean near zero its own (16384 x 4096: off by 2.6e-8 of the
     // means' size, a rounding; the 64-bit sums cost no time there, 48.2 and 48.5 us).
@@ -76,10 +111,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(NormArg
     const float m0 = (float)mean, m1 = (float)(mean - (double)m0);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const bool in = (c * TPR + i) * V < N;
+      const int k = first<V, TAIL>((c * TPR + i) * V, N);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        d[c][e] = in ? (d[c][e] - m0) - m1 : 0.f;
+        d[c][e] = (TAIL ? e >= k : k == 0) ? (d[c][e] - m0) - m1 : 0.f;
         sq[0] = __builtin_fmaf(d[c][e], d[c][e], sq[0]);
       }
     }
@@ -102,7 +137,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(NormArg
 #pragma unroll
           for (int e = 0; e < V; ++e) y[e] += f[e];
         }
-        if (col < N) st_raw<T, V>(Y + t * a.ldy + col, pack<T, V>(y));
+        store_chunk<T, V, TAIL>(Y + t * a.ldy, N, col, y);
       }
       if (i == 0) {
         if (a.mean) a.mean[t] = m0;
@@ -114,8 +149,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(NormArg
   }
 }
 
-template <typename T, int V, int C, int TPR>
+template <typename T, int V, int C, int TPR, bool TAIL>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormArgs a) {
+  constexpr auto load = load_row<T, V, C, TPR, TAIL>;
   constexpr int BT = TPR < 256 ? 256 : TPR, RPB = BT / TPR;
   __shared__ float box[2][2 * (BT / 64)];
   __shared__ float red[RPB > 1 ? (RPB - 1) * TPR * V * C : 1];
@@ -125,18 +161,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormArg
   T *dX = (T *)a.dX;
   const float inv = 1.0f / (float)N;
   Raw<T, V> w[C];
-  if (a.weight) load_row<T, V, C, TPR>((const T *)a.weight, N, i, w);
+  if (a.weight) load((const T *)a.weight, N, i, w);
   float dw[C][V] = {}, db[C][V] = {};
   const int64_t step = (int64_t)gridDim.x * RPB;
-  // (1024 threads leave 128 registers each: no room for a second row.)
-  constexpr bool AHEAD = TPR < 1024;
+  // (32 elements a thread leave no registers for a second row.)
+  constexpr bool AHEAD = V * C <= 16;
   Raw<T, V> x[C], g[C], nx[C], ng[C];
   float mean = 0.f, rstd = 0.f, nmean = 0.f, nrstd = 0.f;
   int64_t t = (int64_t)blockIdx.x * RPB + slot;
   auto fetch = [&](int64_t r, Raw<T, V> (&xx)[C], Raw<T, V> (&gg)[C], float &m, float &s)
                    __attribute__((always_inline)) {
-    load_row<T, V, C, TPR>(X + r * a.ldx, N, i, xx);
-    load_row<T, V, C, TPR>(dY + r * a.lddy, N, i, gg);
+    load(X + r * a.ldx, N, i, xx);
+    load(dY + r * a.lddy, N, i, gg);
     m = a.mean_in[r];
     s = a.rstd_in[r];
   };
@@ -147,16 +183,16 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormArg
     if (!AHEAD && live) fetch(t, x, g, mean, rstd);
     if (AHEAD && t + step < a.T) fetch(t + step, nx, ng, nmean, nrstd);
     Raw<T, V> r[C];
-    if (dR && live) load_row<T, V, C, TPR>(dR + t * a.lddr, N, i, r);
+    if (dR && live) load(dR + t * a.lddr, N, i, r);
     float s[2] = {0.f, 0.f};
     // n of a chunk (zero past the row) and dy; formed again after the sums, which
     // costs less than the registers that would keep them.
     auto norm_of = [&](int c, float (&n)[V], float (&q)[V]) __attribute__((always_inline)) {
-      const bool in = (c * TPR + i) * V < N;
+      const int k = first<V, TAIL>((c * TPR + i) * V, N);
       unpack<T, V>(x[c], n);
       unpack<T, V>(g[c], q);
 #pragma unroll
-      for (int e = 0; e < V; ++e) n[e] = in ? (n[e] - mean) * rstd : 0.f;
+      for (int e = 0; e < V; ++e) n[e] = (TAIL ? e >= k : k == 0) ? (n[e] - mean) * rstd : 0.f;
     };
     if (live) {
 #pragma unroll
@@ -193,7 +229,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormArg
 #pragma unroll
           for (int e = 0; e < V; ++e) y[e] += f[e];
         }
-        if (col < N) st_raw<T, V>(dX + t * a.lddx + col, pack<T, V>(y));
+        store_chunk<T, V, TAIL>(dX + t * a.lddx, N, col, y);
       }
     }
     if constexpr (AHEAD) {
@@ -231,10 +267,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormArg
       const int col = (c * TPR + i) * V;
       if (col >= N) continue;
       if (part) {
+        const int k = first<V, TAIL>(col, N);
 #pragma unroll
-        for (int e = 0; e < V; ++e) part[col + e] = v[c][e];
+        for (int e = 0; e < V; ++e)
+          if (!TAIL || e >= k) part[from<V, TAIL>(col, N) + e] = v[c][e];
       } else if (out) {
-        st_raw<T, V>(out + col, pack<T, V>(v[c]));
+        store_chunk<T, V, TAIL>(out, N, col, v[c]);
       }
     }
   };
@@ -268,43 +306,56 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(NormArgs a) {
   if (out) down(out[col < a.N ? col : col - a.N], s);
 }
 
-// f(V, C, TPR) of a plan.
-template <typename T, typename F>
+// f(V, C, TPR, TAIL) of a plan (capi_train.cpp).
+template <typename T, bool BACK, typename F>
 bool norm_pick(const NormArgs &a, F f) {
   constexpr int VW = 16 / sizeof(T);
-  auto tpr = [&](auto v, auto c) -> bool {
+  constexpr std::integral_constant<int, VW> v{};
+  auto tail = [&](auto c, auto t) -> bool {
+    if (a.N % VW) f(v, c, t, std::true_type{});
+    else f(v, c, t, std::false_type{});
+    return true;
+  };
+  auto tpr = [&](auto c) -> bool {
     switch (a.tpr) {
-      case 64: f(v, c, std::integral_constant<int, 64>{}); return true;
-      case 128: f(v, c, std::integral_constant<int, 128>{}); return true;
-      case 256: f(v, c, std::integral_constant<int, 256>{}); return true;
-      case 512: f(v, c, std::integral_constant<int, 512>{}); return true;
-      case 1024: f(v, c, std::integral_constant<int, 1024>{}); return true;
+      case 64: return tail(c, std::integral_constant<int, 64>{});
+      case 128: return tail(c, std::integral_constant<int, 128>{});
+      case 256: return tail(c, std::integral_constant<int, 256>{});
+      case 512: return tail(c, std::integral_constant<int, 512>{});
+      case 1024:
+        if constexpr (!BACK) return tail(c, std::integral_constant<int, 1024>{});
     }
     return false;
   };
-  if ((int64_t)a.tpr * a.chunks * a.vec < a.N) return false;
-  if (a.vec == 1) return a.chunks == kEPT && tpr(std::integral_constant<int, 1>{}, std::integral_constant<int, kEPT>{});
-  if (a.vec != VW) return false;
-  if (a.chunks == 1) return tpr(std::integral_constant<int, VW>{}, std::integral_constant<int, 1>{});
-  if (a.chunks == 2) return tpr(std::integral_constant<int, VW>{}, std::integral_constant<int, 2>{});
+  if (a.N < VW) {
+    f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 64>{},
+      std::false_type{});
+    return a.tpr == 64;
+  }
+  if ((int64_t)a.tpr * a.chunks * VW < a.N) return false;
+  if (a.chunks == 1) return tpr(std::integral_constant<int, 1>{});
+  if (a.chunks == 2) return tpr(std::integral_constant<int, 2>{});
   if constexpr (VW == 4)
-    if (a.chunks == 4) return tpr(std::integral_constant<int, VW>{}, std::integral_constant<int, 4>{});
+    if (a.chunks == 4) return tpr(std::integral_constant<int, 4>{});
+  if constexpr (BACK)
+    if (a.chunks == 32 / VW && a.tpr == 512)
+      return tail(std::integral_constant<int, 32 / VW>{}, std::integral_constant<int, 512>{});
   return false;
 }
 
 template <typename T>
 hipError_t norm_fwd(const NormArgs &a, hipStream_t s) {
-  const bool ok = norm_pick<T>(a, [&](auto v, auto c, auto t) {
+  const bool ok = norm_pick<T, false>(a, [&](auto v, auto c, auto t, auto tail) {
     constexpr int V = decltype(v)::value, C = decltype(c)::value, TPR = decltype(t)::value;
-    launch_kernel(norm_fwd_kernel<T, V, C, TPR>, dim3((unsigned)a.parts), dim3(std::max(256, TPR)), s, a);
+    launch_kernel(norm_fwd_kernel<T, V, C, TPR, decltype(tail)::value>, dim3((unsigned)a.parts), dim3(std::max(256, TPR)), s, a);
   });
   return ok ? hipGetLastError() : hipErrorInvalidValue;
 }
 template <typename T>
 hipError_t norm_bwd(const NormArgs &a, hipStream_t s) {
-  const bool ok = norm_pick<T>(a, [&](auto v, auto c, auto t) {
+  const bool ok = norm_pick<T, true>(a, [&](auto v, auto c, auto t, auto tail) {
     constexpr int V = decltype(v)::value, C = decltype(c)::value, TPR = decltype(t)::value;
-    launch_kernel(norm_bwd_kernel<T, V, C, TPR>, dim3((unsigned)a.parts), dim3(std::max(256, TPR)), s, a);
+    launch_kernel(norm_bwd_kernel<T, V, C, TPR, decltype(tail)::value>, dim3((unsigned)a.parts), dim3(std::max(256, TPR)), s, a);
   });
   return ok ? hipGetLastError() : hipErrorInvalidValue;
 }

@@ -343,8 +343,8 @@ struct GatedBwdArgs {
 };
 hipError_t launch_gated_bwd(int dtype, const GatedBwdArgs &a, hipStream_t s);
 
-// Layer normalisation (norm.hip): tpr threads per row, `chunks` chunks of `vec`
-// elements each; `parts` workgroups.  The backward's leave partials [parts][2 N]
+// Layer normalisation (norm.hip): tpr threads per row, `chunks` chunks of 16 bytes
+// each; `parts` workgroups.  The backward's leave partials [parts][2 N]
 // (dw, db), which launch_norm_sum adds.
 struct NormArgs {
   const void *X, *weight, *bias, *dY, *dR;
@@ -354,7 +354,7 @@ struct NormArgs {
   float *partials;
   int64_t T, N, ldx, ldy, lddy, lddr, lddx;
   float eps;
-  int tpr, vec, chunks, parts;
+  int tpr, chunks, parts;
 };
 constexpr int64_t kNormMaxN = 16384;
 hipError_t launch_norm_fwd(int dtype, const NormArgs &a, hipStream_t s);

@@ -26,16 +26,19 @@ struct Raw<float, 4> {
   f32x4 x;
 };
 
+// At any element's address: the hardware's 16-byte accesses need no more.
 template <typename T, int V>
 __device__ __forceinline__ Raw<T, V> ld_raw(const T *p) {
+  typedef decltype(Raw<T, V>::x) at __attribute__((aligned(sizeof(T))));
   Raw<T, V> r;
-  r.x = *(const decltype(r.x) *)p;
+  r.x = *(const at *)p;
   return r;
 }
 template <typename T, int V, bool NT = false>
 __device__ __forceinline__ void st_raw(T *p, const Raw<T, V> &r) {
-  if constexpr (NT && V > 1) __builtin_nontemporal_store(r.x, (decltype(r.x) *)p);
-  else *(decltype(r.x) *)p = r.x;
+  typedef decltype(Raw<T, V>::x) at __attribute__((aligned(sizeof(T))));
+  if constexpr (NT && V > 1) __builtin_nontemporal_store(r.x, (at *)p);
+  else *(at *)p = r.x;
 }
 
 __device__ __forceinline__ float up(bf16_t x) { return __uint_as_float((uint32_t)x << 16); }

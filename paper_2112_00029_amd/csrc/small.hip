@@ -20,8 +20,7 @@
 // and the epilogue multiplies the two sums.  It goes by the block rows of the CSR, in
 // which a row's packed blocks follow one another: no workgroup for the slots that a
 // tile of fewer rows leaves empty, and one look-up less on the way to a weight.  (fp32,
-// 256 tokens, 768 -> 2048, b = 32: 23.4 -> 19.3 us with T_lr.)  Behind an empty last row
-// the look-up meets the next list of the layout's one allocation; its value is not used.
+// 256 tokens, 768 -> 2048, b = 32: 23.4 -> 19.3 us with T_lr.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -128,9 +128,10 @@ static void norms(std::mt19937 &rng) {
     const pf::NormArgs &a = pf::g_norm;
     const int vw = dt == PF_BF16 ? 8 : 4;
     EXPECT(a.tpr == 64 || a.tpr == 128 || a.tpr == 256 || a.tpr == 512 || a.tpr == 1024);
-    EXPECT((int64_t)a.tpr * a.vec * a.chunks >= N);
-    EXPECT(a.vec == 1 ? a.chunks == 16 : a.vec == vw && (a.chunks == 1 || a.chunks == 2 || (vw == 4 && a.chunks == 4)));
-    if (a.vec > 1) EXPECT(N % vw == 0 && (T == 1 || (N + pad) % vw == 0));
+    EXPECT((int64_t)a.tpr * vw * a.chunks >= N && (N >= vw || a.tpr == 64));
+    EXPECT(a.chunks == 1 || a.chunks == 2 || (vw == 4 && a.chunks == 4) ||
+           (back && a.tpr == 512 && a.chunks == 32 / vw));
+    EXPECT(!back || a.tpr <= 512);
     EXPECT(a.parts >= 1 && a.parts <= T);
     if (back) {
       EXPECT((pf::g_sums == 1) == (sums && a.parts > 1));

@@ -98,8 +98,7 @@ def test_forward(dtype, N):
     _, y, mean, rstd = _forward(t, dtype, x, None, None, 0)
     _check_fwd(t, x, None, None, y, mean, rstd)
     want = y.clone()
-    # In place, in rows as far apart (other strides may take single elements, whose
-    # sums run in another order).
+    # In place.
     z = _rows(t, T, N, pad, x.dtype)[1].copy_(x)
     _, y, _, _ = _forward(t, dtype, z, None, None, 0, out=z)
     assert t.equal(y, want)
