@@ -7,9 +7,10 @@
 //
 // Every element is read once and written once (the backward reads two or three
 // tensors): memory is the bound.  A row lives in the registers of TPR threads, 16
-// elements each (32 for the backward's longest rows) or fewer, so that mean, variance and output need no second read; the
-// sums cross the wave by DPP and the waves of a row through LDS, one barrier a
-// sum.  Rows of at most 1024 elements take one wave and no barrier.  A workgroup
+// elements each (32 for the backward's longest rows) or fewer, so that mean, variance
+// and output need no second read; the sums cross the wave by DPP and the waves of a
+// row through LDS, one barrier a sum.  Rows of at most 1024 elements take one wave and
+// no barrier.  A workgroup
 // walks over rows (its weights stay in registers, and in the backward its fp32
 // sums of dw and db); the next row's loads are issued before the present row is
 // worked on.  The backward's workgroups leave their sums as one row of fp32
@@ -327,10 +328,11 @@ bool norm_pick(const NormArgs &a, F f) {
     }
     return false;
   };
-  if (a.N < VW) {
+  if (a.N < VW) {  // (single elements)
+    if (a.tpr != 64) return false;
     f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 64>{},
       std::false_type{});
-    return a.tpr == 64;
+    return true;
   }
   if ((int64_t)a.tpr * a.chunks * VW < a.N) return false;
   if (a.chunks == 1) return tpr(std::integral_constant<int, 1>{});
