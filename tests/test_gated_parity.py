@@ -109,7 +109,8 @@ SHAPES = [
     ("bf16", 4100, 4096, 1024, 64, 16, 128), ("bf16", 2509, 2048, 4096, 32, 32, 64),
     ("bf16", 2049, 1024, 4096, 128, 8, 256), ("bf16", 8200, 512, 512, 128, 2, 128),
     ("bf16", 3000, 512, 832, 64, 4, 64), ("bf16", 2100, 512, 1184, 32, 4, 32), ("bf16", 700, 96, 1056, 32, 1, 0),
-    ("bf16", 4500, 1024, 1088, 32, 16, 32),
+    ("bf16", 4500, 1024, 1088, 32, 16, 32), ("fp32", 1501, 512, 1024, 64, 4, 64), ("fp32", 13, 64, 32, 32, 1, 0),
+    ("bf16", 70, 32, 32, 32, 1, 32),
 ]
 
 
@@ -132,6 +133,38 @@ def test_mixed(shape, gamma):
     lay = Gated(*shape, gamma=gamma)
     h, z, _ = lay.run("gelu_tanh", gamma=gamma)
     lay.check(h, z, "gelu_tanh")
+
+
+def test_mixed_gradients():
+    """The mixed layer's gradients are the mixed calls on dZ with the gated layout:
+    dX, dW, dU, dV and the weight's own.  Sums of fp32 products, at most 2 N + r, T or,
+    of the weight's, 1024 in a row; S and T_lr are rounded to fp32 on the way."""
+    gamma, T, K, N, b, r = 0.3, 333, 256, 512, 32, 32
+    lay = Gated("fp32", T, K, N, b, 4, r, gamma=gamma)
+    t, pf = lay.t, lay.pf
+    _, _, tl = lay.run("silu", gamma=gamma)
+    gen = t.Generator(device="cuda").manual_seed(11)
+    dz = t.randn((T, 2 * N), generator=gen, device="cuda")
+    s, dx = lay.empty(r), lay.empty(K)
+    dw, dU, dV = (t.full_like(v, float("nan")) for v in (lay.w, lay.U, lay.V))
+    dg = t.full((1,), float("nan"), device="cuda")
+    ws = dict(workspace=lay.ws, ws_bytes=lay.ws_bytes)
+    pf.pf_linear_bwd_data_mixed(lay.L, "fp32", T, r, gamma, dz, lay.w, lay.U, lay.V, s, dx, **ws)
+    pf.pf_linear_bwd_weight_mixed(lay.L, "fp32", T, r, gamma, dz, lay.x, lay.w, tl, s, dw, dU, dV, dg, **ws)
+    Z, X, W, U, V = (v.double() for v in (dz, lay.x, lay.W, lay.U, lay.V))
+    i, j = np.nonzero(np.repeat(_mask(N // b, K // b, 4), 2, axis=0))
+    blocks = lambda m: m.view(2 * N // b, b, K // b, b).permute(0, 2, 1, 3)[t.from_numpy(i).cuda(), t.from_numpy(j).cuda()]
+    A = lambda v: v.abs()
+    be = 1 - gamma
+    for got, ref, mag, n in (
+            (dx, gamma * Z @ W + be * (Z @ U) @ V, gamma * A(Z) @ A(W) + be * A(Z) @ A(U) @ A(V), 4 * N + 2 * r),
+            (dw, gamma * blocks(Z.t() @ X), gamma * blocks(A(Z).t() @ A(X)), T),
+            (dU, be * Z.t() @ (X @ V.t()), be * A(Z).t() @ (A(X) @ A(V).t()), T + K),
+            (dV, be * (Z @ U).t() @ X, be * (A(Z) @ A(U)).t() @ A(X), T + 2 * N),
+            (dg, (Z * (X @ W.t() - (X @ V.t()) @ U.t())).sum(),
+             (A(Z) * (A(X) @ A(W).t() + (A(X) @ A(V).t()) @ A(U).t())).sum(), T + K + 2 * N + 1024)):
+        bad = (got.double().reshape(ref.shape) - ref).abs() - (n + 8) * E24 * mag
+        assert not (bad > 0).any() and not got.isnan().any(), float(bad.max())
 
 
 def test_other_masks():

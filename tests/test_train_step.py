@@ -106,7 +106,7 @@ class Step:
 @pytest.mark.parametrize("dtype,T,D,F,b,ms,r,act", [
     ("fp32", 70, 128, 192, 32, 4, 32, "gelu"), ("fp32", 300, 256, 512, 64, 4, 64, "silu"),
     ("bf16", 130, 256, 512, 64, 4, 64, "silu"), ("bf16", 1000, 512, 1024, 32, 8, 32, "gelu_tanh"),
-    ("bf16", 2300, 512, 1024, 128, 4, 128, "gelu")])
+    ("bf16", 2300, 512, 1024, 128, 4, 128, "gelu"), ("bf16", 4200, 1024, 1024, 32, 16, 64, "silu")])
 def test_step(dtype, T, D, F, b, ms, r, act):
     s = Step(dtype, T, D, F, b, ms, r, act)
     t = s.t
