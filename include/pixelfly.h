@@ -704,9 +704,9 @@ pf_status pf_layernorm_fwd(pf_dtype dtype, int64_t T, int64_t N, float eps, cons
  *     dweight = column sums of dY o n,  dbias = column sums of dY
  * dR (T x N, or NULL): a gradient that reaches X another way, as a residual stream
  * has it.  dX may be dR, dY or X itself with the same stride; nothing else may
- * overlap.  dweight and dbias (N
- * elements of the call's dtype): either may be NULL; summed in fp32 and a fixed
- * order; with either the call needs a workspace of pf_layernorm_workspace_bytes.
+ * overlap.  dweight and dbias (N elements of the call's dtype): either may be NULL;
+ * summed in fp32 and a fixed order; with either the call needs a workspace of
+ * pf_layernorm_workspace_bytes.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
  */
 pf_status pf_layernorm_bwd(pf_dtype dtype, int64_t T, int64_t N, const void *dY, int64_t lddy,
@@ -748,9 +748,10 @@ void pf_grads_destroy(pf_grads *grads);
  * pf_grads_scale:  the scaling alone, by a sum of squares on the device: with the
  *                  sums of several processes added up in between, the two clip
  *                  gradients that are spread over them.
- * Squares are summed in 64 bits and a fixed order (repeat calls agree bitwise).  A
- * norm that is infinite or NaN scales nothing: the caller sees it in norm and drops
- * the step.  Scaled values are products in fp32, rounded once; tensors in place
+ * Squares are summed in 64 bits and a fixed order (repeat calls agree bitwise).
+ * Gradients that are infinite or NaN scale nothing: the caller sees that in norm and
+ * drops the step.  (Finite ones whose norm passes fp32's range are scaled by it; it
+ * reads infinity.)  Scaled values are products in fp32, rounded once; tensors in place
  * that need no scaling are not touched.  max_norm finite and >= 0.  Workspace of
  * clip and norm: pf_grads_workspace_bytes.  Calls on one list that may overlap need
  * workspaces of their own, and must not write the same tensors.

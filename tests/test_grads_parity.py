@@ -121,6 +121,20 @@ def test_very_small_and_large_gradients(scale):
     _check(t, before, [x], limit, None)
 
 
+@pytest.mark.parametrize("limit", [1.0, 1e-3, 1e-6])
+def test_scale_below_the_types_normal_numbers(limit):
+    """limit / norm is 1e-40 and less: as one fp32 factor it would have lost its digits."""
+    t = torch_cuda()
+    g = t.Generator(device="cuda").manual_seed(6)
+    for dt in (t.float32, t.bfloat16):
+        x = ((t.rand((5000,), generator=g, device="cuda") + 0.1) * 3e38).to(dt)
+        y = t.zeros((5000,), device="cuda")
+        lim = float(t.tensor(limit, dtype=t.float32))
+        before = [x.clone()]
+        assert float(_clip(t, [(x, y)], lim)) == math.inf
+        _check(t, before, [y], lim, None)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 def test_no_number_scales_nothing(bad):
     t = torch_cuda()
