@@ -119,8 +119,11 @@ NormPlan norm_plan(pf_dtype dt, int64_t T, int64_t N, bool backward) {
   // Forward: rows in plenty per CU, so that short ones still fill memory (16384 x
   // 4096: 8 workgroups per CU 52.5 us, 32 48.9).  Backward: two per CU, whose sums of dw
   // and db are then few (16384 x 4096, 1 / 2 / 3 / 4 per CU: 111, 109, 114, 125 us; 16384
-  // x 1024 37, 32, 34, 37).  All of them take the same number of rows, or one less.
-  const int64_t fill = 256 * (backward ? 2 : 32) * 256 / std::max(256, p.tpr);
+  // x 1024 37, 32, 34, 37); four for many short rows (two / four: 65536 x 256 49.5 / 36.6
+  // us, 20000 x 323 19.8 / 18.4, 16384 x 512 16.6 / 17.3, 65536 x 768 86.9 / 95.4).  All
+  // of them take the same number of rows, or one less.
+  const int64_t back = N <= 512 && rows > 4096 ? 4 : 2;
+  const int64_t fill = 256 * (backward ? back : 32) * 256 / std::max(256, p.tpr);
   const int64_t it = (rows + fill - 1) / fill;
   p.parts = (int)((rows + it - 1) / it);
   return p;
