@@ -176,12 +176,14 @@ __device__ __forceinline__ void act_both(int act, const float (&x)[N], float (&f
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         if constexpr (sizeof(T) == 2) {
-          // (The clamp as in act_gelu_tanh_grad; s has its limits there.)
+          // (The clamp as in act_gelu_tanh_grad; s has its limits there.  The median
+          // of a NaN is a bound: NaN is put back.)
           const float v = x[e], z = __builtin_amdgcn_fmed3f(v, -16.f, 16.f), z2 = z * z;
           float s, c;
           act_sigmoid<T>(kTanh2k * __builtin_fmaf(kTanhC * z, z2, z), s, c);
           f[e] = v * s;
           d[e] = __builtin_fmaf(z * s * c, kTanh2k * __builtin_fmaf(3 * kTanhC, z2, 1.0f), s);
+          if (v != v) d[e] = v;
         } else {
           f[e] = act_gelu_tanh<T>(x[e]);
           d[e] = act_gelu_tanh_grad<T>(x[e]);

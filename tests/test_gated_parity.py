@@ -335,3 +335,34 @@ def test_gradients_against_differences():
         # norm here); the kernels' fp32 sums of 60 .. 384 terms below 400 2^-24 of
         # the terms' norm, taken ten times the gradient's.
         assert abs(num - got) <= (1e-6 + 4000 * E24) * float(grad.double().norm()), (k, num, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("act", ACTS)
+def test_backward_not_a_number(dtype, act):
+    """A NaN gate reaches both of its gradients (ReLU's slope there is 0 and the
+    product's without an activation 1) and a NaN factor the gate's; both reach their
+    columns' sums, and nothing else changes."""
+    t = torch_cuda()
+    dt = t.bfloat16 if dtype == "bf16" else t.float32
+    T, N, b = 5, 64, 32
+    g = t.Generator(device="cuda").manual_seed(4)
+    dh = t.randn((T, N), generator=g, device="cuda").to(dt)
+    z = t.randn((T, 2 * N), generator=g, device="cuda").to(dt)
+    want, wdb = _bwd(t, dtype, T, N, b, act, dh, z)
+    z[1, 3] = z[4, 2 * b + 7] = float("nan")  # gates of columns 3 and b + 7
+    z[2, b + 9] = float("nan")                # the other factor of column 9
+    dz, db = _bwd(t, dtype, T, N, b, act, dh, z)
+    hit = t.zeros((T, 2 * N), dtype=t.bool, device="cuda")
+    hit[1, b + 3] = hit[4, 3 * b + 7] = hit[2, 9] = True
+    if act not in ("relu", "none"):
+        hit[1, 3] = hit[4, 2 * b + 7] = True
+    assert t.equal(dz.isnan(), hit), act
+    changed = hit.clone()
+    changed[1, 3] = changed[4, 2 * b + 7] = True
+    assert t.equal(dz[~changed], want[~changed])
+    assert t.equal(db.isnan(), hit.any(0)) and t.equal(db[~changed.any(0)], wdb[~changed.any(0)])
+    if act == "relu":
+        assert dz[1, 3] == 0 and dz[4, 2 * b + 7] == 0
+    if act == "none":
+        assert dz[1, 3] == want[1, 3] and dz[4, 2 * b + 7] == want[4, 2 * b + 7]
