@@ -403,9 +403,10 @@ size_t pf_linear_act_workspace_bytes(pf_dtype dtype, int64_t T, int64_t N);
  *     H = act(Zg) o Zu                              (T x N)
  * on a layout of pf_layout_create_gated (2N = its n_out; INVALID_ARG for another).
  * bias: 2N elements or NULL.  Z receives the pre-activations for the backward; NULL
- * keeps none (serving).  PF_ACT_NONE multiplies the two projections.  Sums,
- * activation and product are fp32, of the unrounded Z; H and Z are rounded once
- * each.  No buffers may overlap.  The mixed form takes gamma as
+ * keeps none (serving).  PF_ACT_NONE multiplies the two projections.  T_lr is
+ * rounded to the call's dtype before U's product takes it, as in pf_linear_fwd (the
+ * way back reads the same numbers).  Sums, activation and product are fp32, of the
+ * unrounded Z; H and Z are rounded once each.  No buffers may overlap.  The mixed form takes gamma as
  * pf_linear_fwd_mixed does.  Workspace: pf_workspace_bytes of the layout.
  * Way back: pf_linear_gated_bwd, then pf_linear_bwd_data and pf_linear_bwd_weight
  * on the same layout with dZ for their dY.  Everything else as pf_linear_fwd.

@@ -230,6 +230,25 @@ def test_captured():
         assert t.equal(out["h"], h) and t.equal(out["z"], z)
 
 
+@pytest.mark.parametrize("shape", [("bf16", 1, 1024, 512, 64, 16, 128), ("bf16", 2509, 1024, 1024, 32, 16, 64),
+                                   ("bf16", 9000, 1024, 512, 128, 8, 256), ("fp32", 256, 768, 512, 32, 16, 32)],
+                         ids=lambda s: "-".join(map(str, s)))
+def test_z_of_the_stored_low_rank_product(shape):
+    """T_lr is one rounding from X V^T, and Z one rounding (and fp32 sums) from the
+    formula with T_lr as it is stored: nothing else is rounded on the way."""
+    lay = Gated(*shape)
+    _, z, tl = lay.run("gelu")
+    u, x, U, V = lay.u, lay.x.double(), lay.U.double(), lay.V.double()
+    ref = x @ V.t()
+    bad = (tl.double() - ref).abs() - (u * ref.abs() + (1 + u) * lay.K * E24 * (x.abs() @ V.abs().t()))
+    assert not (bad > 0).any() and not tl.isnan().any(), ("t", float(bad.max()))
+    t = tl.double()
+    ref = x @ lay.W.t() + t @ U.t() + lay.bias.double()
+    mag = x.abs() @ lay.W.abs().t() + t.abs() @ U.abs().t() + lay.bias.double().abs()
+    bad = (z.double() - ref).abs() - (u * ref.abs() + (1 + u) * (lay.K + lay.r + 4) * E24 * mag)
+    assert not (bad > 0).any() and not z.isnan().any(), ("z", float(bad.max()))
+
+
 # ---- way back ---------------------------------------------------------------
 
 def _bwd(t, dtype, T, N, b, act, dh, z, dbias=True, inplace=False):
