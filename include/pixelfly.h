@@ -275,8 +275,10 @@ pf_status pf_layout_plan_get(const pf_layout *layout, int32_t *stats,
  * 256 for the bf16 kernel whose 256 workgroups first run whole items and
  * then share the remaining items' tokens evenly) and, for the 256 tiles,
  * how many items are shared by several workgroups (their fp32 partial sums
- * added in token order by a second pass).  Errors as the compute calls'
- * argument checks: INVALID_ARG, UNSUPPORTED.
+ * added in token order by a second pass).  A gated layout reports what the plain
+ * calls run on it as the 2 n_out x n_in layer it is: T_lr and the way back are the
+ * gated layer's too, the forward is pf_linear_gated_plan_get's.  Errors as the
+ * compute calls' argument checks: INVALID_ARG, UNSUPPORTED.
  */
 typedef struct {
   int32_t lowrank_t_kernel, lowrank_t_split, lowrank_t_tile_m, lowrank_t_tile_n;
@@ -291,6 +293,21 @@ typedef struct {
 
 pf_status pf_linear_plan_get(const pf_layout *layout, pf_dtype dtype, int64_t T,
                              int32_t r, pf_linear_plan *out);
+
+/*
+ * Diagnostic: the kernel that pf_linear_gated_fwd runs for T tokens at rank r on a
+ * layout of pf_layout_create_gated (host only; the layout need not be uploaded):
+ * the family (kernels as in pf_linear_plan: 1 direct to LDS, 0 staged through
+ * registers, 2 the small-product kernel), the tokens x columns of Z that a workgroup
+ * makes, the depth of a K step and the waves of a workgroup.  Errors: INVALID_ARG
+ * (also for a layout that is not gated), UNSUPPORTED.
+ */
+typedef struct {
+  int32_t kernel, tile_m, tile_n, k_step, waves;
+} pf_linear_gated_plan;
+
+pf_status pf_linear_gated_plan_get(const pf_layout *layout, pf_dtype dtype, int64_t T,
+                                   int32_t r, pf_linear_gated_plan *out);
 
 /*
  * Copy the layout's index arrays and kernel work lists to the current HIP

@@ -135,8 +135,9 @@ bool use_small_nt(int dtype, int blk, int G, int64_t M, int ntiles) {
 // (576: 2304 x 256); b = 128 12.6 / 29.2 (240: 640 x 384), 24.6 / 35.2 (912: 100 x 7296),
 // 35.7 / 33.1 (1836: 269 x 6528); fp32 66 / 98 (644: 1456 x 448, K lists of 960), 55.5 /
 // 65.3 (952: 1070 x 896, 640), 35.8 / 33.4 (1300: 775 x 1664, 224).
+int64_t small_gated_wg(int blk, int64_t M, int npairs) { return (M + 31) / 32 * npairs * (blk / 32); }
 bool use_small_gated(int dtype, int blk, int64_t M, int npairs) {
-  const int64_t wg = (M + 31) / 32 * npairs * (blk / 32);
+  const int64_t wg = small_gated_wg(blk, M, npairs);
   return wg <= (dtype != 0 ? 1280 : blk == 32 ? 384 : blk == 64 ? 512 : 1024);
 }
 // Tiles of 128 stacked columns: short K-steps for blocks of 32 with K lists up to 416,
@@ -556,6 +557,9 @@ NTList gated_list(const pf_layout *L, int dt, int64_t T, int32_t r) {
   return NTList{false, L->G_fwd, (int)L->fwd_tiles.size(), L->kmax_fwd, L->d_fwd_tiles,
                 L->d_kcols_fwd, L->d_blks_fwd};
 }
+// Token tile of the register-staged family: pairs of 128-row blocks are 256 wide.
+int gated_bm(int b) { return b == 128 ? 64 : 128; }
+constexpr char kNotGated[] = "not a gated layout (pf_layout_create_gated)";
 NTList bwd_list(const pf_layout *L, int dt, int64_t T) {
   const bool wide = ntd_width(dt, L->b, L->G_bwd_w) && L->G_bwd_w * L->b == 256 && T >= PF_WIDE_MIN_T;
   if (wide)
@@ -1105,6 +1109,31 @@ pf_status pf_linear_plan_get(const pf_layout *L, pf_dtype dtype, int64_t T, int3
   return PF_OK;
 }
 
+pf_status pf_linear_gated_plan_get(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r,
+                                   pf_linear_gated_plan *o) {
+  if (!o) return fail(PF_ERR_INVALID_ARG, "out is NULL");
+  pf_status st = check_layout_arg(L);
+  if (st != PF_OK) return st;
+  if ((st = check_dtype_r(dtype, T, r, L->b)) != PF_OK) return st;
+  if ((st = check_extent(L, dtype, r)) != PF_OK) return st;
+  if (!L->gated) return fail(PF_ERR_INVALID_ARG, kNotGated);
+  // The decisions of linear_fwd and nt_launch.
+  const int dt = (int)dtype, b = L->b;
+  const NTList l = gated_list(L, dt, T, r);
+  const int kmax = l.kmax + r / b, npairs = L->nb_out / 2;
+  if (use_small_gated(dt, b, T, npairs)) {
+    *o = pf_linear_gated_plan{2, 32, 64, dt == PF_BF16 ? 64 : 32,
+                              pf::small_waves(dt, b, kmax, small_gated_wg(b, T, npairs), true)};
+    return PF_OK;
+  }
+  const NTChoice c = gated_choose(dt, b, l.G, gated_bm(b), kmax, T, l.ntiles);
+  // (K steps and waves: ntd_gated_cfg of gemm_dma.hip, nt_kernel.)
+  const bool shallow = !c.dma || (c.bn == 128 && c.variant == pf::NTD_SHORT_K) ||
+                       (c.bn == 256 && c.variant == pf::NTD_HALF);
+  *o = pf_linear_gated_plan{c.dma, c.bm, c.bn, shallow ? 32 : 64, c.dma && c.bm == 256 && c.bn == 256 ? 8 : 4};
+  return PF_OK;
+}
+
 }  // extern "C"
 
 namespace {
@@ -1183,7 +1212,7 @@ pf_status linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, c
   if ((st = check_extent(L, dtype, r)) != PF_OK) return st;
   const bool gated = epi.epi == pf::kEpiGated;
   if (gated && !L->gated)
-    return fail(PF_ERR_INVALID_ARG, "not a gated layout (pf_layout_create_gated)");
+    return fail(PF_ERR_INVALID_ARG, kNotGated);
   if ((st = need_ptr(X, "X")) != PF_OK || (st = need_ptr(Wblk, "Wblk")) != PF_OK ||
       (st = need_ptr(Y, gated ? "H" : "Y")) != PF_OK)
     return st;
@@ -1242,7 +1271,7 @@ pf_status linear_fwd(const pf_layout *L, pf_dtype dtype, int64_t T, int32_t r, c
   a.blks = tl.blks;
   a.nsplit = 1;
   set_mix(a, mix);
-  const int bm = gated && b == 128 ? 64 : 128;
+  const int bm = gated ? gated_bm(b) : 128;
   return hip_status(nt_launch(PF_KERNEL_SPMM_FWD, dt, b, tl.G, false, bm, tl.kmax + a.nlr, a, s),
                     "forward kernel");
 }

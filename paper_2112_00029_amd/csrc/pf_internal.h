@@ -192,6 +192,15 @@ struct SmallArgs {
 };
 hipError_t launch_small(int dtype, int blk, int G, bool b_kn, int kmax, const NTArgs &nt,
                         hipStream_t s);
+// Waves of its workgroups.  Eight once four would have eight or more steps each.  A
+// gated pair's lists are split by half of the waves: eight of them past four steps while
+// there is a workgroup per CU at most, which is what eight leave room for (1 x 4096, b =
+// 64, K 448, 10.6 -> 10.1 us; but 1 x 16384, b = 128, K 1024, 512 workgroups, 21.3 ->
+// 24.2, 64 x 8192 15.1 -> 18.3).
+inline int small_waves(int dtype, int blk, int kmax, int64_t workgroups, bool gated) {
+  const int64_t steps = (int64_t)kmax * blk * (dtype == 0 ? 2 : 4) / 128;
+  return (gated ? steps > 4 && workgroups <= 256 : steps >= 32) ? 8 : 4;
+}
 // b = 32 backward-data pairs: Wp[p] (64 x 64 bf16) from the blocks of W that
 // src[4p .. 4p + 3] name (-1: zeros).
 hipError_t launch_pair_gather(const void *W, const int32_t *src, int npair, void *Wp,

@@ -357,13 +357,7 @@ hipError_t launch_small(int dtype, int blk, int G, bool b_kn, int kmax, const NT
                                   : (gated ? nt.npairs : (int64_t)nt.ntiles * G) * (blk / 32);
   const int64_t grid = ((nt.M + 31) / 32) * slices;
   if (grid <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  // Eight waves once four would have eight or more steps each.  A pair's lists are
-  // split by half of the waves: eight of them past four steps while there is a
-  // workgroup per CU at most, which is what eight leave room for (1 x 4096, b = 64, K 448,
-  // 10.6 -> 10.1 us; but 1 x 16384, b = 128, K 1024, 512 workgroups, 21.3 -> 24.2, 64 x 8192
-  // 15.1 -> 18.3).
-  const int64_t steps = (int64_t)kmax * blk * (dtype == 0 ? 2 : 4) / 128;
-  const bool deep = gated ? steps > 4 && grid <= 256 : steps >= 32;
+  const bool deep = small_waves(dtype, blk, kmax, grid, gated) == 8;
   if (nt.dense) {
     if (dtype == 0) return hipErrorInvalidValue;
     return b_kn ? small_go<float, 1, true, true, 0>(a, grid, deep, s)

@@ -76,6 +76,10 @@ class pf_linear_plan(ctypes.Structure):
                                                        ("tn_tile", _i32), ("tn_shared", _i32)]
 
 
+class pf_linear_gated_plan(ctypes.Structure):
+    _fields_ = [(n, _i32) for n in ("kernel", "tile_m", "tile_n", "k_step", "waves")]
+
+
 _rows_p = _p  # const pf_attn_tensor *
 
 _SIGS = {
@@ -93,6 +97,7 @@ _SIGS = {
     "pf_layout_check": (_i32, [_p]),
     "pf_layout_plan_get": (_i32, [_p, ctypes.POINTER(_i32), _i32]),
     "pf_linear_plan_get": (_i32, [_p, _i32, _i64, _i32, ctypes.POINTER(pf_linear_plan)]),
+    "pf_linear_gated_plan_get": (_i32, [_p, _i32, _i64, _i32, ctypes.POINTER(pf_linear_gated_plan)]),
     "pf_layout_upload": (_i32, [_p, _p]),
     "pf_layout_destroy": (None, [_p]),
     "pf_workspace_bytes": (_sz, [_p, _i64, _i32, _i32]),
@@ -359,6 +364,13 @@ def pf_linear_plan_get(layout: Layout, dtype, T: int, r: int) -> dict:
     p = pf_linear_plan()
     _check(_lib.pf_linear_plan_get(layout.handle, _dt(dtype), T, r, ctypes.byref(p)))
     return {n: getattr(p, n) for n, _t in pf_linear_plan._fields_}
+
+
+def pf_linear_gated_plan_get(layout: Layout, dtype, T: int, r: int) -> dict:
+    """The kernel pf_linear_gated_fwd runs for T tokens at rank r."""
+    p = pf_linear_gated_plan()
+    _check(_lib.pf_linear_gated_plan_get(layout.handle, _dt(dtype), T, r, ctypes.byref(p)))
+    return {n: getattr(p, n) for n, _t in pf_linear_gated_plan._fields_}
 
 
 def pf_layout_upload(layout: Layout, stream=None) -> None:

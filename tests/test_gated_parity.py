@@ -96,9 +96,9 @@ class Gated:
         assert not (bad > 0).any() and not h.isnan().any(), ("h", act, float(bad.max()))
 
 
-# One for every kernel and tile the forward can run on: few tiles (bf16 and fp32,
-# all blocks, ragged rows, one token), 64- to 256-column tiles, tall and short-K
-# ones, 256 x 256 in bands, tiles that are not full.
+# Few tiles (bf16 and fp32, all blocks, ragged rows, one token), 64- to 256-column
+# tiles of short K steps and of long ones, tiles that are not full.  One for every kernel
+# the forward can run on: tests/test_gated_kernels.py.
 SHAPES = [
     ("bf16", 1, 256, 512, 64, 4, 64), ("bf16", 33, 320, 416, 32, 8, 32), ("bf16", 8, 512, 256, 128, 2, 0),
     ("bf16", 1, 4096, 512, 128, 32, 256), ("fp32", 1, 256, 512, 128, 2, 0),
