@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256) void gated_bwd_kernel(GatedBwdArgs a) {
 
 hipError_t launch_gated_bwd(int dtype, const GatedBwdArgs &a, hipStream_t s) {
   const int64_t grid = (int64_t)a.groups * a.nparts;
-  if (grid <= 0 || grid > 0x7fffffff || a.cw < 1 || a.cw > 64 || 256 % a.cw) return hipErrorInvalidValue;
+  if (grid <= 0 || grid > 0x7fffffff || a.cw < 1 || a.cw > 32 || 256 % a.cw) return hipErrorInvalidValue;
   auto go = [&](auto kernel) { launch_kernel(kernel, dim3((unsigned)grid), dim3(256), s, a); };
   if (dtype == 0) a.stream ? go(gated_bwd_kernel<bf16_t, true>) : go(gated_bwd_kernel<bf16_t, false>);
   else a.stream ? go(gated_bwd_kernel<float, true>) : go(gated_bwd_kernel<float, false>);

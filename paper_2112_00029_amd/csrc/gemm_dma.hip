@@ -741,8 +741,9 @@ hipError_t ntd_go(const NTArgs &a, hipStream_t s) {
 // the operand bytes per flop of the 128 x 128 ones and keep two waves per
 // SIMD; the short-K variant keeps more workgroups per CU in flight when each
 // has only a few steps.
-// The gated forward's tiles: those below but for the tall ones, and 128 x 256 with
-// K-steps of 32 in three stages, two workgroups per CU.
+// The gated forward's tiles (gated_choose of capi.cpp): those above but for the tall
+// ones; 32-deep steps for 128 columns at blocks of 32 alone; and for pairs of 128-row
+// blocks 128 x 256 with K-steps of 32 in three stages, two workgroups per CU.
 template <int BLK, int G, int BM, int BK, int NS, int NW, int OCC>
 hipError_t ntd_gated(const NTArgs &a, hipStream_t s) {
   const int64_t grid = (a.M + BM - 1) / BM * a.ntiles;
@@ -754,7 +755,8 @@ template <int BLK, int G>
 hipError_t ntd_gated_cfg(int variant, const NTArgs &a, hipStream_t s) {
   constexpr int BN = G * BLK;
   if constexpr (BN == 128) {
-    if (variant == NTD_SHORT_K) return ntd_gated<BLK, G, 128, 32, 3, 4, 3>(a, s);
+    if constexpr (BLK == 32)
+      if (variant == NTD_SHORT_K) return ntd_gated<BLK, G, 128, 32, 3, 4, 3>(a, s);
     return ntd_gated<BLK, G, 128, 64, 2, 4, 2>(a, s);
   } else if constexpr (BN == 256) {
     if constexpr (BLK == 128)

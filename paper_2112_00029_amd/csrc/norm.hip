@@ -307,27 +307,10 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(NormArgs a) {
   if (out) down(out[col < a.N ? col : col - a.N], s);
 }
 
-// f(V, C, TPR, TAIL) of a plan (capi_train.cpp).
+// f(V, C, TPR, TAIL) of a plan (capi_train.cpp): one of norm_plan_exists.
 template <typename T, bool BACK, typename F>
 bool norm_pick(const NormArgs &a, F f) {
   constexpr int VW = 16 / sizeof(T);
-  constexpr std::integral_constant<int, VW> v{};
-  auto tail = [&](auto c, auto t) -> bool {
-    if (a.N % VW) f(v, c, t, std::true_type{});
-    else f(v, c, t, std::false_type{});
-    return true;
-  };
-  auto tpr = [&](auto c) -> bool {
-    switch (a.tpr) {
-      case 64: return tail(c, std::integral_constant<int, 64>{});
-      case 128: return tail(c, std::integral_constant<int, 128>{});
-      case 256: return tail(c, std::integral_constant<int, 256>{});
-      case 512: return tail(c, std::integral_constant<int, 512>{});
-      case 1024:
-        if constexpr (!BACK) return tail(c, std::integral_constant<int, 1024>{});
-    }
-    return false;
-  };
   if (a.N < VW) {  // (single elements)
     if (a.tpr != 64) return false;
     f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 64>{},
@@ -335,14 +318,23 @@ bool norm_pick(const NormArgs &a, F f) {
     return true;
   }
   if ((int64_t)a.tpr * a.chunks * VW < a.N) return false;
-  if (a.chunks == 1) return tpr(std::integral_constant<int, 1>{});
-  if (a.chunks == 2) return tpr(std::integral_constant<int, 2>{});
-  if constexpr (VW == 4)
-    if (a.chunks == 4) return tpr(std::integral_constant<int, 4>{});
-  if constexpr (BACK)
-    if (a.chunks == 32 / VW && a.tpr == 512)
-      return tail(std::integral_constant<int, 32 / VW>{}, std::integral_constant<int, 512>{});
-  return false;
+  auto tpr = [&](auto c, auto t) -> bool {
+    if constexpr (norm_plan_exists(VW, BACK, decltype(t)::value, decltype(c)::value)) {
+      if (a.tpr != t || a.chunks != c) return false;
+      constexpr std::integral_constant<int, VW> v{};
+      if (a.N % VW) f(v, c, t, std::true_type{});
+      else f(v, c, t, std::false_type{});
+      return true;
+    }
+    return false;
+  };
+  auto chunks = [&](auto c) -> bool {
+    return tpr(c, std::integral_constant<int, 64>{}) || tpr(c, std::integral_constant<int, 128>{}) ||
+           tpr(c, std::integral_constant<int, 256>{}) || tpr(c, std::integral_constant<int, 512>{}) ||
+           tpr(c, std::integral_constant<int, 1024>{});
+  };
+  return chunks(std::integral_constant<int, 1>{}) || chunks(std::integral_constant<int, 2>{}) ||
+         chunks(std::integral_constant<int, 4>{}) || chunks(std::integral_constant<int, 8>{});
 }
 
 template <typename T>

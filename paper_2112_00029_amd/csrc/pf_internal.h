@@ -339,7 +339,7 @@ hipError_t launch_act_bwd(int dtype, const ActBwdArgs &a, hipStream_t s);
 hipError_t launch_act_dbias(int dtype, const ActBwdArgs &a, hipStream_t s);
 
 // Way back through the gated product (gated.hip): cw chunks of 16 bytes of H's
-// columns per workgroup (a power of two, at most 64), `groups` workgroups across
+// columns per workgroup (a power of two, at most 32), `groups` workgroups across
 // them, nparts parts of rows_per_part rows.  b: columns of a block.  With nparts >
 // 1 and a dbias the sums go to partials [nparts][2 N], which launch_act_dbias adds.
 struct GatedBwdArgs {
@@ -366,6 +366,13 @@ struct NormArgs {
   int tpr, chunks, parts;
 };
 constexpr int64_t kNormMaxN = 16384;
+// Plans with a kernel, of chunks of vw elements: one wave for a row of up to 16
+// elements a thread; more threads with 16 each; and the backward's longest rows.
+constexpr bool norm_plan_exists(int vw, bool backward, int tpr, int chunks) {
+  return (tpr == 64 && (chunks == 1 || chunks == 2 || chunks == 4) && chunks <= 16 / vw) ||
+         ((tpr == 128 || tpr == 256 || tpr == 512 || (tpr == 1024 && !backward)) && chunks == 16 / vw) ||
+         (backward && tpr == 512 && chunks == 32 / vw);
+}
 hipError_t launch_norm_fwd(int dtype, const NormArgs &a, hipStream_t s);
 hipError_t launch_norm_bwd(int dtype, const NormArgs &a, hipStream_t s);
 hipError_t launch_norm_sum(int dtype, const NormArgs &a, hipStream_t s);
