@@ -94,6 +94,25 @@ def test_gated_forward_state_layout_and_gamma(layout):
     assert e.value.status in (pf.PF_ERR_WORKSPACE, pf.PF_ERR_STATE)
 
 
+@pytest.mark.parametrize("dtype,T,K", [("bf16", 4096, 4096), ("bf16", 16384, 16384), ("fp32", 4096, 16384)])
+def test_gated_forward_workspace(dtype, T, K):
+    """Where T_lr's K list is split over workgroups (and has no kernel without a split),
+    its fp32 partial sums are what the call needs; refused before the layout's state."""
+    L, r = pf.pf_layout_create_gated(256, K, 128, 2), 256
+    plan = pf.pf_linear_plan_get(L, dtype, T, r)
+    need = plan["lowrank_t_split"] * T * r * 4
+    assert plan["lowrank_t_split"] > 1 and need <= pf.pf_workspace_bytes(L, T, r, dtype)
+    a = dict(dtype=dtype, T=T, r=r)
+    _refused(pf.PF_ERR_WORKSPACE, f"workspace needs {need} bytes", pf.pf_linear_gated_fwd, *_fwd(L, **a, ws_bytes=need - 1))
+    _refused(pf.PF_ERR_WORKSPACE, f"workspace needs {need} bytes", pf.pf_linear_gated_fwd,
+             *_fwd(L, **a, workspace=None, ws_bytes=0))
+    _refused(pf.PF_ERR_INVALID_ARG, "workspace is NULL", pf.pf_linear_gated_fwd, *_fwd(L, **a, workspace=None, ws_bytes=need))
+    _refused(pf.PF_ERR_INVALID_ARG, "workspace is not", pf.pf_linear_gated_fwd, *_fwd(L, **a, workspace=A + 8, ws_bytes=need))
+    _refused(pf.PF_ERR_STATE, "not uploaded", pf.pf_linear_gated_fwd, *_fwd(L, **a, ws_bytes=need))
+    b = _fwd(L, **a, ws_bytes=need - 1)
+    _refused(pf.PF_ERR_WORKSPACE, "workspace needs", pf.pf_linear_gated_fwd_mixed, *b[:4], 0.5, *b[4:])
+
+
 def _bwd(**kw):
     d = dict(dtype="bf16", T=64, N=512, b=64, act=pf.PF_ACT_SILU, dH=A, Z=A, dZ=A, dbias=A, workspace=A,
              ws_bytes=1 << 30)
