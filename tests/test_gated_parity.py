@@ -295,6 +295,13 @@ def test_backward(dtype, T, N, b):
         assert t.equal(db, db2)
 
 
+@pytest.mark.parametrize("dtype,T,N,b", [("bf16", 8193, 8192, 128), ("fp32", 4097, 8192, 64)])
+def test_backward_past_the_caches(dtype, T, N, b):
+    """dZ of 256 MiB and more takes other stores."""
+    assert 2 * T * N * (2 if dtype == "bf16" else 4) >= 256 << 20
+    test_backward(dtype, T, N, b)
+
+
 def test_backward_large_and_masked_values():
     """Gates far out, where a formula squares or exponentiates: no NaN, and the
     limits of the activations."""
